@@ -17,16 +17,19 @@ Flags:
 import os
 import subprocess
 import sys
+import tempfile
+from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libfewbit.so")
-SOURCES = [os.path.join(CSRC, "fewbit.hip"), os.path.join(CSRC, "fit.cpp")]
+SOURCES = [os.path.join(CSRC, name) for name in
+           ("fewbit.hip", "attention.hip", "qk_norm_rope.hip", "adamw.hip", "fit.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
     "-fno-gpu-flush-denormals-to-zero", "-fno-fast-math", "-ffp-contract=on",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fconstexpr-steps=200000000", "-mllvm", "-amdgpu-kernarg-preload-count=16",
@@ -35,12 +38,17 @@ FLAGS = [
 
 
 NATIVE_OUT = os.path.join(HERE, "_native.so")
-NATIVE_SOURCE = os.path.join(CSRC, "binding.cpp")
+NATIVE_SOURCES = [os.path.join(CSRC, "binding.cpp"), os.path.join(CSRC, "binding_block.cpp")]
 CXX = os.environ.get("CXX", "g++")
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    _compile([HIPCC, *FLAGS, *extra, "-o", OUT + ".tmp", *SOURCES], OUT, verbose)
+    # the sources apart and at the same time, then the library of their objects
+    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(len(SOURCES)) as pool:
+        objects = [os.path.join(d, os.path.basename(src) + ".o") for src in SOURCES]
+        list(pool.map(lambda so: _compile([HIPCC, *FLAGS, *extra, "-c", so[0], "-o", so[1] + ".tmp"], so[1], verbose),
+                      zip(SOURCES, objects)))
+        _compile([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT + ".tmp", *objects], OUT, verbose)
     if _torch_headers():
         build_native(verbose)        # links libfewbit.so, so after it
     else:
@@ -68,7 +76,7 @@ def build_native(verbose: bool = False) -> str:
               # the HIP headers ask for the platform where hipcc does not compile
               "-D__HIP_PLATFORM_AMD__=1", "-DUSE_ROCM=1",
               f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
-              *(f"-I{d}" for d in includes), "-o", NATIVE_OUT + ".tmp", NATIVE_SOURCE,
+              *(f"-I{d}" for d in includes), "-o", NATIVE_OUT + ".tmp", *NATIVE_SOURCES,
               f"-L{HERE}", "-lfewbit", f"-L{libs}", "-lc10", "-lc10_hip", "-ltorch_cpu", "-ltorch_hip",
               "-ltorch_python", "-Wl,-rpath,$ORIGIN"], NATIVE_OUT, verbose)
     return NATIVE_OUT

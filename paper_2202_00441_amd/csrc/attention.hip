@@ -1,0 +1,924 @@
+// attention.hip -- attention and its gradient on the matrix cores.
+//
+// Definitions, layouts and masks are in fewbit_block.h.
+//
+// Rows.  The query heads that share a key head are rows of one problem: row r of
+// a (sequence, key head) is head r % G of query r / G, G query heads to a key
+// head.  So keys and values are read once for all of them, and the gradients of
+// shared keys and values add up in registers, in a fixed order.
+//
+// Orientation.  A 32x32 product of the matrix cores leaves column n in lanes n
+// and n + 32, rows 8 (i / 4) + 4 (lane / 32) + i % 4 in registers i = 0..15.  The
+// scores are formed so that the axis summed over next lies in registers: S^T = K
+// Q^T (a lane is a row of Q) in the forward and for dQ, S = Q K^T (a lane is a
+// key) for dK and dV.  Then softmax statistics are one number per lane, and P
+// goes into the next product as its second operand without leaving the
+// registers: that operand holds, in lane n, eight values k = 8 (lane / 32) + j,
+// and any order of k does when both operands have the same.  The first operand
+// of the second product is V^T (or K^T, dO^T, Q^T): read from the row-major tile
+// in LDS by the transposing load, four rows at a time, in that order.
+//
+// Tiles lie in LDS row-major in 16-byte chunks, chunk c of row r at c ^ f(r): f
+// spreads both the 16-byte reads down a column of chunks and the transposing
+// reads of 4 rows x 32 bytes over all banks.
+#include <algorithm>
+
+#include "block.h"
+
+namespace {
+
+using namespace block;
+
+constexpr float kLog2e = 1.44269504088896340736f;
+
+template <int DT>
+struct Mma;
+template <>
+struct Mma<FEWBIT_BF16> {
+  using T = __bf16;
+  typedef __bf16 V8 __attribute__((ext_vector_type(8)));
+  typedef __bf16 V4 __attribute__((ext_vector_type(4)));
+  typedef float C __attribute__((ext_vector_type(16)));
+  static __device__ __forceinline__ C mul(V8 a, V8 b, C c) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, c, 0, 0, 0); }
+};
+template <>
+struct Mma<FEWBIT_F16> {
+  using T = _Float16;
+  typedef _Float16 V8 __attribute__((ext_vector_type(8)));
+  typedef _Float16 V4 __attribute__((ext_vector_type(4)));
+  typedef float C __attribute__((ext_vector_type(16)));
+  static __device__ __forceinline__ C mul(V8 a, V8 b, C c) { return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0); }
+};
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+
+struct Args {
+  const void *q, *k, *v, *dout, *out;
+  void *o, *dq, *dk, *dv;
+  float *lse, *delta;
+  float *part_o, *part_lse;           // split forward
+  const int32_t *cu_q, *cu_k, *k_len;
+  int64_t qs[3], ks[3], vs[3], ds[3];
+  int64_t rows_q, rows_k;
+  int batch, hq, hkv, g, d;           // g: query heads to a key head
+  int causal, window;
+  float scale;
+  int tiles;                          // of a sequence (packed: places for tiles of all)
+  int chunk, splits;                  // keys of a split, splits
+};
+
+// One (sequence, key head): where its rows begin and how many there are.
+struct Seq {
+  int64_t q0, k0;       // first row in the tensors (packed) or 0
+  int64_t b;            // sequence for the strides and dense layouts (packed: 0)
+  int nq, nk;
+};
+
+__device__ __forceinline__ int clamped(int x, int64_t most) { return static_cast<int>(min(static_cast<int64_t>(max(x, 0)), most)); }
+
+// Rows of packed sequence b in one of the tensors; b = batch: those past the last.
+__device__ __forceinline__ void span(const int32_t* cu, int64_t rows, int batch, int b, int& at, int& n) {
+  at = b == 0 ? 0 : clamped(cu[b], rows);
+  const int end = b == batch ? static_cast<int>(rows) : clamped(cu[b + 1], rows);
+  n = max(end - at, 0);
+}
+
+__device__ __forceinline__ Seq packed_seq(const Args& a, int b) {
+  Seq s;
+  int q0, k0;
+  span(a.cu_q, a.rows_q, a.batch, b, q0, s.nq);
+  span(a.cu_k, a.rows_k, a.batch, b, k0, s.nk);
+  s.q0 = q0;
+  s.k0 = k0;
+  s.b = 0;
+  return s;
+}
+
+// The sequence and tile that place `at` of the tiles of all sequences stands for,
+// `rows` rows (times `times`) to a tile; false past the last.  Rows of no sequence
+// come last; they see, and are seen by, nothing.
+__device__ __forceinline__ bool find_packed(const Args& a, bool keys, int times, int rows, int at, Seq& s, int& tile, int& tiles) {
+  const int lane = threadIdx.x % kWave;
+  int before = 0;
+  for (int b0 = 0; b0 <= a.batch; b0 += kWave) {
+    const int b = b0 + lane;
+    int at_b, n = 0;
+    if (b <= a.batch) span(keys ? a.cu_k : a.cu_q, keys ? a.rows_k : a.rows_q, a.batch, b, at_b, n);
+    const int own = static_cast<int>((static_cast<int64_t>(n) * times + rows - 1) / rows);
+    int sum = own;                                            // of this lane's and all before it
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+      const int other = __shfl_up(sum, step);
+      if (lane >= step) sum += other;
+    }
+    const uint64_t past = __ballot(at < before + sum);
+    if (past) {
+      const int first = __builtin_ctzll(past);
+      const int b1 = __builtin_amdgcn_readfirstlane(b0 + first);
+      tiles = __builtin_amdgcn_readfirstlane(__shfl(own, first));
+      tile = at - before - __builtin_amdgcn_readfirstlane(__shfl(sum - own, first));
+      s = packed_seq(a, b1);
+      if (b1 == a.batch) (keys ? s.nq : s.nk) = 0;
+      return true;
+    }
+    before += __builtin_amdgcn_readfirstlane(__shfl(sum, kWave - 1));
+  }
+  return false;
+}
+
+// This workgroup's key head, sequence and tile.  Neighbouring workgroups have
+// different key heads, so those of one key head, which read the same keys, run on
+// one XCD where the heads are a multiple of eight; tiles come from the last, which
+// under a causal mask see the most keys, to the first.
+__device__ __forceinline__ bool find(const Args& a, bool keys, int times, int rows, int place, Seq& s, int& tile) {
+  if (a.cu_q) {
+    int tiles;
+    if (!find_packed(a, keys, times, rows, place, s, tile, tiles)) return false;
+    tile = keys ? tile : tiles - 1 - tile;
+    return true;
+  }
+  s.b = place % a.batch;
+  tile = place / a.batch;
+  if (!keys) tile = a.tiles - 1 - tile;       // of keys the first are seen by the most rows
+  s.q0 = s.k0 = 0;
+  s.nq = static_cast<int>(a.rows_q);
+  s.nk = a.k_len ? clamped(a.k_len[s.b], a.rows_k) : static_cast<int>(a.rows_k);
+  return true;
+}
+
+template <int D>
+__device__ __forceinline__ int swizzle(int row) {
+  return D == 128 ? ((row & 7) << 1) ^ ((row >> 3) & 1) : ((row >> 1) & 3) << 1;
+}
+
+// A tile of ROWS rows of D elements in LDS, and the part of it that a thread of
+// THREADS carries there from the tensor.
+template <int DT, int D, int ROWS, int THREADS>
+struct Tile {
+  using T = typename Mma<DT>::T;
+  using V8 = typename Mma<DT>::V8;
+  static constexpr int kChunks = D / 8, kPer = ROWS * kChunks / THREADS, kStep = THREADS / kChunks;
+  static_assert(kPer >= 1 && ROWS * kChunks % THREADS == 0, "whole chunks for every thread");
+
+  u32x4 r[kPer];
+
+  // row(i): the tensor's row for row i of the tile, or null
+  template <class F>
+  __device__ __forceinline__ void fetch(int d, F row) {
+    const int c = threadIdx.x % kChunks;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const T* p = row(static_cast<int>(threadIdx.x) / kChunks + j * kStep);
+      r[j] = p && c * 8 < d ? *reinterpret_cast<const u32x4*>(p + c * 8) : u32x4{0, 0, 0, 0};
+    }
+  }
+  __device__ __forceinline__ void put(T* lds) const {
+    const int c = threadIdx.x % kChunks;
+#pragma unroll
+    for (int j = 0; j < kPer; ++j) {
+      const int row = static_cast<int>(threadIdx.x) / kChunks + j * kStep;
+      *reinterpret_cast<u32x4*>(lds + row * D + ((c ^ swizzle<D>(row)) * 8)) = r[j];
+    }
+  }
+};
+
+// First operand from rows: lane m holds row `row0 + m % 32`, elements 16 step + 8
+// (lane / 32) ..+7.
+template <int DT, int D>
+struct RowReader {
+  using T = typename Mma<DT>::T;
+  using V8 = typename Mma<DT>::V8;
+  int at;
+  __device__ __forceinline__ RowReader() {
+    const int lane = threadIdx.x % kWave, row = lane % 32;
+    at = row * D + ((lane / 32) ^ swizzle<D>(row)) * 8;
+  }
+  __device__ __forceinline__ V8 read(const T* lds, int row0, int step) const {
+    return *reinterpret_cast<const V8*>(lds + row0 * D + (at ^ (step * 16)));
+  }
+};
+
+// First operand from columns: lane m holds column 32 tile + m % 32, of the rows
+// row0 + 8 (j / 4) + 4 (lane / 32) + j % 4, j = 0..7.  Of 16 lanes that read
+// together, lane i points at four elements of row i / 4 and receives element i of
+// each row.
+template <int DT, int D>
+struct ColumnReader {
+  using T = typename Mma<DT>::T;
+  using V8 = typename Mma<DT>::V8;
+  int at;
+  __device__ __forceinline__ ColumnReader() {
+    const int lane = threadIdx.x % kWave, i = lane % 16, row = 4 * (lane / 32) + i / 4;
+    const int chunk = 2 * (lane / 16 % 2) + i % 4 / 2;
+    at = row * D + (chunk ^ swizzle<D>(row)) * 8 + i % 2 * 4;
+  }
+  __device__ __forceinline__ s16x4 four(const T* lds, int row0, int tile, int up) const {
+    // row0 is a multiple of 16; rows 8 further on have another bit of the swizzle (D = 128)
+    const int x = at ^ (tile * 32) ^ (D == 128 ? up * 8 : 0);
+    using L = __attribute__((address_space(3))) s16x4*;
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((L)(const_cast<T*>(lds) + (row0 + 8 * up) * D + x));
+  }
+  __device__ __forceinline__ V8 read(const T* lds, int row0, int tile) const {
+    const s16x4 a = four(lds, row0, tile, 0), b = four(lds, row0, tile, 1);
+    return __builtin_bit_cast(V8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+  }
+};
+
+// Second operand from registers 8 step ..+7 of a product.
+template <int DT>
+__device__ __forceinline__ typename Mma<DT>::V8 narrow(const f32x16& x, int step) {
+  typename Mma<DT>::V8 r;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) r[j] = static_cast<typename Mma<DT>::T>(x[8 * step + j]);
+  return r;
+}
+
+// A row of a tensor as second operand: elements 16 step + 8 (lane / 32) ..+7 of
+// lane's row, zeros for a row that is not there.
+template <int DT, int D>
+__device__ __forceinline__ void load_rows(const typename Mma<DT>::T* row, int d, typename Mma<DT>::V8 (&x)[D / 16]) {
+  using V8 = typename Mma<DT>::V8;
+  const int c = threadIdx.x % kWave / 32 * 8;
+#pragma unroll
+  for (int s = 0; s < D / 16; ++s) {
+    x[s] = V8{};
+    if (row && 16 * s + c < d) x[s] = *reinterpret_cast<const V8*>(row + 16 * s + c);
+  }
+}
+
+// Registers of D / 32 products whose lane is a row of the result, 32 elements each.
+template <int DT, int D>
+__device__ __forceinline__ void store_rows(typename Mma<DT>::T* row, int d, const f32x16 (&x)[D / 32], float scale) {
+  using V4 = typename Mma<DT>::V4;
+  const int c = threadIdx.x % kWave / 32 * 4;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      V4 y;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) y[j] = static_cast<typename Mma<DT>::T>(x[t][4 * u + j] * scale);
+      const int at = 32 * t + 8 * u + c;
+      if (at < d) *reinterpret_cast<V4*>(row + at) = y;
+    }
+}
+
+// The first and one past the last key that query `pos` sees.
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range keys_of(const Args& a, const Seq& s, int pos) {
+  const int64_t here = static_cast<int64_t>(pos) + s.nk - s.nq;
+  Range r{0, s.nk};
+  if (a.causal) r.hi = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(s.nk), here + 1)));
+  if (a.window) r.lo = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(s.nk), here + 1 - a.window)));
+  return r;
+}
+
+__device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + i % 4; }      // plus 4 (lane / 32)
+
+// ---------------------------------------------------------------- forward
+// Softmax statistics and output of the lane's row.
+template <int D>
+struct Running {
+  float most = -INFINITY, sum = 0.0f;       // sum: of this lane's half of the keys
+  f32x16 o[D / 32] = {};
+};
+
+// SUBS tiles of 32 keys, from row0 of the tiles in LDS and key k0 of the sequence.
+template <int DT, int D, int SUBS>
+__device__ __forceinline__ void attend(const typename Mma<DT>::T* lk, const typename Mma<DT>::T* lv, int row0, int k0,
+                                       const typename Mma<DT>::V8 (&q)[D / 16], const RowReader<DT, D>& rows,
+                                       const ColumnReader<DT, D>& columns, bool masked, Range r, float scale2, Running<D>& x) {
+  const int half = threadIdx.x % kWave / 32 * 4;
+  f32x16 s[SUBS];
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u) {
+    s[u] = f32x16{};
+#pragma unroll
+    for (int step = 0; step < D / 16; ++step) s[u] = Mma<DT>::mul(rows.read(lk, row0 + 32 * u, step), q[step], s[u]);
+  }
+  if (masked) {
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + 32 * u + key_of(i) + half;
+        if (key < r.lo || key >= r.hi) s[u][i] = -INFINITY;
+      }
+  }
+  float most = x.most;
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) most = fmaxf(most, s[u][i]);
+  const Two both = halves32(most);
+  most = fmaxf(both.a, both.b);
+  const float base = most == -INFINITY ? 0.0f : most * scale2;
+  if (__any(most != x.most)) {
+    const float fade = __builtin_amdgcn_exp2f(x.most * scale2 - base);
+    x.sum *= fade;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) x.o[t][i] *= fade;
+    x.most = most;
+  }
+  float sum = 0.0f;
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      s[u][i] = __builtin_amdgcn_exp2f(s[u][i] * scale2 - base);
+      sum += s[u][i];
+    }
+  x.sum += sum;
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u)
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      const auto p = narrow<DT>(s[u], step);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) x.o[t] = Mma<DT>::mul(columns.read(lv, row0 + 32 * u + 16 * step, t), p, x.o[t]);
+    }
+}
+
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kRowsWave = 32, kRowsGroup = kWaves * kRowsWave;      // rows of a wave and of a workgroup
+constexpr int kKeys = 64;                                           // keys of a pass
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  __shared__ __attribute__((aligned(16))) T lk[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T lv[kKeys * D];
+  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  Seq s;
+  int tile;
+  if (!find(a, false, a.g, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  const int rows = s.nq * a.g, first = tile * kRowsGroup;
+  if (first >= rows) return;
+  const int row = first + wave * kRowsWave + lane % 32;
+  const bool there = row < rows;
+  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
+  typename Mma<DT>::V8 q[D / 16];
+  load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+
+  // keys that any row of the workgroup sees, that this lane's row sees, and that
+  // all rows of the wave see
+  const Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsGroup, rows) - 1) / a.g).hi};
+  const Range own = keys_of(a, s, pos);
+  const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
+  const Range every{keys_of(a, s, max(w1, w0) / a.g).lo, keys_of(a, s, w0 / a.g).hi};
+
+  const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
+  const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
+  Tile<DT, D, kKeys, kThreads> tk, tv;
+  const auto fetch = [&](int k0) {
+    tk.fetch(a.d, [&](int i) { return k0 + i < s.nk ? kb + (k0 + i) * a.ks[1] : nullptr; });
+    tv.fetch(a.d, [&](int i) { return k0 + i < s.nk ? vb + (k0 + i) * a.vs[1] : nullptr; });
+  };
+  const RowReader<DT, D> rr;
+  const ColumnReader<DT, D> cr;
+  Running<D> x;
+  const float scale2 = a.scale * kLog2e;
+  const int begin = all.lo / kKeys * kKeys;
+  if (begin < all.hi) fetch(begin);
+  for (int k0 = begin; k0 < all.hi; k0 += kKeys) {
+    __syncthreads();
+    tk.put(lk);
+    tv.put(lv);
+    if (k0 + kKeys < all.hi) fetch(k0 + kKeys);
+    __syncthreads();
+    attend<DT, D, kKeys / 32>(lk, lv, 0, k0, q, rr, cr, k0 < every.lo || k0 + kKeys > every.hi, own, scale2, x);
+  }
+  if (!there) return;
+  const Two both = halves32(x.sum);
+  const float sum = both.a + both.b;
+  store_rows<DT, D>(static_cast<T*>(a.o) + ((s.b * a.rows_q + s.q0 + pos) * a.hq + head) * a.d, a.d, x.o, sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f);
+  if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = sum == 0.0f ? -INFINITY : x.most * a.scale + logf(sum);
+}
+
+// Few rows over many keys (single tokens over a cache): a workgroup takes 32 rows
+// and one run of keys, and its waves different keys of each pass, whose results
+// they add up at the end.  Runs' results are added by a second kernel.
+constexpr int kKeysSplit = 32 * kWaves;
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  __shared__ __attribute__((aligned(16))) char lds[2 * kKeysSplit * D * sizeof(T)];
+  T *lk = reinterpret_cast<T*>(lds), *lv = lk + kKeysSplit * D;
+  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int split = blockIdx.x / a.hkv % a.splits;
+  Seq s;
+  int tile;
+  if (!find(a, false, a.g, kRowsWave, blockIdx.x / a.hkv / a.splits, s, tile)) return;
+  const int rows = s.nq * a.g, first = tile * kRowsWave;
+  if (first >= rows) return;
+  const int row = first + lane % 32;
+  const bool there = row < rows;
+  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
+  const Range own = keys_of(a, s, pos);
+  const Range every{keys_of(a, s, (min(first + kRowsWave, rows) - 1) / a.g).lo, keys_of(a, s, first / a.g).hi};
+  Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsWave, rows) - 1) / a.g).hi};
+  all.lo = max(all.lo, split * a.chunk);
+  all.hi = static_cast<int>(min(static_cast<int64_t>(all.hi), (split + static_cast<int64_t>(1)) * a.chunk));
+  const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head;           // the row in dense layouts
+  Running<D> x;
+  if (all.lo < all.hi) {
+    typename Mma<DT>::V8 q[D / 16];
+    load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+    const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
+    const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
+    Tile<DT, D, kKeysSplit, kThreads> tk, tv;
+    const auto fetch = [&](int k0) {
+      tk.fetch(a.d, [&](int i) { return k0 + i < all.hi ? kb + (k0 + i) * a.ks[1] : nullptr; });
+      tv.fetch(a.d, [&](int i) { return k0 + i < all.hi ? vb + (k0 + i) * a.vs[1] : nullptr; });
+    };
+    const RowReader<DT, D> rr;
+    const ColumnReader<DT, D> cr;
+    const Range mine{max(own.lo, all.lo), min(own.hi, all.hi)};
+    const Range sure{max(every.lo, all.lo), min(every.hi, all.hi)};
+    const int begin = all.lo / kKeysSplit * kKeysSplit;
+    fetch(begin);
+    for (int k0 = begin; k0 < all.hi; k0 += kKeysSplit) {
+      __syncthreads();
+      tk.put(lk);
+      tv.put(lv);
+      if (k0 + kKeysSplit < all.hi) fetch(k0 + kKeysSplit);
+      __syncthreads();
+      const int kw = k0 + 32 * wave;
+      attend<DT, D, 1>(lk, lv, 32 * wave, kw, q, rr, cr, kw < sure.lo || kw + 32 > sure.hi, mine, a.scale * kLog2e, x);
+    }
+    // the waves' results: statistics, then outputs one after another
+    __syncthreads();
+    float* stats = reinterpret_cast<float*>(lds);           // [wave][2][32]
+    const Two both = halves32(x.sum);
+    x.sum = both.a + both.b;
+    if (lane < 32) {
+      stats[wave * 64 + lane] = x.most;
+      stats[wave * 64 + 32 + lane] = x.sum;
+    }
+    __syncthreads();
+    float most = -INFINITY;
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[w * 64 + lane % 32]);
+    const float base = most == -INFINITY ? 0.0f : most;
+    const float scale2 = a.scale * kLog2e;
+    float sum = 0.0f;
+    for (int w = 0; w < kWaves; ++w)
+      sum += stats[w * 64 + 32 + lane % 32] * __builtin_amdgcn_exp2f((stats[w * 64 + lane % 32] - base) * scale2);
+    const float fade = __builtin_amdgcn_exp2f((x.most - base) * scale2);
+    x.most = most;
+    x.sum = sum;
+    __syncthreads();
+    float* acc = reinterpret_cast<float*>(lds);             // [register][lane]
+    for (int w = 1; w < kWaves; ++w) {
+      if (wave == w) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[(t * 16 + i) * kWave + lane] = x.o[t][i] * fade;
+      }
+      __syncthreads();
+      if (wave == 0) {
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) x.o[t][i] = (w == 1 ? x.o[t][i] * fade : x.o[t][i]) + acc[(t * 16 + i) * kWave + lane];
+      }
+      __syncthreads();
+    }
+  }
+  if (wave != 0 || !there) return;
+  const float inverse = x.sum > 0.0f || x.sum != x.sum ? 1.0f / x.sum : 0.0f;
+  const float lse = x.sum == 0.0f ? -INFINITY : x.most * a.scale + logf(x.sum);
+  if (a.splits == 1) {
+    store_rows<DT, D>(static_cast<T*>(a.o) + at * a.d, a.d, x.o, inverse);
+    if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = lse;
+    return;
+  }
+  const int64_t part = at * a.splits + split;
+  if (lane < 32) a.part_lse[part] = lse;
+  if (lse == -INFINITY) return;                             // its output is not read
+  float* out = a.part_o + part * a.d;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int c = 32 * t + 8 * u + lane / 32 * 4;
+      if (c < a.d)
+        *reinterpret_cast<f32x4*>(out + c) = f32x4{x.o[t][4 * u], x.o[t][4 * u + 1], x.o[t][4 * u + 2], x.o[t][4 * u + 3]} * inverse;
+    }
+}
+
+// out = sum of the runs' outputs, each by its share exp(lse_run - lse); a wave takes
+// a row, two elements a lane.
+template <int DT>
+__global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  const int lane = threadIdx.x % kWave;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;
+  const int64_t rows = a.batch * a.rows_q;
+  if (at >= rows * a.hq) return;
+  const float* lse = a.part_lse + at * a.splits;
+  float most = -INFINITY;
+  for (int i = lane; i < a.splits; i += kWave) most = fmaxf(most, lse[i]);
+  most = across<6>(most, [](float x, float y) { return fmaxf(x, y); });
+  const float base = most == -INFINITY ? 0.0f : most;
+  float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
+  for (int i = 0; i < a.splits; ++i) {
+    const float w = __builtin_amdgcn_exp2f((lse[i] - base) * kLog2e);
+    sum += w;
+    if (lse[i] != -INFINITY && 2 * lane < a.d) {
+      const float* o = a.part_o + (at * a.splits + i) * a.d + 2 * lane;
+      o0 += w * o[0];
+      o1 += w * o[1];
+    }
+  }
+  const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  if (2 * lane < a.d) {
+    T* out = static_cast<T*>(a.o) + at * a.d + 2 * lane;
+    out[0] = static_cast<T>(o0 * inverse);
+    out[1] = static_cast<T>(o1 * inverse);
+  }
+  const int64_t row = at / a.hq, head = at % a.hq, b = row / a.rows_q;
+  if (lane == 0) a.lse[(b * a.hq + head) * a.rows_q + row % a.rows_q] = sum == 0.0f ? -INFINITY : base + logf(sum);
+}
+
+// ---------------------------------------------------------------- backward
+// With P from lse, delta_i = <dO_i, O_i>, dP = dO V^T and dS = P (dP - delta):
+//   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
+// dQ needs all keys of a row and dK, dV all rows of a key: one kernel for each,
+// both of which form S and dP (seven products where five would do, but no sums
+// across workgroups: nothing is added atomically, and no gradient waits in memory).
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  using V8 = typename Mma<DT>::V8;
+  __shared__ __attribute__((aligned(16))) T lk[kKeys * D];
+  __shared__ __attribute__((aligned(16))) T lv[kKeys * D];
+  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  Seq s;
+  int tile;
+  if (!find(a, false, a.g, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  const int rows = s.nq * a.g, first = tile * kRowsGroup;
+  if (first >= rows) return;
+  const int row = first + wave * kRowsWave + lane % 32;
+  const bool there = row < rows;
+  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
+  const int64_t at = ((s.b * a.rows_q + s.q0 + pos) * a.hq + head) * a.d;
+  const int64_t stat = (s.b * a.hq + head) * a.rows_q + s.q0 + pos;
+  V8 q[D / 16], dout[D / 16];
+  load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+  load_rows<DT, D>(there ? static_cast<const T*>(a.dout) + s.b * a.ds[0] + (s.q0 + pos) * a.ds[1] + head * a.ds[2] : nullptr, a.d, dout);
+  float delta = 0.0f;
+  {
+    V8 o[D / 16];
+    load_rows<DT, D>(there ? static_cast<const T*>(a.out) + at : nullptr, a.d, o);
+#pragma unroll
+    for (int i = 0; i < D / 16; ++i)
+#pragma unroll
+      for (int j = 0; j < 8; ++j) delta += static_cast<float>(o[i][j]) * static_cast<float>(dout[i][j]);
+    const Two both = halves32(delta);
+    delta = both.a + both.b;
+  }
+  if (there && lane < 32) a.delta[stat] = delta;
+  float lse = there ? a.lse[stat] : -INFINITY;
+  lse = lse == -INFINITY ? INFINITY : lse * kLog2e;           // of an empty row no key is seen
+
+  const Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsGroup, rows) - 1) / a.g).hi};
+  const Range own = keys_of(a, s, pos);
+  const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
+  const Range every{keys_of(a, s, max(w1, w0) / a.g).lo, keys_of(a, s, w0 / a.g).hi};
+
+  const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
+  const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
+  Tile<DT, D, kKeys, kThreads> tk, tv;
+  const auto fetch = [&](int k0) {
+    tk.fetch(a.d, [&](int i) { return k0 + i < s.nk ? kb + (k0 + i) * a.ks[1] : nullptr; });
+    tv.fetch(a.d, [&](int i) { return k0 + i < s.nk ? vb + (k0 + i) * a.vs[1] : nullptr; });
+  };
+  const RowReader<DT, D> rr;
+  const ColumnReader<DT, D> cr;
+  f32x16 dq[D / 32] = {};
+  const float scale2 = a.scale * kLog2e;
+  const int begin = all.lo / kKeys * kKeys;
+  if (begin < all.hi) fetch(begin);
+  for (int k0 = begin; k0 < all.hi; k0 += kKeys) {
+    __syncthreads();
+    tk.put(lk);
+    tv.put(lv);
+    if (k0 + kKeys < all.hi) fetch(k0 + kKeys);
+    __syncthreads();
+    const bool masked = k0 < every.lo || k0 + kKeys > every.hi;
+#pragma unroll
+    for (int u = 0; u < kKeys / 32; ++u) {
+      f32x16 p = {}, dp = {};
+#pragma unroll
+      for (int step = 0; step < D / 16; ++step) {
+        p = Mma<DT>::mul(rr.read(lk, 32 * u, step), q[step], p);
+        dp = Mma<DT>::mul(rr.read(lv, 32 * u, step), dout[step], dp);
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - lse);
+        if (masked) {
+          const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
+          if (key < own.lo || key >= own.hi) p[i] = 0.0f;
+        }
+        p[i] *= dp[i] - delta;
+      }
+#pragma unroll
+      for (int step = 0; step < 2; ++step) {
+        const V8 ds = narrow<DT>(p, step);
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(lk, 32 * u + 16 * step, t), ds, dq[t]);
+      }
+    }
+  }
+  if (there) store_rows<DT, D>(static_cast<T*>(a.dq) + at, a.d, dq, a.scale);
+}
+
+constexpr int kRowsPass = 32;       // rows of a pass of the dK, dV kernel
+
+template <int DT, int D>
+__global__ __launch_bounds__(kThreads, 1) void attn_dkv_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  using V8 = typename Mma<DT>::V8;
+  __shared__ __attribute__((aligned(16))) T lq[kRowsPass * D];
+  __shared__ __attribute__((aligned(16))) T ld[kRowsPass * D];
+  __shared__ __attribute__((aligned(16))) float stats[2][kRowsPass];
+  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  Seq s;
+  int tile;
+  if (!find(a, true, 1, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  // keys past those that are there have gradients too: zeros
+  const int keys = a.cu_k ? (s.nk > 0 ? s.nk : 0) : static_cast<int>(a.rows_k), first = tile * kRowsGroup;
+  if (first >= keys) return;
+  const int key = first + wave * kRowsWave + lane % 32;
+  const bool there = key < s.nk;
+  V8 k[D / 16], v[D / 16];
+  load_rows<DT, D>(there ? static_cast<const T*>(a.k) + s.b * a.ks[0] + (s.k0 + key) * a.ks[1] + hk * a.ks[2] : nullptr, a.d, k);
+  load_rows<DT, D>(there ? static_cast<const T*>(a.v) + s.b * a.vs[0] + (s.k0 + key) * a.vs[1] + hk * a.vs[2] : nullptr, a.d, v);
+
+  // rows (query * G + head) that see a key: from lo to before hi
+  const int rows = s.nq * a.g;
+  const auto rows_of = [&](int j) {
+    const int64_t here = static_cast<int64_t>(j) - s.nk + s.nq;        // the query that stands at key j
+    Range r{0, rows};
+    if (a.causal) r.lo = static_cast<int>(max(static_cast<int64_t>(0), min(here * a.g, static_cast<int64_t>(rows))));
+    if (a.window) r.hi = static_cast<int>(max(static_cast<int64_t>(0), min((here + a.window) * a.g, static_cast<int64_t>(rows))));
+    if (j >= s.nk) r.hi = 0;
+    return r;
+  };
+  const int last = min(first + kRowsGroup, s.nk) - 1;
+  Range all{0, 0};
+  if (first < s.nk) all = Range{rows_of(first).lo, rows_of(last).hi};
+  const Range own = rows_of(key);
+  const int w0 = first + wave * kRowsWave, w1 = w0 + kRowsWave - 1;
+  const Range every{rows_of(w1).lo, w1 < s.nk ? rows_of(w0).hi : 0};
+
+  const T* qb = static_cast<const T*>(a.q) + s.b * a.qs[0] + s.q0 * a.qs[1] + static_cast<int64_t>(hk) * a.g * a.qs[2];
+  const T* db = static_cast<const T*>(a.dout) + s.b * a.ds[0] + s.q0 * a.ds[1] + static_cast<int64_t>(hk) * a.g * a.ds[2];
+  const int64_t sb = (s.b * a.hq + static_cast<int64_t>(hk) * a.g) * a.rows_q + s.q0;
+  Tile<DT, D, kRowsPass, kThreads> tq, td;
+  float stat = 0.0f;
+  const auto fetch = [&](int r0) {
+    tq.fetch(a.d, [&](int i) { return r0 + i < rows ? qb + (r0 + i) / a.g * a.qs[1] + (r0 + i) % a.g * a.qs[2] : nullptr; });
+    td.fetch(a.d, [&](int i) { return r0 + i < rows ? db + (r0 + i) / a.g * a.ds[1] + (r0 + i) % a.g * a.ds[2] : nullptr; });
+    if (threadIdx.x < 2 * kRowsPass) {
+      const int r = r0 + threadIdx.x % kRowsPass;
+      const bool lse = threadIdx.x < kRowsPass;
+      stat = lse ? INFINITY : 0.0f;
+      if (r < rows) {
+        stat = (lse ? a.lse : a.delta)[sb + static_cast<int64_t>(r % a.g) * a.rows_q + r / a.g];
+        if (lse) stat = stat == -INFINITY ? INFINITY : stat * kLog2e;
+      }
+    }
+  };
+  const RowReader<DT, D> rr;
+  const ColumnReader<DT, D> cr;
+  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  const float scale2 = a.scale * kLog2e;
+  const int begin = all.lo / kRowsPass * kRowsPass;
+  if (begin < all.hi) fetch(begin);
+  for (int r0 = begin; r0 < all.hi; r0 += kRowsPass) {
+    __syncthreads();
+    tq.put(lq);
+    td.put(ld);
+    if (threadIdx.x < 2 * kRowsPass) stats[threadIdx.x / kRowsPass][threadIdx.x % kRowsPass] = stat;
+    if (r0 + kRowsPass < all.hi) fetch(r0 + kRowsPass);
+    __syncthreads();
+    const bool masked = r0 < every.lo || r0 + kRowsPass > every.hi;
+    f32x16 p = {}, dp = {};
+#pragma unroll
+    for (int step = 0; step < D / 16; ++step) {
+      p = Mma<DT>::mul(rr.read(lq, 0, step), k[step], p);
+      dp = Mma<DT>::mul(rr.read(ld, 0, step), v[step], dp);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const f32x4 lse = *reinterpret_cast<const f32x4*>(&stats[0][8 * u + lane / 32 * 4]);
+      const f32x4 delta = *reinterpret_cast<const f32x4*>(&stats[1][8 * u + lane / 32 * 4]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int i = 4 * u + j;
+        p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - lse[j]);
+        if (masked) {
+          const int r = r0 + key_of(i) + lane / 32 * 4;
+          if (r < own.lo || r >= own.hi) p[i] = 0.0f;
+        }
+        dp[i] = p[i] * (dp[i] - delta[j]);
+      }
+    }
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      const V8 pn = narrow<DT>(p, step), ds = narrow<DT>(dp, step);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) {
+        dv[t] = Mma<DT>::mul(cr.read(ld, 16 * step, t), pn, dv[t]);
+        dk[t] = Mma<DT>::mul(cr.read(lq, 16 * step, t), ds, dk[t]);
+      }
+    }
+  }
+  if (key >= keys) return;
+  const int64_t at = ((s.b * a.rows_k + s.k0 + key) * a.hkv + hk) * a.d;
+  store_rows<DT, D>(static_cast<T*>(a.dk) + at, a.d, dk, a.scale);
+  store_rows<DT, D>(static_cast<T*>(a.dv) + at, a.d, dv, 1.0f);
+}
+
+// ---------------------------------------------------------------- host side
+int check(const fewbit_attn* a) {
+  if (!a) return FEWBIT_E_NULL;
+  if (a->dtype != FEWBIT_F16 && a->dtype != FEWBIT_BF16) return FEWBIT_E_DTYPE;
+  if (a->reserved != 0 || a->heads_q < 1 || a->heads_kv < 1 || a->heads_q % a->heads_kv != 0) return FEWBIT_E_INVALID;
+  if (a->head_dim < 8 || a->head_dim > 128 || a->head_dim % 8 != 0) return FEWBIT_E_INVALID;
+  if ((a->causal != 0 && a->causal != 1) || a->window < 0 || (a->window > 0 && !a->causal)) return FEWBIT_E_INVALID;
+  if (!(a->scale > 0.0f && std::isfinite(a->scale))) return FEWBIT_E_INVALID;
+  constexpr int64_t kMost = int64_t{1} << 30;
+  if (a->batch < 0 || a->batch >= kMost || a->rows_q < 0 || a->rows_k < 0 || a->rows_k >= kMost || a->heads_q >= 1 << 20 ||
+      a->rows_q >= kMost / (a->heads_q / a->heads_kv))
+    return FEWBIT_E_INVALID;
+  if ((a->cu_q == nullptr) != (a->cu_k == nullptr) || (a->cu_q && a->k_len)) return FEWBIT_E_INVALID;
+  return FEWBIT_OK;
+}
+
+bool strides_fit(const int64_t (&s)[3]) { return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0; }
+
+int64_t over(int64_t n, int64_t per) { return (n + per - 1) / per; }
+
+// Places for tiles of `per` rows: exact, or for packed sequences as many as any
+// division into batch (and one for the rows past the last) can need.
+int64_t places_of(const fewbit_attn* a, int64_t rows, int64_t per) {
+  return a->cu_q ? over(rows, per) + a->batch + 1 : over(rows, per) * a->batch;
+}
+
+// How the forward runs: keys of a split, and how many; 0: the kernel for many rows.
+struct Plan {
+  int64_t chunk, splits;
+};
+Plan plan_of(const fewbit_attn* a) {
+  const int64_t rows = a->rows_q * (a->heads_q / a->heads_kv);
+  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return {0, 0};
+  const int64_t many = over(rows, kRowsGroup) * a->heads_kv * a->batch, cus = device_cus();
+  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return {0, 0};
+  const int64_t few = over(rows, kRowsWave) * a->heads_kv * a->batch;
+  const int64_t splits = std::max<int64_t>(1, std::min(over(4 * cus, few), over(a->rows_k, 2 * kKeysSplit)));
+  const int64_t chunk = over(over(a->rows_k, splits), kKeysSplit) * kKeysSplit;
+  return {chunk, over(a->rows_k, chunk)};
+}
+
+Args args_of(const fewbit_attn* a) {
+  Args r{};
+  r.cu_q = a->cu_q;
+  r.cu_k = a->cu_k;
+  r.k_len = a->k_len;
+  for (int i = 0; i < 3; ++i) {
+    r.qs[i] = a->q_stride[i];
+    r.ks[i] = a->k_stride[i];
+    r.vs[i] = a->v_stride[i];
+    r.ds[i] = a->dout_stride[i];
+  }
+  r.rows_q = a->rows_q;
+  r.rows_k = a->rows_k;
+  r.batch = static_cast<int>(a->batch);
+  r.hq = a->heads_q;
+  r.hkv = a->heads_kv;
+  r.g = a->heads_q / a->heads_kv;
+  r.d = a->head_dim;
+  r.causal = a->causal;
+  r.window = a->window;
+  r.scale = a->scale;
+  r.splits = 1;
+  return r;
+}
+
+bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // fewer than 2^32 threads
+
+#define FEWBIT_ATTN_START(KERNEL, ARGS, GROUPS, STREAM)                                                              \
+  ((ARGS).d <= 64 ? (bf16 ? launch(KERNEL<FEWBIT_BF16, 64>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)    \
+                          : launch(KERNEL<FEWBIT_F16, 64>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS))    \
+                  : (bf16 ? launch(KERNEL<FEWBIT_BF16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)   \
+                          : launch(KERNEL<FEWBIT_F16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)))
+
+}  // namespace
+
+extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward) {
+  const int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  const int64_t rows = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
+  if (backward) return rows * static_cast<int64_t>(sizeof(float));
+  const Plan p = plan_of(a);
+  return p.splits > 1 ? rows * p.splits * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float)) : 0;
+}
+
+extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* k, const void* v, void* out, float* lse,
+                               void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  if (a->batch == 0 && a->cu_q == nullptr) return FEWBIT_OK;
+  if (a->rows_q == 0) return FEWBIT_OK;
+  if (!q || !out || !lse || (a->rows_k > 0 && (!k || !v))) return FEWBIT_E_NULL;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out)) return FEWBIT_E_ALIGN;
+  if (!strides_fit(a->q_stride) || !strides_fit(a->k_stride) || !strides_fit(a->v_stride)) return FEWBIT_E_ALIGN;
+  const int64_t need = fewbit_attn_workspace(a, 0);
+  if (need > 0 && !workspace) return FEWBIT_E_NULL;
+  if (workspace_bytes < need) return FEWBIT_E_INVALID;
+  if (need > 0 && misaligned(workspace)) return FEWBIT_E_ALIGN;
+  rc = check_stream_device(static_cast<hipStream_t>(stream));
+  if (rc != FEWBIT_OK) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf16 = a->dtype == FEWBIT_BF16;
+  Args r = args_of(a);
+  r.q = q;
+  r.k = k;
+  r.v = v;
+  r.o = out;
+  r.lse = lse;
+  const int64_t rows = a->rows_q * r.g;
+  const Plan plan = plan_of(a);
+  if (plan.splits == 0) {
+    r.tiles = static_cast<int>(over(rows, kRowsGroup));
+    const int64_t groups = places_of(a, rows, kRowsGroup) * r.hkv;
+    if (!fits_launch(groups)) return FEWBIT_E_INVALID;
+    return launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_fwd_kernel, r, groups, st));
+  }
+  r.tiles = static_cast<int>(over(rows, kRowsWave));
+  r.chunk = static_cast<int>(plan.chunk);
+  r.splits = static_cast<int>(plan.splits);
+  if (r.splits > 1) {
+    r.part_o = static_cast<float*>(workspace);
+    r.part_lse = r.part_o + a->batch * a->rows_q * r.hq * plan.splits * r.d;
+  }
+  const int64_t groups = places_of(a, rows, kRowsWave) * r.hkv * plan.splits, joins = over(a->batch * a->rows_q * r.hq, kWaves);
+  if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
+  rc = launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_split_kernel, r, groups, st));
+  if (rc != FEWBIT_OK || r.splits == 1) return rc;
+  return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_join_kernel<FEWBIT_BF16> : attn_join_kernel<FEWBIT_F16>,
+                                                 dim3(static_cast<unsigned>(joins)), kThreads, st, r));
+}
+
+extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const void* q, const void* k, const void* v,
+                               const void* out, const float* lse, void* dq, void* dk, void* dv, void* workspace,
+                               int64_t workspace_bytes, void* stream) {
+  int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  if ((a->batch == 0 && a->cu_q == nullptr) || (a->rows_q == 0 && a->rows_k == 0)) return FEWBIT_OK;
+  if (a->rows_q > 0 && (!q || !dout || !out || !lse || !dq || !workspace)) return FEWBIT_E_NULL;
+  if (a->rows_k > 0 && (!k || !v || !dk || !dv)) return FEWBIT_E_NULL;
+  if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(dout) || misaligned(dq) ||
+      misaligned(dk) || misaligned(dv))
+    return FEWBIT_E_ALIGN;
+  if (!strides_fit(a->q_stride) || !strides_fit(a->k_stride) || !strides_fit(a->v_stride) || !strides_fit(a->dout_stride))
+    return FEWBIT_E_ALIGN;
+  if (workspace_bytes < fewbit_attn_workspace(a, 1)) return FEWBIT_E_INVALID;
+  rc = check_stream_device(static_cast<hipStream_t>(stream));
+  if (rc != FEWBIT_OK) return rc;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  const bool bf16 = a->dtype == FEWBIT_BF16;
+  Args r = args_of(a);
+  r.q = q;
+  r.k = k;
+  r.v = v;
+  r.out = out;
+  r.dout = dout;
+  r.lse = const_cast<float*>(lse);
+  r.delta = static_cast<float*>(workspace);
+  r.dq = dq;
+  r.dk = dk;
+  r.dv = dv;
+  const int64_t rows = a->rows_q * r.g;
+  const int64_t q_groups = places_of(a, rows, kRowsGroup) * r.hkv, k_groups = places_of(a, a->rows_k, kRowsGroup) * r.hkv;
+  if (!fits_launch(q_groups) || !fits_launch(k_groups)) return FEWBIT_E_INVALID;
+  if (a->rows_q > 0) {
+    r.tiles = static_cast<int>(over(rows, kRowsGroup));
+    rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dq_kernel, r, q_groups, st));
+    if (rc != FEWBIT_OK) return rc;
+  }
+  if (a->rows_k > 0) {
+    r.tiles = static_cast<int>(over(a->rows_k, kRowsGroup));
+    rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dkv_kernel, r, k_groups, st));
+  }
+  return rc;
+}

@@ -18,18 +18,13 @@
 #include <torch/csrc/autograd/python_variable.h>
 #include <torch/csrc/autograd/saved_variable.h>
 #include <torch/csrc/dynamo/compiled_autograd.h>
-#include <torch/csrc/jit/frontend/tracer.h>
 #include <torch/csrc/utils/object_ptr.h>
 #include <torch/csrc/utils/pybind.h>
 
 #include <ATen/ATen.h>
-#include <ATen/PythonTorchFunctionTLS.h>
 #include <ATen/SequenceNumber.h>
-#include <ATen/hip/impl/HIPStreamMasqueradingAsCUDA.h>
 #include <ATen/record_function.h>
 #include <c10/core/DeviceGuard.h>
-#include <c10/core/impl/LocalDispatchKeySet.h>
-#include <c10/core/impl/TorchDispatchModeTLS.h>
 
 #include <algorithm>
 #include <cstring>
@@ -38,43 +33,18 @@
 #include <typeinfo>
 #include <vector>
 
+#include "binding.h"
 #include "fewbit.h"
 
 namespace {
 
+using namespace binding;
 using torch::autograd::variable_list;
 
 // The general backward of the package, (table bytes, grad, codes) -> grad_in,
 // and its exception class, (status, where); set once at import.
 PyObject* general_bwd = nullptr;
 PyObject* error_class = nullptr;
-
-// Storage type of the C ABI, or -1.
-int storage_type(const at::Tensor& t) {
-  switch (t.scalar_type()) {
-    case at::kFloat: return FEWBIT_F32;
-    case at::kHalf: return FEWBIT_F16;
-    case at::kBFloat16: return FEWBIT_BF16;
-    default: return -1;
-  }
-}
-
-// Nothing watches or rewrites tensor operations on this thread.
-bool plain_mode() {
-  return !c10::impl::TorchDispatchModeTLS::any_modes_set() && !at::impl::torch_function_mode_enabled() &&
-         !torch::jit::tracer::isTracing() &&
-         !c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::FuncTorchDynamicLayerFrontMode) &&
-         !c10::impl::tls_is_dispatch_key_included(c10::DispatchKey::PythonTLSSnapshot);
-}
-
-// An ordinary dense device tensor, not a wrapper and not a lazy view.
-bool plain(const at::Tensor& t) {
-  constexpr c10::DispatchKeySet kOdd({c10::DispatchKey::Python, c10::DispatchKey::FuncTorchGradWrapper,
-                                      c10::DispatchKey::FuncTorchBatched, c10::DispatchKey::Functionalize,
-                                      c10::DispatchKey::ZeroTensor, c10::DispatchKey::Conjugate,
-                                      c10::DispatchKey::Negative});
-  return t.is_cuda() && t.layout() == at::kStrided && !t.key_set().has_any(kOdd);
-}
 
 const at::Tensor* plain_tensor(PyObject* o) {
   if (!THPVariable_CheckExact(o)) return nullptr;
@@ -102,10 +72,6 @@ bool table_of(PyObject* o, fewbit_table* t) {
   if (ok) std::memcpy(t, b.buf, sizeof *t);
   PyBuffer_Release(&b);
   return ok && t->bits >= 1 && t->bits <= 4;
-}
-
-void* stream_of(const at::Tensor& t) {
-  return c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(t.device().index()).stream();
 }
 
 at::Tensor new_codes(const at::Tensor& x, int bits) {
@@ -380,6 +346,8 @@ PyMODINIT_FUNC PyInit__native(void) {
   HANDLE_TH_ERRORS
   torch::autograd::_initFunctionPyTypeObject(node_type, "FewBitActivationBackward", node_properties, nullptr);
   torch::autograd::registerCppFunction(typeid(FewBitNode), &node_type);
-  return PyModule_Create(&module_def);
+  PyObject* module = PyModule_Create(&module_def);
+  if (module && PyModule_AddFunctions(module, binding::block_methods()) != 0) Py_CLEAR(module);
+  return module;
   END_HANDLE_TH_ERRORS
 }

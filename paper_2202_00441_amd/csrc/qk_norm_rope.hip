@@ -1,0 +1,437 @@
+// qk_norm_rope.hip -- RMS norm of every query and key head and its rotary
+// position in one pass, and the gradients.
+//
+// Formulas in fewbit_block.h.  Bound by HBM: the forward reads and writes each
+// element once; the backward reads the input and the incoming gradient and
+// writes the gradient, and recomputes the norm instead of keeping it.
+//
+// A row (one head of one token) is held by a group of 4, 8 or 16 lanes, 16
+// elements each: two 16-byte chunks that hold both elements of eight rotated
+// pairs, so that neither the rotation nor the tables' angles cross lanes, and
+// the row's sums take two to four cross-lane steps.  A group walks the heads of
+// one token (or a share of them): the token's angles are read once and stay in
+// registers.
+//
+// Backward: with g the incoming gradient turned back, x the input, r = 1 /
+// sqrt(mean(x^2) + eps) and u = x r,
+//   dw = sum over rows of g u,   dx = r (g w - u mean(g w u)).
+// Lanes add dw up in registers over all their rows, workgroups in LDS, and a
+// second kernel adds the workgroups' sums, each in a fixed order.
+#include <algorithm>
+
+#include "block.h"
+
+namespace {
+
+using namespace block;
+
+constexpr int kThreads = 256;
+constexpr int kN = 16;          // elements of a lane
+constexpr int kParts = 1024;    // workgroups of the backward at most: the rows the second kernel adds
+
+struct Side {
+  const void* x;
+  const void* w;
+  const void* dy;       // backward
+  void* y;              // forward: output; backward: gradient
+  int64_t xs[3], ds[3];
+  int heads;
+};
+
+struct Args {
+  Side s[2];
+  const float *cos, *sin;
+  const int64_t* pos;
+  int64_t ps[2];
+  int64_t tokens_all;   // batch * tokens
+  int64_t table_rows;
+  uint32_t tokens;
+  int d, rot;
+  int share;            // heads of a group's walk
+  int shares;           // groups of a token
+  float eps;
+  float* parts;         // backward: [workgroups][2][head_dim]
+};
+
+// Where a lane's two chunks of eight elements begin in a row.
+struct Chunks {
+  int a, b;
+  bool some, turned;
+};
+template <bool INTER>
+__device__ __forceinline__ Chunks chunks_of(int lane, int d, int rot) {
+  if (INTER) return {16 * lane, 16 * lane + 8, 16 * lane < d, 16 * lane < rot};
+  const int half = rot / 2;
+  if (8 * lane < half) return {8 * lane, 8 * lane + half, true, true};
+  const int at = rot + 16 * lane - 2 * half;            // past the rotated part
+  return {at, at + 8, at < d, false};
+}
+
+// x[0..7], x[8..15] are a lane's chunks; pair j is (x[j], x[8 + j]), or, of
+// adjacent elements, (x[2j], x[2j + 1]).
+template <bool INTER>
+__device__ __forceinline__ void turn(float (&x)[kN], const float (&c)[8], const float (&s)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    float &a = x[INTER ? 2 * j : j], &b = x[INTER ? 2 * j + 1 : 8 + j];
+    const float u = a * c[j] - b * s[j];
+    b = b * c[j] + a * s[j];
+    a = u;
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void load_row(const T* row, const Chunks& at, float (&x)[kN]) {
+  float a[8], b[8];
+  load(row + at.a, a);
+  load(row + at.b, b);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    x[i] = a[i];
+    x[8 + i] = b[i];
+  }
+}
+template <class T>
+__device__ __forceinline__ void store_row(T* row, const Chunks& at, const float (&x)[kN]) {
+  float a[8], b[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    a[i] = x[i];
+    b[i] = x[8 + i];
+  }
+  store(row + at.a, a);
+  store(row + at.b, b);
+}
+
+template <int LEVELS>
+__device__ __forceinline__ float row_sum(float x) {
+  return across<LEVELS>(x, [](float a, float b) { return a + b; });
+}
+
+// The angles of a lane's pairs; 1 and 0 outside the rotated part, NaN for a
+// position that the tables do not hold (nothing is read for it).
+__device__ __forceinline__ void angles(const Args& a, int lane, bool turned, int64_t b, int64_t t, float (&c)[8], float (&s)[8]) {
+#pragma unroll
+  for (int j = 0; j < 8; ++j) {
+    c[j] = 1.0f;
+    s[j] = 0.0f;
+  }
+  if (!turned) return;
+  const int64_t pos = a.pos ? a.pos[b * a.ps[0] + t * a.ps[1]] : t;
+  if (pos >= 0 && pos < a.table_rows) {
+    load(a.cos + pos * (a.rot / 2) + 8 * lane, c);
+    load(a.sin + pos * (a.rot / 2) + 8 * lane, s);
+  } else {
+#pragma unroll
+    for (int j = 0; j < 8; ++j) c[j] = s[j] = __builtin_nanf("");
+  }
+}
+
+// LEVELS: a group has 2^LEVELS lanes.
+template <int DT, bool INTER, int LEVELS>
+__global__ __launch_bounds__(kThreads) void qk_fwd_kernel(const Args a) {
+  using T = typename Store<DT>::type;
+  constexpr int kLanes = 1 << LEVELS;
+  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
+  const int64_t token = unit / a.shares;
+  if (token >= a.tokens_all) return;
+  const int lane = threadIdx.x % kLanes, share = static_cast<int>(unit - token * a.shares);
+  const Chunks at = chunks_of<INTER>(lane, a.d, a.rot);
+  const int64_t b = token / a.tokens, t = token - b * a.tokens;
+  float c[8], s[8];
+  angles(a, lane, at.turned, b, t, c, s);
+  const int last = min((share + 1) * a.share, a.s[0].heads + a.s[1].heads);
+  for (int head = share * a.share; head < last; ++head) {
+    const Side& side = a.s[head >= a.s[0].heads];
+    const int h = head >= a.s[0].heads ? head - a.s[0].heads : head;
+    float x[kN] = {}, w[kN] = {};
+    if (at.some) {
+      load_row(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at, x);
+      load_row(static_cast<const T*>(side.w), at, w);
+    }
+    float sum = 0.0f;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) sum += x[i] * x[i];
+    const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) x[i] = x[i] * r * w[i];
+    if (at.turned) turn<INTER>(x, c, s);
+    if (at.some) store_row(static_cast<T*>(side.y) + (token * side.heads + h) * a.d, at, x);
+  }
+}
+
+template <int DT, bool INTER, int LEVELS>
+__global__ __launch_bounds__(kThreads) void qk_bwd_kernel(const Args a) {
+  using T = typename Store<DT>::type;
+  constexpr int kLanes = 1 << LEVELS, kGroups = kThreads / kLanes;
+  __shared__ float sums[kGroups][kLanes * kN];
+  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  const Chunks at = chunks_of<INTER>(lane, a.d, a.rot);
+  const int64_t units = a.tokens_all * a.shares, step = static_cast<int64_t>(gridDim.x) * kGroups;
+  float dw[2][kN] = {};
+  for (int64_t unit = static_cast<int64_t>(blockIdx.x) * kGroups + group; unit < units; unit += step) {
+    const int64_t token = unit / a.shares;
+    const int share = static_cast<int>(unit - token * a.shares);
+    const int64_t b = token / a.tokens, t = token - b * a.tokens;
+    float c[8], s[8];
+    angles(a, lane, at.turned, b, t, c, s);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) s[j] = -s[j];
+#pragma unroll
+    for (int kind = 0; kind < 2; ++kind) {
+      const Side& side = a.s[kind];
+      const int first = max(share * a.share - (kind ? a.s[0].heads : 0), 0);
+      const int last = min((share + 1) * a.share - (kind ? a.s[0].heads : 0), side.heads);
+      if (first >= last) continue;
+      float w[kN] = {};
+      if (at.some) load_row(static_cast<const T*>(side.w), at, w);
+      for (int h = first; h < last; ++h) {
+        float x[kN] = {}, g[kN] = {};
+        if (at.some) {
+          load_row(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at, x);
+          load_row(static_cast<const T*>(side.dy) + b * side.ds[0] + t * side.ds[1] + h * side.ds[2], at, g);
+        }
+        if (at.turned) turn<INTER>(g, c, s);
+        float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          sum += x[i] * x[i];
+          dot += g[i] * w[i] * x[i];
+        }
+        const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
+        const float mean = row_sum<LEVELS>(dot) * r / a.d;
+#pragma unroll
+        for (int i = 0; i < kN; ++i) {
+          const float u = x[i] * r;
+          dw[kind][i] += g[i] * u;
+          x[i] = r * (g[i] * w[i] - u * mean);
+        }
+        if (at.some) store_row(static_cast<T*>(side.y) + (token * side.heads + h) * a.d, at, x);
+      }
+    }
+  }
+  // the workgroup's sums: groups in pairs, then the next pairs
+#pragma unroll
+  for (int kind = 0; kind < 2; ++kind) {
+    if (kind) __syncthreads();
+#pragma unroll
+    for (int i = 0; i < kN; ++i) sums[group][i * kLanes + lane] = dw[kind][i];
+    for (int n = kGroups / 2; n > 0; n /= 2) {
+      __syncthreads();
+      for (int e = threadIdx.x; e < n * kLanes * kN; e += kThreads) {
+        const int g = e / (kLanes * kN), i = e % (kLanes * kN);
+        sums[g][i] += sums[g + n][i];
+      }
+    }
+    __syncthreads();
+    if (group == 0 && at.some) {
+      float* out = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + kind) * a.d;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) out[i < 8 ? at.a + i : at.b + i - 8] = sums[0][i * kLanes + lane];
+    }
+  }
+}
+
+// The sum of `rows` rows of 2 * d floats: a workgroup takes 16 columns, 64 sums
+// of every 64th row each, then adds those in pairs.
+constexpr int kColumns = 16, kRows = 64;
+__global__ __launch_bounds__(kColumns* kRows) void qk_sum_kernel(const float* parts, int rows, int d, float* dq_w, float* dk_w) {
+  __shared__ float sums[kRows][kColumns];
+  const int col = blockIdx.x * kColumns + threadIdx.x % kColumns, row = threadIdx.x / kColumns;
+  float sum = 0.0f;
+  for (int r = row; r < rows; r += kRows) sum += parts[static_cast<int64_t>(r) * 2 * d + col];
+  sums[row][threadIdx.x % kColumns] = sum;
+  for (int n = kRows / 2; n > 0; n /= 2) {
+    __syncthreads();
+    if (row < n) sums[row][threadIdx.x % kColumns] += sums[row + n][threadIdx.x % kColumns];
+  }
+  if (row == 0) {
+    float* out = col < d ? dq_w : dk_w;
+    if (out) out[col < d ? col : col - d] = sums[0][threadIdx.x];
+  }
+}
+
+int check(const fewbit_qk* a) {
+  if (!a) return FEWBIT_E_NULL;
+  if (a->dtype < FEWBIT_F32 || a->dtype > FEWBIT_BF16) return FEWBIT_E_DTYPE;
+  if (a->reserved != 0 || a->heads_q < 0 || a->heads_k < 0 || a->batch < 0 || a->tokens < 0 || a->table_rows < 0)
+    return FEWBIT_E_INVALID;
+  if (a->head_dim < 16 || a->head_dim > 256 || a->head_dim % 16 != 0) return FEWBIT_E_INVALID;
+  if (a->rot < 0 || a->rot > a->head_dim || a->rot % 16 != 0) return FEWBIT_E_INVALID;
+  if (a->interleaved != 0 && a->interleaved != 1) return FEWBIT_E_INVALID;
+  if (!(a->eps >= 0.0f && std::isfinite(a->eps))) return FEWBIT_E_INVALID;
+  if (a->heads_q > 1 << 16 || a->heads_k > 1 << 16) return FEWBIT_E_INVALID;
+  if (a->tokens >= int64_t{1} << 31 || a->batch >= int64_t{1} << 31) return FEWBIT_E_INVALID;
+  if (a->tokens > 0 && a->batch > (int64_t{1} << 34) / a->tokens) return FEWBIT_E_INVALID;
+  return FEWBIT_OK;
+}
+
+bool nothing(const fewbit_qk* a) { return a->batch == 0 || a->tokens == 0 || a->heads_q + a->heads_k == 0; }
+
+// Rows start at multiples of 16 bytes.
+bool strides_fit(const fewbit_qk* a, const int64_t (&s)[3]) {
+  const int64_t per = a->dtype == FEWBIT_F32 ? 4 : 8;
+  return s[0] % per == 0 && s[1] % per == 0 && s[2] % per == 0;
+}
+
+int levels_of(int d) { return d <= 64 ? 2 : d <= 128 ? 3 : 4; }
+
+// Heads of a group's walk: all of a token's where that fills the chip (16 waves
+// per CU), fewer where there are few tokens.
+int share_of(const fewbit_qk* a) {
+  const int heads = a->heads_q + a->heads_k;
+  const int64_t groups = static_cast<int64_t>(device_cus()) * 16 * (kWave >> levels_of(a->head_dim));
+  const int64_t all = a->batch * a->tokens;
+  const int64_t shares = all >= groups ? 1 : (groups + all - 1) / all;
+  return shares >= heads ? 1 : static_cast<int>((heads + shares - 1) / shares);
+}
+
+Args args_of(const fewbit_qk* a, const float* cos, const float* sin, const int64_t* pos) {
+  Args r{};
+  for (int i = 0; i < 3; ++i) {
+    r.s[0].xs[i] = a->q_stride[i];
+    r.s[1].xs[i] = a->k_stride[i];
+    r.s[0].ds[i] = a->dq_stride[i];
+    r.s[1].ds[i] = a->dk_stride[i];
+  }
+  r.s[0].heads = a->heads_q;
+  r.s[1].heads = a->heads_k;
+  r.cos = cos;
+  r.sin = sin;
+  r.pos = pos;
+  r.ps[0] = a->position_stride[0];
+  r.ps[1] = a->position_stride[1];
+  r.tokens_all = a->batch * a->tokens;
+  r.table_rows = a->table_rows;
+  r.tokens = static_cast<uint32_t>(a->tokens);
+  r.d = a->head_dim;
+  r.rot = a->rot;
+  r.share = share_of(a);
+  r.shares = (a->heads_q + a->heads_k + r.share - 1) / r.share;
+  r.eps = a->eps;
+  return r;
+}
+
+int64_t groups_of(const fewbit_qk* a, const Args& r) {
+  const int64_t per = kThreads >> levels_of(a->head_dim);
+  return (r.tokens_all * r.shares + per - 1) / per;
+}
+
+// Workgroups of the backward: what the chip holds at once, four per CU (each
+// leaves a row for the second kernel).
+int64_t parts_of(const fewbit_qk* a, const Args& r) {
+  const int64_t most = std::min<int64_t>(kParts, 4 * static_cast<int64_t>(device_cus()));
+  return std::min(groups_of(a, r), most);
+}
+
+template <int DT, bool INTER, int LEVELS>
+hipError_t start_at(const Args& r, bool back, unsigned groups, hipStream_t s) {
+  return back ? launch(qk_bwd_kernel<DT, INTER, LEVELS>, dim3(groups), kThreads, s, r)
+              : launch(qk_fwd_kernel<DT, INTER, LEVELS>, dim3(groups), kThreads, s, r);
+}
+template <int DT, bool INTER>
+hipError_t start_inter(const fewbit_qk* a, const Args& r, bool back, unsigned groups, hipStream_t s) {
+  switch (levels_of(a->head_dim)) {
+    case 2: return start_at<DT, INTER, 2>(r, back, groups, s);
+    case 3: return start_at<DT, INTER, 3>(r, back, groups, s);
+    default: return start_at<DT, INTER, 4>(r, back, groups, s);
+  }
+}
+template <int DT>
+hipError_t start_dt(const fewbit_qk* a, const Args& r, bool back, unsigned groups, hipStream_t s) {
+  return a->interleaved ? start_inter<DT, true>(a, r, back, groups, s) : start_inter<DT, false>(a, r, back, groups, s);
+}
+hipError_t start(const fewbit_qk* a, const Args& r, bool back, unsigned groups, hipStream_t s) {
+  return a->dtype == FEWBIT_F32   ? start_dt<FEWBIT_F32>(a, r, back, groups, s)
+         : a->dtype == FEWBIT_F16 ? start_dt<FEWBIT_F16>(a, r, back, groups, s)
+                                  : start_dt<FEWBIT_BF16>(a, r, back, groups, s);
+}
+
+// Checks that both directions make of what they read.
+int check_inputs(const fewbit_qk* a, const void* q, const void* k, const void* qw, const void* kw, const float* cos,
+                 const float* sin) {
+  if (a->heads_q > 0 && (!q || !qw)) return FEWBIT_E_NULL;
+  if (a->heads_k > 0 && (!k || !kw)) return FEWBIT_E_NULL;
+  if (a->rot > 0 && a->table_rows > 0 && (!cos || !sin)) return FEWBIT_E_NULL;
+  if (misaligned(q) || misaligned(k) || misaligned(qw) || misaligned(kw) || misaligned(cos) || misaligned(sin))
+    return FEWBIT_E_ALIGN;
+  if ((a->heads_q > 0 && !strides_fit(a, a->q_stride)) || (a->heads_k > 0 && !strides_fit(a, a->k_stride)))
+    return FEWBIT_E_ALIGN;
+  return FEWBIT_OK;
+}
+
+}  // namespace
+
+extern "C" int fewbit_qk_fwd(const fewbit_qk* a, const void* q, const void* k, const void* q_weight,
+                             const void* k_weight, const float* cos, const float* sin, const int64_t* positions,
+                             void* q_out, void* k_out, void* stream) {
+  int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  if (nothing(a)) return FEWBIT_OK;
+  rc = check_inputs(a, q, k, q_weight, k_weight, cos, sin);
+  if (rc != FEWBIT_OK) return rc;
+  if ((a->heads_q > 0 && !q_out) || (a->heads_k > 0 && !k_out)) return FEWBIT_E_NULL;
+  if (misaligned(q_out) || misaligned(k_out)) return FEWBIT_E_ALIGN;
+  rc = check_stream_device(static_cast<hipStream_t>(stream));
+  if (rc != FEWBIT_OK) return rc;
+  Args r = args_of(a, cos, sin, positions);
+  r.s[0].x = q;
+  r.s[1].x = k;
+  r.s[0].w = q_weight;
+  r.s[1].w = k_weight;
+  r.s[0].y = q_out;
+  r.s[1].y = k_out;
+  const int64_t groups = groups_of(a, r);
+  if (groups >= int64_t{1} << 24) return FEWBIT_E_INVALID;       // fewer than 2^32 threads: more than a device holds
+  return launch_status("fewbit_qk_fwd", start(a, r, false, static_cast<unsigned>(groups), static_cast<hipStream_t>(stream)));
+}
+
+extern "C" int64_t fewbit_qk_workspace(const fewbit_qk* a) {
+  const int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  if (nothing(a)) return 0;
+  return parts_of(a, args_of(a, nullptr, nullptr, nullptr)) * 2 * a->head_dim * static_cast<int64_t>(sizeof(float));
+}
+
+extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void* dk_out, const void* q, const void* k,
+                             const void* q_weight, const void* k_weight, const float* cos, const float* sin,
+                             const int64_t* positions, void* dq, void* dk, float* dq_weight, float* dk_weight,
+                             void* workspace, int64_t workspace_bytes, void* stream) {
+  int rc = check(a);
+  if (rc != FEWBIT_OK) return rc;
+  const bool none = nothing(a);           // no rows: the weights' gradients are 0
+  if ((a->heads_q > 0 && !dq_weight) || (a->heads_k > 0 && !dk_weight)) return FEWBIT_E_NULL;
+  if (!none) {
+    rc = check_inputs(a, q, k, q_weight, k_weight, cos, sin);
+    if (rc != FEWBIT_OK) return rc;
+    if ((a->heads_q > 0 && (!dq_out || !dq)) || (a->heads_k > 0 && (!dk_out || !dk)) || !workspace) return FEWBIT_E_NULL;
+    if (misaligned(dq_out) || misaligned(dk_out) || misaligned(dq) || misaligned(dk) || misaligned(workspace))
+      return FEWBIT_E_ALIGN;
+    if ((a->heads_q > 0 && !strides_fit(a, a->dq_stride)) || (a->heads_k > 0 && !strides_fit(a, a->dk_stride)))
+      return FEWBIT_E_ALIGN;
+    if (workspace_bytes < fewbit_qk_workspace(a)) return FEWBIT_E_INVALID;
+  }
+  if (!dq_weight && !dk_weight) return FEWBIT_OK;         // no heads, and nothing to write zeros to
+  rc = check_stream_device(static_cast<hipStream_t>(stream));
+  if (rc != FEWBIT_OK) return rc;
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  int64_t parts = 0;
+  if (!none) {
+    Args r = args_of(a, cos, sin, positions);
+    r.s[0].x = q;
+    r.s[1].x = k;
+    r.s[0].w = q_weight;
+    r.s[1].w = k_weight;
+    r.s[0].dy = dq_out;
+    r.s[1].dy = dk_out;
+    r.s[0].y = dq;
+    r.s[1].y = dk;
+    r.parts = static_cast<float*>(workspace);
+    parts = parts_of(a, r);
+    rc = launch_status("fewbit_qk_bwd", start(a, r, true, static_cast<unsigned>(parts), s));
+    if (rc != FEWBIT_OK) return rc;
+  }
+  return launch_status("fewbit_qk_bwd", launch(qk_sum_kernel, dim3(2 * a->head_dim / kColumns), kColumns * kRows, s,
+                                               static_cast<const float*>(workspace), static_cast<int>(parts), a->head_dim,
+                                               dq_weight, dk_weight));
+}
