@@ -22,6 +22,7 @@
 // spreads both the 16-byte reads down a column of chunks and the transposing
 // reads of 4 rows x 32 bytes over all banks.
 #include <algorithm>
+#include <type_traits>
 
 #include "block.h"
 
@@ -52,10 +53,23 @@ struct Mma<FEWBIT_F16> {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
+// x / n for 0 <= x < 2^31: the high half of a product with 2^32 / n rounded up is at
+// most one too many.
+struct Divisor {
+  uint32_t n, inverse;
+  __device__ __forceinline__ int divide(int x) const {
+    if (n == 1) return x;
+    const uint32_t q = __umulhi(static_cast<uint32_t>(x), inverse);
+    return static_cast<int>(q * n > static_cast<uint32_t>(x) ? q - 1 : q);
+  }
+};
+
 struct Args {
   const void *q, *k, *v, *dout, *out;
   void *o, *dq, *dk, *dv;
-  float *lse, *delta;
+  float* lse;
+  float* stats;                       // backward: lse * log2(e) of every row (infinity if it is empty), then delta; lifted
+  int64_t stats_delta;
   float *part_o, *part_lse;           // split forward
   const int32_t *cu_q, *cu_k, *k_len;
   int64_t qs[3], ks[3], vs[3], ds[3];
@@ -63,6 +77,7 @@ struct Args {
   int batch, hq, hkv, g, d;           // g: query heads to a key head
   int causal, window;
   float scale;
+  Divisor by_g;
   int tiles;                          // of a sequence (packed: places for tiles of all)
   int chunk, splits;                  // keys of a split, splits
 };
@@ -151,36 +166,71 @@ __device__ __forceinline__ int swizzle(int row) {
   return D == 128 ? ((row & 7) << 1) ^ ((row >> 3) & 1) : ((row >> 1) & 3) << 1;
 }
 
-// A tile of ROWS rows of D elements in LDS, and the part of it that a thread of
-// THREADS carries there from the tensor.
-template <int DT, int D, int ROWS, int THREADS>
-struct Tile {
+// Brings a tile of ROWS rows of D elements to LDS, 16 bytes a lane and load, without
+// registers between.  A load writes 1 KiB of LDS in lane order, so the swizzle is in
+// which chunk of its row a lane asks for.  Rows past the last are read as the last,
+// chunks past head_dim as the first: what multiplies them is 0 (masked scores; the
+// other operand's elements past head_dim) or is not stored.
+template <int DT, int D, int ROWS, int WAVES>
+struct Stage {
   using T = typename Mma<DT>::T;
-  using V8 = typename Mma<DT>::V8;
-  static constexpr int kChunks = D / 8, kPer = ROWS * kChunks / THREADS, kStep = THREADS / kChunks;
-  static_assert(kPer >= 1 && ROWS * kChunks % THREADS == 0, "whole chunks for every thread");
+  static constexpr int kChunks = D / 8, kRowsLoad = kWave / kChunks, kLoads = ROWS / kRowsLoad / WAVES;
+  static constexpr int kKinds = 16 / (kRowsLoad * WAVES) > 1 ? 16 / (kRowsLoad * WAVES) : 1;      // of swizzles among a wave's loads
+  static_assert(ROWS % (kRowsLoad * WAVES) == 0, "whole loads for every wave");
+  int wave, row, chunk[kKinds];
 
-  u32x4 r[kPer];
-
-  // row(i): the tensor's row for row i of the tile, or null
-  template <class F>
-  __device__ __forceinline__ void fetch(int d, F row) {
-    const int c = threadIdx.x % kChunks;
+  __device__ __forceinline__ Stage(int d, int wave_) : wave(__builtin_amdgcn_readfirstlane(wave_)) {
+    const int lane = threadIdx.x % kWave;
+    row = lane / kChunks;
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const T* p = row(static_cast<int>(threadIdx.x) / kChunks + j * kStep);
-      r[j] = p && c * 8 < d ? *reinterpret_cast<const u32x4*>(p + c * 8) : u32x4{0, 0, 0, 0};
+    for (int j = 0; j < kKinds; ++j) {
+      const int c = (lane % kChunks) ^ swizzle<D>(row + row_of(j));
+      chunk[j] = c * 8 < d ? c * 8 : 0;
     }
   }
-  __device__ __forceinline__ void put(T* lds) const {
-    const int c = threadIdx.x % kChunks;
+  __device__ __forceinline__ int row_of(int j) const { return (j * WAVES + wave) * kRowsLoad; }
+  // at(i): where row i of the tile begins
+  template <class F>
+  __device__ __forceinline__ void issue(T* lds, F at) const {
 #pragma unroll
-    for (int j = 0; j < kPer; ++j) {
-      const int row = static_cast<int>(threadIdx.x) / kChunks + j * kStep;
-      *reinterpret_cast<u32x4*>(lds + row * D + ((c ^ swizzle<D>(row)) * 8)) = r[j];
+    for (int j = 0; j < kLoads; ++j) {
+      const T* p = at(row + row_of(j)) + chunk[j % kKinds];
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                       (__attribute__((address_space(3))) void*)(lds + row_of(j) * D), 16, 0, 0);
     }
   }
 };
+
+// Two tiles that come and are worked on together.
+template <class T, int N>
+struct Pair {
+  __attribute__((aligned(16))) T a[N];
+  __attribute__((aligned(16))) T b[N];
+};
+
+// This wave's loads to LDS are done.
+__device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0)
+
+// Walks tiles at, at + step, .. < end through two buffers: while one is worked on the
+// next tile comes into the other.  (Buffers are apart so that the compiler does not make
+// reads of one wait for loads into the other.)
+// GROUP: the buffers are the workgroup's, else each wave's own.
+template <bool GROUP, class Buffer, class Issue, class Work>
+__device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work) {
+  if (at >= end) return;
+  issue(a, at);
+  for (; at < end; at += 2 * step) {
+    landed();
+    if (GROUP) __syncthreads();
+    if (at + step < end) issue(b, at + step);
+    work(a, at);
+    if (at + step >= end) break;
+    landed();
+    if (GROUP) __syncthreads();
+    if (at + 2 * step < end) issue(a, at + 2 * step);
+    work(b, at + step);
+  }
+}
 
 // First operand from rows: lane m holds row `row0 + m % 32`, elements 16 step + 8
 // (lane / 32) ..+7.
@@ -189,6 +239,13 @@ struct RowReader {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
   int at;
+  // A copy whose addresses are formed where they are used: the compiler else keeps the
+  // address of every read of a tile in a register of its own throughout.
+  __device__ __forceinline__ RowReader here() const {
+    RowReader r = *this;
+    asm volatile("" : "+v"(r.at));
+    return r;
+  }
   __device__ __forceinline__ RowReader() {
     const int lane = threadIdx.x % kWave, row = lane % 32;
     at = row * D + ((lane / 32) ^ swizzle<D>(row)) * 8;
@@ -207,6 +264,11 @@ struct ColumnReader {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
   int at;
+  __device__ __forceinline__ ColumnReader here() const {
+    ColumnReader r = *this;
+    asm volatile("" : "+v"(r.at));
+    return r;
+  }
   __device__ __forceinline__ ColumnReader() {
     const int lane = threadIdx.x % kWave, i = lane % 16, row = 4 * (lane / 32) + i / 4;
     const int chunk = 2 * (lane / 16 % 2) + i % 4 / 2;
@@ -350,8 +412,7 @@ constexpr int kKeys = 64;                                           // keys of a
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   using T = typename Mma<DT>::T;
-  __shared__ __attribute__((aligned(16))) T lk[kKeys * D];
-  __shared__ __attribute__((aligned(16))) T lv[kKeys * D];
+  __shared__ Pair<T, kKeys * D> buf0, buf1;
   const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   Seq s;
   int tile;
@@ -373,25 +434,18 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
 
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
-  Tile<DT, D, kKeys, kThreads> tk, tv;
-  const auto fetch = [&](int k0) {
-    tk.fetch(a.d, [&](int i) { return k0 + i < s.nk ? kb + (k0 + i) * a.ks[1] : nullptr; });
-    tv.fetch(a.d, [&](int i) { return k0 + i < s.nk ? vb + (k0 + i) * a.vs[1] : nullptr; });
-  };
+  const Stage<DT, D, kKeys, kWaves> stage(a.d, wave);
   const RowReader<DT, D> rr;
   const ColumnReader<DT, D> cr;
   Running<D> x;
-  const float scale2 = a.scale * kLog2e;
-  const int begin = all.lo / kKeys * kKeys;
-  if (begin < all.hi) fetch(begin);
-  for (int k0 = begin; k0 < all.hi; k0 += kKeys) {
-    __syncthreads();
-    tk.put(lk);
-    tv.put(lv);
-    if (k0 + kKeys < all.hi) fetch(k0 + kKeys);
-    __syncthreads();
-    attend<DT, D, kKeys / 32>(lk, lv, 0, k0, q, rr, cr, k0 < every.lo || k0 + kKeys > every.hi, own, scale2, x);
-  }
+  walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+       [&](Pair<T, kKeys * D>& to, int k0) {
+         stage.issue(to.a, [&](int i) { return kb + min(k0 + i, s.nk - 1) * a.ks[1]; });
+         stage.issue(to.b, [&](int i) { return vb + min(k0 + i, s.nk - 1) * a.vs[1]; });
+       },
+       [&](const Pair<T, kKeys * D>& in, int k0) {
+         attend<DT, D, kKeys / 32>(in.a, in.b, 0, k0, q, rr, cr, k0 < every.lo || k0 + kKeys > every.hi, own, a.scale * kLog2e, x);
+       });
   if (!there) return;
   const Two both = halves32(x.sum);
   const float sum = both.a + both.b;
@@ -405,10 +459,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
 constexpr int kKeysSplit = 32 * kWaves;
 
 template <int DT, int D>
-__global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
+__global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
-  __shared__ __attribute__((aligned(16))) char lds[2 * kKeysSplit * D * sizeof(T)];
-  T *lk = reinterpret_cast<T*>(lds), *lv = lk + kKeysSplit * D;
+  __shared__ Pair<T, 32 * D> buf0[kWaves], buf1[kWaves];
   const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   const int split = blockIdx.x / a.hkv % a.splits;
   Seq s;
@@ -431,29 +484,22 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
     const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
     const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
-    Tile<DT, D, kKeysSplit, kThreads> tk, tv;
-    const auto fetch = [&](int k0) {
-      tk.fetch(a.d, [&](int i) { return k0 + i < all.hi ? kb + (k0 + i) * a.ks[1] : nullptr; });
-      tv.fetch(a.d, [&](int i) { return k0 + i < all.hi ? vb + (k0 + i) * a.vs[1] : nullptr; });
-    };
+    const Stage<DT, D, 32, 1> stage(a.d, 0);
     const RowReader<DT, D> rr;
     const ColumnReader<DT, D> cr;
     const Range mine{max(own.lo, all.lo), min(own.hi, all.hi)};
     const Range sure{max(every.lo, all.lo), min(every.hi, all.hi)};
-    const int begin = all.lo / kKeysSplit * kKeysSplit;
-    fetch(begin);
-    for (int k0 = begin; k0 < all.hi; k0 += kKeysSplit) {
-      __syncthreads();
-      tk.put(lk);
-      tv.put(lv);
-      if (k0 + kKeysSplit < all.hi) fetch(k0 + kKeysSplit);
-      __syncthreads();
-      const int kw = k0 + 32 * wave;
-      attend<DT, D, 1>(lk, lv, 32 * wave, kw, q, rr, cr, kw < sure.lo || kw + 32 > sure.hi, mine, a.scale * kLog2e, x);
-    }
+    walk<false>(all.lo / 32 * 32 + 32 * wave, kKeysSplit, all.hi, buf0[wave], buf1[wave],
+                [&](Pair<T, 32 * D>& to, int k0) {
+                  stage.issue(to.a, [&](int i) { return kb + min(k0 + i, all.hi - 1) * a.ks[1]; });
+                  stage.issue(to.b, [&](int i) { return vb + min(k0 + i, all.hi - 1) * a.vs[1]; });
+                },
+                [&](const Pair<T, 32 * D>& in, int k0) {
+                  attend<DT, D, 1>(in.a, in.b, 0, k0, q, rr, cr, k0 < sure.lo || k0 + 32 > sure.hi, mine, a.scale * kLog2e, x);
+                });
     // the waves' results: statistics, then outputs one after another
     __syncthreads();
-    float* stats = reinterpret_cast<float*>(lds);           // [wave][2][32]
+    float* stats = reinterpret_cast<float*>(buf0);          // [wave][2][32]
     const Two both = halves32(x.sum);
     x.sum = both.a + both.b;
     if (lane < 32) {
@@ -472,7 +518,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     x.most = most;
     x.sum = sum;
     __syncthreads();
-    float* acc = reinterpret_cast<float*>(lds);             // [register][lane]
+    float* acc = reinterpret_cast<float*>(buf0);            // [register][lane]
     for (int w = 1; w < kWaves; ++w) {
       if (wave == w) {
 #pragma unroll
@@ -547,6 +593,11 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
 }
 
 // ---------------------------------------------------------------- backward
+// The kernel for dK and dV hands P over in the storage type.  In fp16 it hands over
+// 2^15 P, for which small probabilities keep all of their bits too.
+template <int DT>
+constexpr int kLift = DT == FEWBIT_F16 ? 15 : 0;
+
 // With P from lse, delta_i = <dO_i, O_i>, dP = dO V^T and dS = P (dP - delta):
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
 // dQ needs all keys of a row and dK, dV all rows of a key: one kernel for each,
@@ -556,8 +607,7 @@ template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
-  __shared__ __attribute__((aligned(16))) T lk[kKeys * D];
-  __shared__ __attribute__((aligned(16))) T lv[kKeys * D];
+  __shared__ Pair<T, kKeys * D> buf0, buf1;
   const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
   Seq s;
   int tile;
@@ -583,9 +633,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
     const Two both = halves32(delta);
     delta = both.a + both.b;
   }
-  if (there && lane < 32) a.delta[stat] = delta;
   float lse = there ? a.lse[stat] : -INFINITY;
   lse = lse == -INFINITY ? INFINITY : lse * kLog2e;           // of an empty row no key is seen
+  if (there && lane < 32) {
+    a.stats[stat] = lse - kLift<DT>;
+    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift<DT>);
+  }
 
   const Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsGroup, rows) - 1) / a.g).hi};
   const Range own = keys_of(a, s, pos);
@@ -594,73 +647,87 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
 
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
-  Tile<DT, D, kKeys, kThreads> tk, tv;
-  const auto fetch = [&](int k0) {
-    tk.fetch(a.d, [&](int i) { return k0 + i < s.nk ? kb + (k0 + i) * a.ks[1] : nullptr; });
-    tv.fetch(a.d, [&](int i) { return k0 + i < s.nk ? vb + (k0 + i) * a.vs[1] : nullptr; });
-  };
-  const RowReader<DT, D> rr;
-  const ColumnReader<DT, D> cr;
+  const Stage<DT, D, kKeys, kWaves> stage(a.d, wave);
+  const RowReader<DT, D> rows_at;
+  const ColumnReader<DT, D> columns_at;
   f32x16 dq[D / 32] = {};
   const float scale2 = a.scale * kLog2e;
-  const int begin = all.lo / kKeys * kKeys;
-  if (begin < all.hi) fetch(begin);
-  for (int k0 = begin; k0 < all.hi; k0 += kKeys) {
-    __syncthreads();
-    tk.put(lk);
-    tv.put(lv);
-    if (k0 + kKeys < all.hi) fetch(k0 + kKeys);
-    __syncthreads();
-    const bool masked = k0 < every.lo || k0 + kKeys > every.hi;
+  walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+       [&](Pair<T, kKeys * D>& to, int k0) {
+         stage.issue(to.a, [&](int i) { return kb + min(k0 + i, s.nk - 1) * a.ks[1]; });
+         stage.issue(to.b, [&](int i) { return vb + min(k0 + i, s.nk - 1) * a.vs[1]; });
+       },
+       [&](const Pair<T, kKeys * D>& in, int k0) {
+         const auto rr = rows_at.here();
+         const auto cr = columns_at.here();
+         const bool masked = k0 < every.lo || k0 + kKeys > every.hi;
 #pragma unroll
-    for (int u = 0; u < kKeys / 32; ++u) {
-      f32x16 p = {}, dp = {};
+         for (int u = 0; u < kKeys / 32; ++u) {
+           f32x16 p = {}, dp = {};
 #pragma unroll
-      for (int step = 0; step < D / 16; ++step) {
-        p = Mma<DT>::mul(rr.read(lk, 32 * u, step), q[step], p);
-        dp = Mma<DT>::mul(rr.read(lv, 32 * u, step), dout[step], dp);
-      }
+           for (int step = 0; step < D / 16; ++step) {
+             p = Mma<DT>::mul(rr.read(in.a, 32 * u, step), q[step], p);
+             dp = Mma<DT>::mul(rr.read(in.b, 32 * u, step), dout[step], dp);
+           }
+           if (masked) {
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - lse);
-        if (masked) {
-          const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
-          if (key < own.lo || key >= own.hi) p[i] = 0.0f;
-        }
-        p[i] *= dp[i] - delta;
-      }
+             for (int i = 0; i < 16; ++i) {
+               const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
+               if (key < own.lo || key >= own.hi) p[i] = -INFINITY;
+             }
+           }
 #pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        const V8 ds = narrow<DT>(p, step);
+           for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - lse) * (dp[i] - delta);
 #pragma unroll
-        for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(lk, 32 * u + 16 * step, t), ds, dq[t]);
-      }
-    }
-  }
+           for (int step = 0; step < 2; ++step) {
+             const V8 ds = narrow<DT>(p, step);
+#pragma unroll
+             for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), ds, dq[t]);
+           }
+         }
+       });
   if (there) store_rows<DT, D>(static_cast<T*>(a.dq) + at, a.d, dq, a.scale);
 }
 
-constexpr int kRowsPass = 32;       // rows of a pass of the dK, dV kernel
+// A workgroup takes 4 runs of 32 SUBS keys and walks the rows that see them, 32 at a
+// time.  Two waves share a run: one forms S, P and dV, the other dP, dS and dK, one
+// tile of rows behind, with P handed over in LDS.  So each wave holds one of K and V
+// and one of the two gradients, the same products run on both sides, and the two waves
+// of a SIMD are always one of either kind.  The tiles come through three buffers.
+constexpr int kRowsPass = 64;
+constexpr int kPairs = 4, kThreadsPairs = 2 * kPairs * kWave;
 
-template <int DT, int D>
-__global__ __launch_bounds__(kThreads, 1) void attn_dkv_kernel(const Args a) {
+template <int DT, int D, int SUBS>
+__global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
-  __shared__ __attribute__((aligned(16))) T lq[kRowsPass * D];
-  __shared__ __attribute__((aligned(16))) T ld[kRowsPass * D];
-  __shared__ __attribute__((aligned(16))) float stats[2][kRowsPass];
-  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  constexpr int kRun = 32 * SUBS, kGroup = kPairs * kRun;
+  struct Buffer : Pair<T, kRowsPass * D> {        // rows of Q and dO
+    __attribute__((aligned(16))) float stats[2][kRowsPass];
+  };
+  __shared__ Buffer buf0, buf1, buf2;
+  __shared__ V8 handed[2][kPairs][SUBS][kRowsPass / 16][kWave];
+  const int hk = blockIdx.x % a.hkv, lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), pair = wave % kPairs;
+  const bool second = wave >= kPairs;             // of a pair: dP, dS and dK
   Seq s;
   int tile;
-  if (!find(a, true, 1, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  if (!find(a, true, 1, kGroup, blockIdx.x / a.hkv, s, tile)) return;
   // keys past those that are there have gradients too: zeros
-  const int keys = a.cu_k ? (s.nk > 0 ? s.nk : 0) : static_cast<int>(a.rows_k), first = tile * kRowsGroup;
+  const int keys = a.cu_k ? s.nk : static_cast<int>(a.rows_k), first = tile * kGroup;
   if (first >= keys) return;
-  const int key = first + wave * kRowsWave + lane % 32;
-  const bool there = key < s.nk;
-  V8 k[D / 16], v[D / 16];
-  load_rows<DT, D>(there ? static_cast<const T*>(a.k) + s.b * a.ks[0] + (s.k0 + key) * a.ks[1] + hk * a.ks[2] : nullptr, a.d, k);
-  load_rows<DT, D>(there ? static_cast<const T*>(a.v) + s.b * a.vs[0] + (s.k0 + key) * a.vs[1] + hk * a.vs[2] : nullptr, a.d, v);
+  const int run = first + pair * kRun;
+  V8 kv[SUBS][D / 16];
+  {
+    const T* base = second ? static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2]
+                           : static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
+    const int64_t stride = second ? a.vs[1] : a.ks[1];
+#pragma unroll
+    for (int u = 0; u < SUBS; ++u) {
+      const int key = run + 32 * u + lane % 32;
+      load_rows<DT, D>(key < s.nk ? base + key * stride : nullptr, a.d, kv[u]);
+    }
+  }
 
   // rows (query * G + head) that see a key: from lo to before hi
   const int rows = s.nq * a.g;
@@ -672,80 +739,124 @@ __global__ __launch_bounds__(kThreads, 1) void attn_dkv_kernel(const Args a) {
     if (j >= s.nk) r.hi = 0;
     return r;
   };
-  const int last = min(first + kRowsGroup, s.nk) - 1;
   Range all{0, 0};
-  if (first < s.nk) all = Range{rows_of(first).lo, rows_of(last).hi};
-  const Range own = rows_of(key);
-  const int w0 = first + wave * kRowsWave, w1 = w0 + kRowsWave - 1;
-  const Range every{rows_of(w1).lo, w1 < s.nk ? rows_of(w0).hi : 0};
+  if (first < s.nk) all = Range{rows_of(first).lo, rows_of(min(first + kGroup, s.nk) - 1).hi};
+  const Range every{rows_of(run + kRun - 1).lo, run + kRun <= s.nk ? rows_of(run).hi : 0};
 
   const T* qb = static_cast<const T*>(a.q) + s.b * a.qs[0] + s.q0 * a.qs[1] + static_cast<int64_t>(hk) * a.g * a.qs[2];
   const T* db = static_cast<const T*>(a.dout) + s.b * a.ds[0] + s.q0 * a.ds[1] + static_cast<int64_t>(hk) * a.g * a.ds[2];
   const int64_t sb = (s.b * a.hq + static_cast<int64_t>(hk) * a.g) * a.rows_q + s.q0;
-  Tile<DT, D, kRowsPass, kThreads> tq, td;
-  float stat = 0.0f;
-  const auto fetch = [&](int r0) {
-    tq.fetch(a.d, [&](int i) { return r0 + i < rows ? qb + (r0 + i) / a.g * a.qs[1] + (r0 + i) % a.g * a.qs[2] : nullptr; });
-    td.fetch(a.d, [&](int i) { return r0 + i < rows ? db + (r0 + i) / a.g * a.ds[1] + (r0 + i) % a.g * a.ds[2] : nullptr; });
-    if (threadIdx.x < 2 * kRowsPass) {
-      const int r = r0 + threadIdx.x % kRowsPass;
-      const bool lse = threadIdx.x < kRowsPass;
-      stat = lse ? INFINITY : 0.0f;
-      if (r < rows) {
-        stat = (lse ? a.lse : a.delta)[sb + static_cast<int64_t>(r % a.g) * a.rows_q + r / a.g];
-        if (lse) stat = stat == -INFINITY ? INFINITY : stat * kLog2e;
-      }
+  const Stage<DT, D, kRowsPass, kPairs> stage(a.d, pair);
+  const auto issue = [&](Buffer& to, int r0) {
+    // the first waves of the pairs bring Q and lse, the second dO and delta
+    const T* base = second ? db : qb;
+    const int64_t pos_stride = second ? a.ds[1] : a.qs[1], head_stride = second ? a.ds[2] : a.qs[2];
+    stage.issue(second ? to.b : to.a, [&](int i) {
+      const int r = min(r0 + i, rows - 1), pos = a.by_g.divide(r);
+      return base + pos * pos_stride + (r - pos * a.g) * head_stride;
+    });
+    if (pair == 0) {                 // lse for the first, delta for the second
+      const int r = min(r0 + lane, rows - 1), pos = a.by_g.divide(r);
+      const float* p = a.stats + (second ? a.stats_delta : 0) + sb + (r - pos * a.g) * a.rows_q + pos;
+      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                       (__attribute__((address_space(3))) void*)to.stats[second], 4, 0, 0);
     }
   };
-  const RowReader<DT, D> rr;
-  const ColumnReader<DT, D> cr;
-  f32x16 dk[D / 32] = {}, dv[D / 32] = {};
+  const RowReader<DT, D> rows_at;
+  const ColumnReader<DT, D> columns_at;
+  f32x16 acc[SUBS][D / 32] = {};
+  constexpr float lower = 1.0f / (1 << kLift<DT>);
   const float scale2 = a.scale * kLog2e;
-  const int begin = all.lo / kRowsPass * kRowsPass;
-  if (begin < all.hi) fetch(begin);
-  for (int r0 = begin; r0 < all.hi; r0 += kRowsPass) {
-    __syncthreads();
-    tq.put(lq);
-    td.put(ld);
-    if (threadIdx.x < 2 * kRowsPass) stats[threadIdx.x / kRowsPass][threadIdx.x % kRowsPass] = stat;
-    if (r0 + kRowsPass < all.hi) fetch(r0 + kRowsPass);
-    __syncthreads();
-    const bool masked = r0 < every.lo || r0 + kRowsPass > every.hi;
-    f32x16 p = {}, dp = {};
+  // One side's part of a tile of rows: SECOND and MASKED are constants, so that each
+  // is one run of code in which products and the rest overlap.
+  const auto work = [&](auto SECOND, auto MASKED, const Buffer& in, int r0, int slot) {
+    const T *x = SECOND ? in.b : in.a, *y = SECOND ? in.a : in.b;
+    const auto rr = rows_at.here();
+    const auto cr = columns_at.here();
 #pragma unroll
-    for (int step = 0; step < D / 16; ++step) {
-      p = Mma<DT>::mul(rr.read(lq, 0, step), k[step], p);
-      dp = Mma<DT>::mul(rr.read(ld, 0, step), v[step], dp);
-    }
+    for (int h = 0; h < kRowsPass / 32; ++h) {
+      f32x16 p[SUBS] = {};
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const f32x4 lse = *reinterpret_cast<const f32x4*>(&stats[0][8 * u + lane / 32 * 4]);
-      const f32x4 delta = *reinterpret_cast<const f32x4*>(&stats[1][8 * u + lane / 32 * 4]);
+      for (int step = 0; step < D / 16; ++step) {
+        const V8 row = rr.read(x, 32 * h, step);
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int i = 4 * u + j;
-        p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - lse[j]);
-        if (masked) {
-          const int r = r0 + key_of(i) + lane / 32 * 4;
-          if (r < own.lo || r >= own.hi) p[i] = 0.0f;
+        for (int u = 0; u < SUBS; ++u) p[u] = Mma<DT>::mul(row, kv[u][step], p[u]);
+      }
+      V8 n[SUBS][2];
+#pragma unroll
+      for (int u = 0; u < SUBS; ++u) {
+        if (MASKED) {
+          const Range own = rows_of(run + 32 * u + lane % 32);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            const int r = r0 + 32 * h + key_of(i) + lane / 32 * 4;
+            if (r < own.lo || r >= own.hi) p[u][i] = -INFINITY;
+          }
         }
-        dp[i] = p[i] * (dp[i] - delta[j]);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) {
+          const f32x4 stat = *reinterpret_cast<const f32x4*>(&in.stats[SECOND][32 * h + 8 * c + lane / 32 * 4]);
+          const V8 given = SECOND ? handed[slot][pair][u][2 * h + c / 2][lane] : V8{};
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const int i = 4 * c + j;
+            p[u][i] = SECOND ? static_cast<float>(given[i % 8]) * (p[u][i] * lower - stat[j])
+                             : __builtin_amdgcn_exp2f(p[u][i] * scale2 - stat[j]);
+          }
+        }
+#pragma unroll
+        for (int step = 0; step < 2; ++step) {
+          n[u][step] = narrow<DT>(p[u], step);
+          if (!SECOND) handed[slot][pair][u][2 * h + step][lane] = n[u][step];
+        }
       }
+#pragma unroll
+      for (int step = 0; step < 2; ++step)
+#pragma unroll
+        for (int t = 0; t < D / 32; ++t) {
+          const V8 column = cr.read(y, 32 * h + 16 * step, t);
+#pragma unroll
+          for (int u = 0; u < SUBS; ++u) acc[u][t] = Mma<DT>::mul(column, n[u][step], acc[u][t]);
+        }
     }
-#pragma unroll
-    for (int step = 0; step < 2; ++step) {
-      const V8 pn = narrow<DT>(p, step), ds = narrow<DT>(dp, step);
-#pragma unroll
-      for (int t = 0; t < D / 32; ++t) {
-        dv[t] = Mma<DT>::mul(cr.read(ld, 16 * step, t), pn, dv[t]);
-        dk[t] = Mma<DT>::mul(cr.read(lq, 16 * step, t), ds, dk[t]);
-      }
+  };
+
+  // turn i: tile i + 1 comes, the pairs' first waves work on tile i and their second
+  // waves on tile i - 1
+  const int begin = all.lo / kRowsPass * kRowsPass, tiles = all.hi > begin ? (all.hi - begin + kRowsPass - 1) / kRowsPass : 0;
+  const auto turn = [&](Buffer& now, Buffer& before, Buffer& next, int i) {
+    landed();
+    __syncthreads();
+    if (i + 1 < tiles) issue(next, begin + (i + 1) * kRowsPass);
+    const int r0 = begin + i * kRowsPass;
+    constexpr std::true_type yes{};
+    constexpr std::false_type no{};
+    if (second) {
+      if (i > 0) work(yes, no, before, r0 - kRowsPass, (i - 1) & 1);
+    } else if (i < tiles) {
+      if (r0 < every.lo || r0 + kRowsPass > every.hi)
+        work(no, yes, now, r0, i & 1);
+      else
+        work(no, no, now, r0, i & 1);
+    }
+  };
+  if (tiles > 0) {
+    issue(buf0, begin);
+    for (int i = 0; i <= tiles; i += 3) {
+      turn(buf0, buf2, buf1, i);
+      if (i + 1 > tiles) break;
+      turn(buf1, buf0, buf2, i + 1);
+      if (i + 2 > tiles) break;
+      turn(buf2, buf1, buf0, i + 2);
     }
   }
-  if (key >= keys) return;
-  const int64_t at = ((s.b * a.rows_k + s.k0 + key) * a.hkv + hk) * a.d;
-  store_rows<DT, D>(static_cast<T*>(a.dk) + at, a.d, dk, a.scale);
-  store_rows<DT, D>(static_cast<T*>(a.dv) + at, a.d, dv, 1.0f);
+#pragma unroll
+  for (int u = 0; u < SUBS; ++u) {
+    const int key = run + 32 * u + lane % 32;
+    if (key >= keys) continue;
+    store_rows<DT, D>(static_cast<T*>(second ? a.dk : a.dv) + ((s.b * a.rows_k + s.k0 + key) * a.hkv + hk) * a.d, a.d, acc[u],
+                      second ? a.scale : lower);
+  }
 }
 
 // ---------------------------------------------------------------- host side
@@ -810,6 +921,7 @@ Args args_of(const fewbit_attn* a) {
   r.causal = a->causal;
   r.window = a->window;
   r.scale = a->scale;
+  r.by_g = {static_cast<uint32_t>(r.g), static_cast<uint32_t>(((uint64_t{1} << 32) + r.g - 1) / r.g)};
   r.splits = 1;
   return r;
 }
@@ -822,13 +934,21 @@ bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // 
                   : (bf16 ? launch(KERNEL<FEWBIT_BF16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)   \
                           : launch(KERNEL<FEWBIT_F16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)))
 
+// Runs of 64 keys where two of them and their gradients fit a wave's registers, else 32.
+int64_t keys_dkv(int d) { return kPairs * (d <= 64 ? 64 : 32); }
+
+hipError_t start_dkv(const Args& r, bool bf16, unsigned groups, hipStream_t st) {
+  return r.d <= 64 ? launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 64, 2> : attn_dkv_kernel<FEWBIT_F16, 64, 2>, dim3(groups), kThreadsPairs, st, r)
+                   : launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 128, 1> : attn_dkv_kernel<FEWBIT_F16, 128, 1>, dim3(groups), kThreadsPairs, st, r);
+}
+
 }  // namespace
 
 extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward) {
   const int rc = check(a);
   if (rc != FEWBIT_OK) return rc;
   const int64_t rows = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
-  if (backward) return rows * static_cast<int64_t>(sizeof(float));
+  if (backward) return 2 * rows * static_cast<int64_t>(sizeof(float));
   const Plan p = plan_of(a);
   return p.splits > 1 ? rows * p.splits * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float)) : 0;
 }
@@ -904,12 +1024,13 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   r.out = out;
   r.dout = dout;
   r.lse = const_cast<float*>(lse);
-  r.delta = static_cast<float*>(workspace);
+  r.stats = static_cast<float*>(workspace);
+  r.stats_delta = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
   r.dq = dq;
   r.dk = dk;
   r.dv = dv;
   const int64_t rows = a->rows_q * r.g;
-  const int64_t q_groups = places_of(a, rows, kRowsGroup) * r.hkv, k_groups = places_of(a, a->rows_k, kRowsGroup) * r.hkv;
+  const int64_t q_groups = places_of(a, rows, kRowsGroup) * r.hkv, k_groups = places_of(a, a->rows_k, keys_dkv(r.d)) * r.hkv;
   if (!fits_launch(q_groups) || !fits_launch(k_groups)) return FEWBIT_E_INVALID;
   if (a->rows_q > 0) {
     r.tiles = static_cast<int>(over(rows, kRowsGroup));
@@ -917,8 +1038,8 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
     if (rc != FEWBIT_OK) return rc;
   }
   if (a->rows_k > 0) {
-    r.tiles = static_cast<int>(over(a->rows_k, kRowsGroup));
-    rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dkv_kernel, r, k_groups, st));
+    r.tiles = static_cast<int>(over(a->rows_k, keys_dkv(r.d)));
+    rc = launch_status("fewbit_attn_bwd", start_dkv(r, bf16, static_cast<unsigned>(k_groups), st));
   }
   return rc;
 }
