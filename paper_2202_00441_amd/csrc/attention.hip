@@ -18,9 +18,7 @@
 // of the second product is V^T (or K^T, dO^T, Q^T): read from the row-major tile
 // in LDS by the transposing load, four rows at a time, in that order.
 //
-// Tiles lie in LDS row-major in 16-byte chunks, chunk c of row r at c ^ f(r): f
-// spreads both the 16-byte reads down a column of chunks and the transposing
-// reads of 4 rows x 32 bytes over all banks.
+// Tiles lie in LDS row-major in 16-byte chunks, chunk c of row r at c ^ f(r) (swizzle).
 #include <algorithm>
 #include <type_traits>
 
@@ -161,9 +159,21 @@ __device__ __forceinline__ bool find(const Args& a, bool keys, int times, int ro
   return true;
 }
 
+// Sixteen lanes that read a chunk each of rows one after another, and 32 lanes of a
+// transposing read, which take 64 bytes of four rows, then touch every bank once.
 template <int D>
 __device__ __forceinline__ int swizzle(int row) {
-  return D == 128 ? ((row & 7) << 1) ^ ((row >> 3) & 1) : ((row >> 1) & 3) << 1;
+  return D == 128 ? (row & 3) << 2 | (row >> 2 & 3) : (row >> 1 & 1) << 2 | (row >> 2 & 3);
+}
+
+// Elements that rows may lie apart for a lane's offset inside a load to fit 31 bits.
+constexpr int64_t kNear = int64_t{1} << 26;
+
+template <class T>
+__device__ __forceinline__ const T* uniform(const T* p) {
+  const uint64_t x = reinterpret_cast<uint64_t>(p);
+  const uint32_t lo = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x)), hi = __builtin_amdgcn_readfirstlane(static_cast<uint32_t>(x >> 32));
+  return reinterpret_cast<const T*>(static_cast<uint64_t>(hi) << 32 | lo);
 }
 
 // Brings a tile of ROWS rows of D elements to LDS, 16 bytes a lane and load, without
@@ -193,11 +203,57 @@ struct Stage {
   template <class F>
   __device__ __forceinline__ void issue(T* lds, F at) const {
 #pragma unroll
-    for (int j = 0; j < kLoads; ++j) {
-      const T* p = at(row + row_of(j)) + chunk[j % kKinds];
-      __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                       (__attribute__((address_space(3))) void*)(lds + row_of(j) * D), 16, 0, 0);
-    }
+    for (int j = 0; j < kLoads; ++j) load(at(row + row_of(j)) + chunk[j % kKinds], lds, j);
+  }
+  // The same for rows `stride` apart from `base` on (the same for all lanes), at most
+  // kNear: the address is a scalar and a lane's offset, which is there already.
+  __device__ __forceinline__ void issue(T* lds, const T* base, int64_t stride, const uint32_t (&offset)[kKinds]) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j)
+      load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(uniform(base + row_of(j) * stride)) + offset[j % kKinds]), lds, j);
+  }
+  // The same with an offset of its own for every load.
+  __device__ __forceinline__ void issue(T* lds, const T* base, const uint32_t (&offset)[kLoads]) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(uniform(base)) + offset[j]), lds, j);
+  }
+  template <class F>
+  __device__ __forceinline__ void offsets(F at, uint32_t (&offset)[kLoads]) const {
+#pragma unroll
+    for (int j = 0; j < kLoads; ++j) offset[j] = static_cast<uint32_t>(at(row + row_of(j)) + chunk[j % kKinds]) * 2;
+  }
+  __device__ __forceinline__ void offsets(int64_t stride, uint32_t (&offset)[kKinds]) const {
+#pragma unroll
+    for (int j = 0; j < kKinds; ++j) offset[j] = static_cast<uint32_t>(row * static_cast<int>(stride) + chunk[j]) * 2;
+  }
+
+ private:
+  __device__ __forceinline__ void load(const T* p, T* lds, int j) const {
+    __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
+                                     (__attribute__((address_space(3))) void*)(lds + row_of(j) * D), 16, 0, 0);
+  }
+};
+
+// Rows first .. of a tensor as a walk over tiles of ROWS wants them: whole tiles of
+// rows not too far apart by the quick way, the others with each row's own address.
+template <int DT, int D, int ROWS, int WAVES>
+struct Rows {
+  using T = typename Mma<DT>::T;
+  using S = Stage<DT, D, ROWS, WAVES>;
+  const T* base;
+  int64_t stride;
+  int last;             // the last row there is
+  bool near;
+  uint32_t offset[S::kKinds];
+  __device__ __forceinline__ Rows(const S& stage, const T* base_, int64_t stride_, int last_)
+      : base(base_), stride(stride_), last(last_), near(stride_ < kNear) {
+    stage.offsets(stride_, offset);
+  }
+  __device__ __forceinline__ void issue(const S& stage, T* lds, int first) const {
+    if (near && first + ROWS - 1 <= last)
+      stage.issue(lds, base + first * stride, stride, offset);
+    else
+      stage.issue(lds, [&](int i) { return base + min(first + i, last) * stride; });
   }
 };
 
@@ -238,7 +294,7 @@ template <int DT, int D>
 struct RowReader {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
-  int at;
+  int at;       // in bytes
   // A copy whose addresses are formed where they are used: the compiler else keeps the
   // address of every read of a tile in a register of its own throughout.
   __device__ __forceinline__ RowReader here() const {
@@ -248,10 +304,10 @@ struct RowReader {
   }
   __device__ __forceinline__ RowReader() {
     const int lane = threadIdx.x % kWave, row = lane % 32;
-    at = row * D + ((lane / 32) ^ swizzle<D>(row)) * 8;
+    at = (row * D + ((lane / 32) ^ swizzle<D>(row)) * 8) * 2;
   }
   __device__ __forceinline__ V8 read(const T* lds, int row0, int step) const {
-    return *reinterpret_cast<const V8*>(lds + row0 * D + (at ^ (step * 16)));
+    return *reinterpret_cast<const V8*>(reinterpret_cast<const char*>(lds + row0 * D) + (at ^ (step * 32)));
   }
 };
 
@@ -272,13 +328,13 @@ struct ColumnReader {
   __device__ __forceinline__ ColumnReader() {
     const int lane = threadIdx.x % kWave, i = lane % 16, row = 4 * (lane / 32) + i / 4;
     const int chunk = 2 * (lane / 16 % 2) + i % 4 / 2;
-    at = row * D + (chunk ^ swizzle<D>(row)) * 8 + i % 2 * 4;
+    at = (row * D + (chunk ^ swizzle<D>(row)) * 8 + i % 2 * 4) * 2;
   }
   __device__ __forceinline__ s16x4 four(const T* lds, int row0, int tile, int up) const {
-    // row0 is a multiple of 16; rows 8 further on have another bit of the swizzle (D = 128)
-    const int x = at ^ (tile * 32) ^ (D == 128 ? up * 8 : 0);
+    // row0 is a multiple of 16; rows 8 further on have another bit of the swizzle
+    const char* p = reinterpret_cast<const char*>(lds + (row0 + 8 * up) * D) + (at ^ (tile * 64) ^ (up * 32));
     using L = __attribute__((address_space(3))) s16x4*;
-    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((L)(const_cast<T*>(lds) + (row0 + 8 * up) * D + x));
+    return __builtin_amdgcn_ds_read_tr16_b64_v4i16((L)const_cast<char*>(p));
   }
   __device__ __forceinline__ V8 read(const T* lds, int row0, int tile) const {
     const s16x4 a = four(lds, row0, tile, 0), b = four(lds, row0, tile, 1);
@@ -340,7 +396,11 @@ __device__ __forceinline__ Range keys_of(const Args& a, const Seq& s, int pos) {
 __device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + i % 4; }      // plus 4 (lane / 32)
 
 // ---------------------------------------------------------------- forward
-// Softmax statistics and output of the lane's row.
+// Softmax statistics and output of the lane's row.  `most` is what exponentials are
+// taken from: a score of the row, at most kSlack (of base-2 logarithms) under its largest
+// so far.  Sums and outputs are rescaled only where a score exceeds that, not for every
+// new maximum; nothing is lost by it, exponentials below 2^kSlack round as those below 1.
+constexpr float kSlack = 8.0f;
 template <int D>
 struct Running {
   float most = -INFINITY, sum = 0.0f;       // sum: of this lane's half of the keys
@@ -376,8 +436,8 @@ __device__ __forceinline__ void attend(const typename Mma<DT>::T* lk, const type
     for (int i = 0; i < 16; ++i) most = fmaxf(most, s[u][i]);
   const Two both = halves32(most);
   most = fmaxf(both.a, both.b);
-  const float base = most == -INFINITY ? 0.0f : most * scale2;
-  if (__any(most != x.most)) {
+  if (__any((most - x.most) * scale2 > kSlack)) {
+    const float base = most == -INFINITY ? 0.0f : most * scale2;
     const float fade = __builtin_amdgcn_exp2f(x.most * scale2 - base);
     x.sum *= fade;
 #pragma unroll
@@ -386,6 +446,7 @@ __device__ __forceinline__ void attend(const typename Mma<DT>::T* lk, const type
       for (int i = 0; i < 16; ++i) x.o[t][i] *= fade;
     x.most = most;
   }
+  const float base = x.most == -INFINITY ? 0.0f : x.most * scale2;
   float sum = 0.0f;
 #pragma unroll
   for (int u = 0; u < SUBS; ++u)
@@ -435,13 +496,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
   const Stage<DT, D, kKeys, kWaves> stage(a.d, wave);
+  const Rows<DT, D, kKeys, kWaves> keys(stage, kb, a.ks[1], s.nk - 1), values(stage, vb, a.vs[1], s.nk - 1);
   const RowReader<DT, D> rr;
   const ColumnReader<DT, D> cr;
   Running<D> x;
   walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
-         stage.issue(to.a, [&](int i) { return kb + min(k0 + i, s.nk - 1) * a.ks[1]; });
-         stage.issue(to.b, [&](int i) { return vb + min(k0 + i, s.nk - 1) * a.vs[1]; });
+         keys.issue(stage, to.a, k0);
+         values.issue(stage, to.b, k0);
        },
        [&](const Pair<T, kKeys * D>& in, int k0) {
          attend<DT, D, kKeys / 32>(in.a, in.b, 0, k0, q, rr, cr, k0 < every.lo || k0 + kKeys > every.hi, own, a.scale * kLog2e, x);
@@ -485,14 +547,15 @@ __global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(const Args a) {
     const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
     const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
     const Stage<DT, D, 32, 1> stage(a.d, 0);
+    const Rows<DT, D, 32, 1> keys(stage, kb, a.ks[1], all.hi - 1), values(stage, vb, a.vs[1], all.hi - 1);
     const RowReader<DT, D> rr;
     const ColumnReader<DT, D> cr;
     const Range mine{max(own.lo, all.lo), min(own.hi, all.hi)};
     const Range sure{max(every.lo, all.lo), min(every.hi, all.hi)};
     walk<false>(all.lo / 32 * 32 + 32 * wave, kKeysSplit, all.hi, buf0[wave], buf1[wave],
                 [&](Pair<T, 32 * D>& to, int k0) {
-                  stage.issue(to.a, [&](int i) { return kb + min(k0 + i, all.hi - 1) * a.ks[1]; });
-                  stage.issue(to.b, [&](int i) { return vb + min(k0 + i, all.hi - 1) * a.vs[1]; });
+                  keys.issue(stage, to.a, k0);
+                  values.issue(stage, to.b, k0);
                 },
                 [&](const Pair<T, 32 * D>& in, int k0) {
                   attend<DT, D, 1>(in.a, in.b, 0, k0, q, rr, cr, k0 < sure.lo || k0 + 32 > sure.hi, mine, a.scale * kLog2e, x);
@@ -608,7 +671,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
   __shared__ Pair<T, kKeys * D> buf0, buf1;
-  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int hk = blockIdx.x % a.hkv, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
   Seq s;
   int tile;
   if (!find(a, false, a.g, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
@@ -644,20 +707,23 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   const Range own = keys_of(a, s, pos);
   const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
   const Range every{keys_of(a, s, max(w1, w0) / a.g).lo, keys_of(a, s, w0 / a.g).hi};
+  const Range any{keys_of(a, s, w0 / a.g).lo, keys_of(a, s, max(w1, w0) / a.g).hi};
 
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
   const Stage<DT, D, kKeys, kWaves> stage(a.d, wave);
+  const Rows<DT, D, kKeys, kWaves> keys(stage, kb, a.ks[1], s.nk - 1), values(stage, vb, a.vs[1], s.nk - 1);
   const RowReader<DT, D> rows_at;
   const ColumnReader<DT, D> columns_at;
   f32x16 dq[D / 32] = {};
   const float scale2 = a.scale * kLog2e;
   walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
-         stage.issue(to.a, [&](int i) { return kb + min(k0 + i, s.nk - 1) * a.ks[1]; });
-         stage.issue(to.b, [&](int i) { return vb + min(k0 + i, s.nk - 1) * a.vs[1]; });
+         keys.issue(stage, to.a, k0);
+         values.issue(stage, to.b, k0);
        },
        [&](const Pair<T, kKeys * D>& in, int k0) {
+         if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
          const auto rr = rows_at.here();
          const auto cr = columns_at.here();
          const bool masked = k0 < every.lo || k0 + kKeys > every.hi;
@@ -741,20 +807,30 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   };
   Range all{0, 0};
   if (first < s.nk) all = Range{rows_of(first).lo, rows_of(min(first + kGroup, s.nk) - 1).hi};
-  const Range every{rows_of(run + kRun - 1).lo, run + kRun <= s.nk ? rows_of(run).hi : 0};
+  const Range every{rows_of(run + kRun - 1).lo, run + kRun <= s.nk ? rows_of(run).hi : 0};      // that all keys of the run are seen by
+  const Range any{rows_of(run).lo, run < s.nk ? rows_of(min(run + kRun, s.nk) - 1).hi : 0};      // that any is
 
   const T* qb = static_cast<const T*>(a.q) + s.b * a.qs[0] + s.q0 * a.qs[1] + static_cast<int64_t>(hk) * a.g * a.qs[2];
   const T* db = static_cast<const T*>(a.dout) + s.b * a.ds[0] + s.q0 * a.ds[1] + static_cast<int64_t>(hk) * a.g * a.ds[2];
   const int64_t sb = (s.b * a.hq + static_cast<int64_t>(hk) * a.g) * a.rows_q + s.q0;
   const Stage<DT, D, kRowsPass, kPairs> stage(a.d, pair);
+  const T* base = second ? db : qb;
+  const int64_t pos_stride = second ? a.ds[1] : a.qs[1], head_stride = second ? a.ds[2] : a.qs[2];
+  // with a power of two of heads to a key head, rows of whole tiles lie alike in all tiles
+  const int g_bits = __builtin_ctz(a.g);
+  const bool near = a.g == 1 << g_bits && a.g <= kRowsPass && pos_stride < kNear / 16 && head_stride < kNear / 16;
+  uint32_t offset[decltype(stage)::kLoads];
+  stage.offsets([&](int i) { return (i >> g_bits) * static_cast<int>(pos_stride) + (i & (a.g - 1)) * static_cast<int>(head_stride); }, offset);
   const auto issue = [&](Buffer& to, int r0) {
     // the first waves of the pairs bring Q and lse, the second dO and delta
-    const T* base = second ? db : qb;
-    const int64_t pos_stride = second ? a.ds[1] : a.qs[1], head_stride = second ? a.ds[2] : a.qs[2];
-    stage.issue(second ? to.b : to.a, [&](int i) {
-      const int r = min(r0 + i, rows - 1), pos = a.by_g.divide(r);
-      return base + pos * pos_stride + (r - pos * a.g) * head_stride;
-    });
+    T* lds = second ? to.b : to.a;
+    if (near && r0 + kRowsPass <= rows)
+      stage.issue(lds, base + static_cast<int64_t>(r0 >> g_bits) * pos_stride, offset);
+    else
+      stage.issue(lds, [&](int i) {
+        const int r = min(r0 + i, rows - 1), pos = a.by_g.divide(r);
+        return base + pos * pos_stride + (r - pos * a.g) * head_stride;
+      });
     if (pair == 0) {                 // lse for the first, delta for the second
       const int r = min(r0 + lane, rows - 1), pos = a.by_g.divide(r);
       const float* p = a.stats + (second ? a.stats_delta : 0) + sb + (r - pos * a.g) * a.rows_q + pos;
@@ -831,8 +907,10 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
     const int r0 = begin + i * kRowsPass;
     constexpr std::true_type yes{};
     constexpr std::false_type no{};
+    const int mine = second ? r0 - kRowsPass : r0;            // rows that none of the run's keys is seen by are left out
+    if (mine + kRowsPass <= any.lo || mine >= any.hi) return;
     if (second) {
-      if (i > 0) work(yes, no, before, r0 - kRowsPass, (i - 1) & 1);
+      if (i > 0) work(yes, no, before, mine, (i - 1) & 1);
     } else if (i < tiles) {
       if (r0 < every.lo || r0 + kRowsPass > every.hi)
         work(no, yes, now, r0, i & 1);
