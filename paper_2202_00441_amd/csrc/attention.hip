@@ -77,7 +77,7 @@ struct Args {
   float scale;
   Divisor by_g;
   int tiles;                          // of a sequence (packed: places for tiles of all)
-  int chunk, splits;                  // keys of a split, splits
+  int shares, unit_rows;              // split forward: workgroups of a key head, rows of a unit
 };
 
 // One (sequence, key head): where its rows begin and how many there are.
@@ -181,7 +181,8 @@ __device__ __forceinline__ const T* uniform(const T* p) {
 // which chunk of its row a lane asks for.  Rows past the last are read as the last,
 // chunks past head_dim as the first: what multiplies them is 0 (masked scores; the
 // other operand's elements past head_dim) or is not stored.
-template <int DT, int D, int ROWS, int WAVES>
+// POLICY: cache policy of the loads, 2 for what is read once (non-temporal).
+template <int DT, int D, int ROWS, int WAVES, int POLICY = 0>
 struct Stage {
   using T = typename Mma<DT>::T;
   static constexpr int kChunks = D / 8, kRowsLoad = kWave / kChunks, kLoads = ROWS / kRowsLoad / WAVES;
@@ -230,16 +231,16 @@ struct Stage {
  private:
   __device__ __forceinline__ void load(const T* p, T* lds, int j) const {
     __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)p,
-                                     (__attribute__((address_space(3))) void*)(lds + row_of(j) * D), 16, 0, 0);
+                                     (__attribute__((address_space(3))) void*)(lds + row_of(j) * D), 16, 0, POLICY);
   }
 };
 
 // Rows first .. of a tensor as a walk over tiles of ROWS wants them: whole tiles of
 // rows not too far apart by the quick way, the others with each row's own address.
-template <int DT, int D, int ROWS, int WAVES>
+template <int DT, int D, int ROWS, int WAVES, int POLICY = 0>
 struct Rows {
   using T = typename Mma<DT>::T;
-  using S = Stage<DT, D, ROWS, WAVES>;
+  using S = Stage<DT, D, ROWS, WAVES, POLICY>;
   const T* base;
   int64_t stride;
   int last;             // the last row there is
@@ -264,25 +265,28 @@ struct Pair {
   __attribute__((aligned(16))) T b[N];
 };
 
-// This wave's loads to LDS are done.
-__device__ __forceinline__ void landed() { __builtin_amdgcn_s_waitcnt(0x0f70); }      // vmcnt(0)
+// All but the last N of this wave's loads to LDS are done.
+template <int N>
+__device__ __forceinline__ void landed() {
+  static_assert(N < 16, "one field of the wait's operand");
+  __builtin_amdgcn_s_waitcnt(0x0f70 | N);       // vmcnt(N), nothing else
+}
 
 // Walks tiles at, at + step, .. < end through two buffers: while one is worked on the
 // next tile comes into the other.  (Buffers are apart so that the compiler does not make
 // reads of one wait for loads into the other.)
-// GROUP: the buffers are the workgroup's, else each wave's own.
-template <bool GROUP, class Buffer, class Issue, class Work>
+template <class Buffer, class Issue, class Work>
 __device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work) {
   if (at >= end) return;
   issue(a, at);
   for (; at < end; at += 2 * step) {
-    landed();
-    if (GROUP) __syncthreads();
+    landed<0>();
+    __syncthreads();
     if (at + step < end) issue(b, at + step);
     work(a, at);
     if (at + step >= end) break;
-    landed();
-    if (GROUP) __syncthreads();
+    landed<0>();
+    __syncthreads();
     if (at + 2 * step < end) issue(a, at + 2 * step);
     work(b, at + step);
   }
@@ -407,18 +411,18 @@ struct Running {
   f32x16 o[D / 32] = {};
 };
 
-// SUBS tiles of 32 keys, from row0 of the tiles in LDS and key k0 of the sequence.
+// The probabilities (from x.most) of SUBS runs of 32 keys from key k0 of the sequence
+// on, their keys in lk.
 template <int DT, int D, int SUBS>
-__device__ __forceinline__ void attend(const typename Mma<DT>::T* lk, const typename Mma<DT>::T* lv, int row0, int k0,
-                                       const typename Mma<DT>::V8 (&q)[D / 16], const RowReader<DT, D>& rows,
-                                       const ColumnReader<DT, D>& columns, bool masked, Range r, float scale2, Running<D>& x) {
+__device__ __forceinline__ void score(const typename Mma<DT>::T* lk, int k0, const typename Mma<DT>::V8 (&q)[D / 16],
+                                      const RowReader<DT, D>& rows, bool masked, Range r, float scale2, Running<D>& x,
+                                      f32x16 (&s)[SUBS]) {
   const int half = threadIdx.x % kWave / 32 * 4;
-  f32x16 s[SUBS];
 #pragma unroll
   for (int u = 0; u < SUBS; ++u) {
     s[u] = f32x16{};
 #pragma unroll
-    for (int step = 0; step < D / 16; ++step) s[u] = Mma<DT>::mul(rows.read(lk, row0 + 32 * u, step), q[step], s[u]);
+    for (int step = 0; step < D / 16; ++step) s[u] = Mma<DT>::mul(rows.read(lk, 32 * u, step), q[step], s[u]);
   }
   if (masked) {
 #pragma unroll
@@ -456,19 +460,26 @@ __device__ __forceinline__ void attend(const typename Mma<DT>::T* lk, const type
       sum += s[u][i];
     }
   x.sum += sum;
+}
+
+// Adds up the values, in lv, by their probabilities.
+template <int DT, int D, int SUBS>
+__device__ __forceinline__ void gather(const typename Mma<DT>::T* lv, const ColumnReader<DT, D>& columns,
+                                       const f32x16 (&s)[SUBS], Running<D>& x) {
 #pragma unroll
   for (int u = 0; u < SUBS; ++u)
 #pragma unroll
     for (int step = 0; step < 2; ++step) {
       const auto p = narrow<DT>(s[u], step);
 #pragma unroll
-      for (int t = 0; t < D / 32; ++t) x.o[t] = Mma<DT>::mul(columns.read(lv, row0 + 32 * u + 16 * step, t), p, x.o[t]);
+      for (int t = 0; t < D / 32; ++t) x.o[t] = Mma<DT>::mul(columns.read(lv, 32 * u + 16 * step, t), p, x.o[t]);
     }
 }
 
 constexpr int kThreads = 256, kWaves = kThreads / kWave;
 constexpr int kRowsWave = 32, kRowsGroup = kWaves * kRowsWave;      // rows of a wave and of a workgroup
 constexpr int kKeys = 64;                                           // keys of a pass
+constexpr int kPassesShare = 2;                                     // of a share of the split forward at least
 
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
@@ -500,13 +511,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   const RowReader<DT, D> rr;
   const ColumnReader<DT, D> cr;
   Running<D> x;
-  walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+  walk(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
          keys.issue(stage, to.a, k0);
          values.issue(stage, to.b, k0);
        },
        [&](const Pair<T, kKeys * D>& in, int k0) {
-         attend<DT, D, kKeys / 32>(in.a, in.b, 0, k0, q, rr, cr, k0 < every.lo || k0 + kKeys > every.hi, own, a.scale * kLog2e, x);
+         f32x16 p[kKeys / 32];
+         score<DT, D, kKeys / 32>(in.a, k0, q, rr, k0 < every.lo || k0 + kKeys > every.hi, own, a.scale * kLog2e, x, p);
+         gather<DT, D, kKeys / 32>(in.b, cr, p, x);
        });
   if (!there) return;
   const Two both = halves32(x.sum);
@@ -515,144 +528,249 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = sum == 0.0f ? -INFINITY : x.most * a.scale + logf(sum);
 }
 
-// Few rows over many keys (single tokens over a cache): a workgroup takes 32 rows
-// and one run of keys, and its waves different keys of each pass, whose results
-// they add up at the end.  Runs' results are added by a second kernel.
+// Few rows over many keys (single tokens over a cache).  Work is cut into units of 32
+// rows of one sequence and key head, and the units' passes of 128 keys, all in one line,
+// into equal shares, one to a workgroup: whatever the lengths of the caches, all
+// workgroups end at the same time.  A workgroup's waves take different keys of each pass
+// and add their results up at the end of the unit, or of the share; what belongs to a
+// unit that is not all in one share is left in the workspace and added by a second
+// kernel.  Share w and unit u meet at most once, and of all meetings in line each has
+// the next w or the next u: w + u numbers them.
 constexpr int kKeysSplit = 32 * kWaves;
 
-template <int DT, int D>
-__global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(const Args a) {
-  using T = typename Mma<DT>::T;
-  __shared__ Pair<T, 32 * D> buf0[kWaves], buf1[kWaves];
-  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
-  const int split = blockIdx.x / a.hkv % a.splits;
+// Unit `unit`: its sequence, and the keys that its rows see, from a multiple of 32 on.
+struct Unit {
   Seq s;
-  int tile;
-  if (!find(a, false, a.g, kRowsWave, blockIdx.x / a.hkv / a.splits, s, tile)) return;
-  const int rows = s.nq * a.g, first = tile * kRowsWave;
-  if (first >= rows) return;
-  const int row = first + lane % 32;
-  const bool there = row < rows;
-  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
-  const Range own = keys_of(a, s, pos);
-  const Range every{keys_of(a, s, (min(first + kRowsWave, rows) - 1) / a.g).lo, keys_of(a, s, first / a.g).hi};
-  Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsWave, rows) - 1) / a.g).hi};
-  all.lo = max(all.lo, split * a.chunk);
-  all.hi = static_cast<int>(min(static_cast<int64_t>(all.hi), (split + static_cast<int64_t>(1)) * a.chunk));
-  const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head;           // the row in dense layouts
-  Running<D> x;
-  if (all.lo < all.hi) {
-    typename Mma<DT>::V8 q[D / 16];
-    load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
-    const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
-    const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
-    const Stage<DT, D, 32, 1> stage(a.d, 0);
-    const Rows<DT, D, 32, 1> keys(stage, kb, a.ks[1], all.hi - 1), values(stage, vb, a.vs[1], all.hi - 1);
-    const RowReader<DT, D> rr;
-    const ColumnReader<DT, D> cr;
-    const Range mine{max(own.lo, all.lo), min(own.hi, all.hi)};
-    const Range sure{max(every.lo, all.lo), min(every.hi, all.hi)};
-    walk<false>(all.lo / 32 * 32 + 32 * wave, kKeysSplit, all.hi, buf0[wave], buf1[wave],
-                [&](Pair<T, 32 * D>& to, int k0) {
-                  keys.issue(stage, to.a, k0);
-                  values.issue(stage, to.b, k0);
-                },
-                [&](const Pair<T, 32 * D>& in, int k0) {
-                  attend<DT, D, 1>(in.a, in.b, 0, k0, q, rr, cr, k0 < sure.lo || k0 + 32 > sure.hi, mine, a.scale * kLog2e, x);
-                });
-    // the waves' results: statistics, then outputs one after another
-    __syncthreads();
-    float* stats = reinterpret_cast<float*>(buf0);          // [wave][2][32]
-    const Two both = halves32(x.sum);
-    x.sum = both.a + both.b;
-    if (lane < 32) {
-      stats[wave * 64 + lane] = x.most;
-      stats[wave * 64 + 32 + lane] = x.sum;
-    }
-    __syncthreads();
-    float most = -INFINITY;
-    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[w * 64 + lane % 32]);
-    const float base = most == -INFINITY ? 0.0f : most;
-    const float scale2 = a.scale * kLog2e;
-    float sum = 0.0f;
-    for (int w = 0; w < kWaves; ++w)
-      sum += stats[w * 64 + 32 + lane % 32] * __builtin_amdgcn_exp2f((stats[w * 64 + lane % 32] - base) * scale2);
-    const float fade = __builtin_amdgcn_exp2f((x.most - base) * scale2);
-    x.most = most;
-    x.sum = sum;
-    __syncthreads();
-    float* acc = reinterpret_cast<float*>(buf0);            // [register][lane]
-    for (int w = 1; w < kWaves; ++w) {
-      if (wave == w) {
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) acc[(t * 16 + i) * kWave + lane] = x.o[t][i] * fade;
-      }
-      __syncthreads();
-      if (wave == 0) {
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-          for (int i = 0; i < 16; ++i) x.o[t][i] = (w == 1 ? x.o[t][i] * fade : x.o[t][i]) + acc[(t * 16 + i) * kWave + lane];
-      }
-      __syncthreads();
-    }
-  }
-  if (wave != 0 || !there) return;
-  const float inverse = x.sum > 0.0f || x.sum != x.sum ? 1.0f / x.sum : 0.0f;
-  const float lse = x.sum == 0.0f ? -INFINITY : x.most * a.scale + logf(x.sum);
-  if (a.splits == 1) {
-    store_rows<DT, D>(static_cast<T*>(a.o) + at * a.d, a.d, x.o, inverse);
-    if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = lse;
-    return;
-  }
-  const int64_t part = at * a.splits + split;
-  if (lane < 32) a.part_lse[part] = lse;
-  if (lse == -INFINITY) return;                             // its output is not read
-  float* out = a.part_o + part * a.d;
-#pragma unroll
-  for (int t = 0; t < D / 32; ++t)
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int c = 32 * t + 8 * u + lane / 32 * 4;
-      if (c < a.d)
-        *reinterpret_cast<f32x4*>(out + c) = f32x4{x.o[t][4 * u], x.o[t][4 * u + 1], x.o[t][4 * u + 2], x.o[t][4 * u + 3]} * inverse;
-    }
+  int first, rows;      // of its rows, and of all rows of the sequence
+  Range keys;
+  int passes;           // at least one
+};
+__device__ __forceinline__ Unit unit_of(const Args& a, int unit) {
+  Unit u;
+  u.s.b = unit / a.tiles;
+  u.s.q0 = u.s.k0 = 0;
+  u.s.nq = static_cast<int>(a.rows_q);
+  u.s.nk = a.k_len ? clamped(a.k_len[u.s.b], a.rows_k) : static_cast<int>(a.rows_k);
+  u.rows = u.s.nq * a.g;
+  u.first = unit % a.tiles * kRowsWave;
+  u.keys.lo = keys_of(a, u.s, u.first / a.g).lo / 32 * 32;
+  u.keys.hi = max(u.keys.lo, keys_of(a, u.s, (min(u.first + kRowsWave, u.rows) - 1) / a.g).hi);
+  u.passes = max(1, (u.keys.hi - u.keys.lo + kKeysSplit - 1) / kKeysSplit);
+  return u;
 }
 
-// out = sum of the runs' outputs, each by its share exp(lse_run - lse); a wave takes
-// a row, two elements a lane.
+// All units' passes in line: passes of a share, and of all units, and those before unit
+// `stop`.  Units are alike where a sequence is one unit and none is shorter.
+struct Line {
+  int share, all, before;
+};
+__device__ __forceinline__ Line line_of(const Args& a, int stop) {
+  Line l;
+  if (!a.k_len && a.tiles == 1) {
+    const int each = unit_of(a, 0).passes;
+    l.all = each * a.batch;
+    l.before = each * stop;
+  } else {
+    const int lane = threadIdx.x % kWave, units = a.batch * a.tiles;
+    int all = 0, before = 0;
+    for (int u = lane; u < units; u += kWave) {
+      const int n = unit_of(a, u).passes;
+      all += n;
+      if (u < stop) before += n;
+    }
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+      all += __shfl_xor(all, step);
+      before += __shfl_xor(before, step);
+    }
+    l.all = __builtin_amdgcn_readfirstlane(all);
+    l.before = __builtin_amdgcn_readfirstlane(before);
+  }
+  l.share = max(kPassesShare, (l.all + a.shares - 1) / a.shares);
+  return l;
+}
+
+// The unit that pass `at` of the line is in, and which of its passes it is.
+__device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
+  if (!a.k_len && a.tiles == 1) {
+    const int each = unit_of(a, 0).passes, unit = at / each;
+    pass = at - unit * each;
+    return unit;
+  }
+  const int lane = threadIdx.x % kWave, units = a.batch * a.tiles;
+  int before = 0;
+  for (int u0 = 0; u0 < units; u0 += kWave) {
+    const int own = u0 + lane < units ? unit_of(a, u0 + lane).passes : 0;
+    int sum = own;
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+      const int other = __shfl_up(sum, step);
+      if (lane >= step) sum += other;
+    }
+    const uint64_t past = __ballot(at < before + sum);
+    if (past) {
+      const int first = __builtin_ctzll(past);
+      pass = __builtin_amdgcn_readfirstlane(at - before - __shfl(sum - own, first));
+      return __builtin_amdgcn_readfirstlane(u0 + first);
+    }
+    before += __builtin_amdgcn_readfirstlane(__shfl(sum, kWave - 1));
+  }
+  pass = 0;
+  return units;
+}
+
+// ONCE: all rows of a sequence are one unit, so keys are read once and not kept in the
+// caches (64 caches of 8192 keys, 16 heads to 4: 200 -> 177 us).
+template <int DT, int D, bool ONCE>
+__global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
+  using T = typename Mma<DT>::T;
+  __shared__ __attribute__((aligned(16))) T lk[kWaves][32 * D], lv[kWaves][32 * D];
+  __shared__ float stats[kWaves][2][32];
+  const int hk = blockIdx.x % a.hkv, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int share = blockIdx.x / a.hkv;
+  const Line line = line_of(a, 0);
+  if (share > (line.all - 1) / line.share) return;
+  int at = share * line.share;
+  const int end = at + min(line.share, line.all - at);
+  int pass;
+  for (int unit = unit_at(a, at, pass); at < end; ++unit, pass = 0) {
+    const Unit u = unit_of(a, unit);
+    const Seq& s = u.s;
+    const int passes = min(u.passes - pass, end - at);
+    const bool whole = passes == u.passes;
+    at += passes;
+    const int row = u.first + lane % 32;
+    const bool there = row < u.rows;
+    const int pos = min(row, u.rows - 1) / a.g, head = hk * a.g + min(row, u.rows - 1) % a.g;
+    const Range own = keys_of(a, s, pos);
+    const Range every{keys_of(a, s, (min(u.first + kRowsWave, u.rows) - 1) / a.g).lo, keys_of(a, s, u.first / a.g).hi};
+    Range all;
+    all.lo = u.keys.lo + pass * kKeysSplit;
+    all.hi = min(u.keys.hi, all.lo + passes * kKeysSplit);
+    Running<D> x;
+    if (all.lo < all.hi) {
+      typename Mma<DT>::V8 q[D / 16];
+      load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + pos * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+      const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + hk * a.ks[2];
+      const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + hk * a.vs[2];
+      constexpr int kPolicy = ONCE ? 2 : 0;
+      const Stage<DT, D, 32, 1, kPolicy> stage(a.d, 0);
+      const Rows<DT, D, 32, 1, kPolicy> keys(stage, kb, a.ks[1], all.hi - 1), values(stage, vb, a.vs[1], all.hi - 1);
+      const RowReader<DT, D> rr;
+      const ColumnReader<DT, D> cr;
+      // Each wave has buffers of its own: while it works on keys the next keys, and while
+      // it works on values the next values, are on their way.
+      constexpr int kLoads = decltype(stage)::kLoads;
+      int k0 = all.lo + 32 * wave;
+      if (k0 < all.hi) {
+        keys.issue(stage, lk[wave], k0);
+        values.issue(stage, lv[wave], k0);
+      }
+      for (; k0 < all.hi; k0 += kKeysSplit) {
+        f32x16 p[1];
+        landed<kLoads>();
+        score<DT, D, 1>(lk[wave], k0, q, rr.here(), k0 < every.lo || k0 + 32 > min(every.hi, all.hi), Range{own.lo, min(own.hi, all.hi)},
+                        a.scale * kLog2e, x, p);
+        keys.issue(stage, lk[wave], k0 + kKeysSplit);       // past the end: the last row, again and again
+        landed<kLoads>();
+        gather<DT, D, 1>(lv[wave], cr.here(), p, x);
+        values.issue(stage, lv[wave], k0 + kKeysSplit);
+      }
+      landed<0>();
+    }
+    // The waves' results.  Wave t adds up all waves' columns 32 t ..+31 and writes them;
+    // the others' come through LDS, three parts for each t.
+    const Two both = halves32(x.sum);
+    if (lane < 32) {
+      stats[wave][0][lane] = x.most;
+      stats[wave][1][lane] = both.a + both.b;
+    }
+    __syncthreads();
+    float most = -INFINITY, sum = 0.0f;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) most = fmaxf(most, stats[w][0][lane % 32]);
+    const float base = most == -INFINITY ? 0.0f : most, scale2 = a.scale * kLog2e;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w)
+      sum += stats[w][1][lane % 32] * __builtin_amdgcn_exp2f((stats[w][0][lane % 32] - base) * scale2);
+    const float fade = __builtin_amdgcn_exp2f((x.most - base) * scale2);
+    const auto parts = [&](int t) { return reinterpret_cast<float*>(t < D / 64 ? lk : lv) + t % (D / 64) * 3 * 16 * kWave + lane; };
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      if (wave == t) continue;
+      float* to = parts(t) + (wave - (wave > t)) * 16 * kWave;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) to[i * kWave] = x.o[t][i] * fade;
+    }
+    __syncthreads();
+    const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+    const float lse = sum == 0.0f ? -INFINITY : most * a.scale + logf(sum);
+    const int64_t part = (static_cast<int64_t>(share + unit) * a.hkv + hk) * a.unit_rows + lane % 32;
+    if (there && wave == 0 && lane < 32) (whole ? a.lse[(s.b * a.hq + head) * a.rows_q + pos] : a.part_lse[part]) = lse;
+#pragma unroll
+    for (int t = 0; t < D / 32; ++t) {
+      if (wave != t) continue;
+      const float* from = parts(t);
+      float o[16];
+#pragma unroll
+      for (int i = 0; i < 16; ++i)
+        o[i] = (x.o[t][i] * fade + from[i * kWave] + from[(16 + i) * kWave] + from[(32 + i) * kWave]) * inverse;
+#pragma unroll
+      for (int c4 = 0; c4 < 4; ++c4) {
+        const int c = 32 * t + 8 * c4 + lane / 32 * 4;
+        if (!there || c >= a.d) continue;
+        const f32x4 y{o[4 * c4], o[4 * c4 + 1], o[4 * c4 + 2], o[4 * c4 + 3]};
+        if (whole)
+          *reinterpret_cast<typename Mma<DT>::V4*>(static_cast<T*>(a.o) + ((s.b * a.rows_q + pos) * a.hq + head) * a.d + c) =
+              __builtin_convertvector(y, typename Mma<DT>::V4);
+        else
+          *reinterpret_cast<f32x4*>(a.part_o + part * a.d + c) = y;
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// Rows of units that several shares worked on: out = sum of their outputs, each by its
+// weight exp(lse_share - lse); a wave takes a row, two elements a lane.
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
   using T = typename Mma<DT>::T;
-  const int lane = threadIdx.x % kWave;
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + threadIdx.x / kWave;
-  const int64_t rows = a.batch * a.rows_q;
-  if (at >= rows * a.hq) return;
-  const float* lse = a.part_lse + at * a.splits;
+  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + wave;       // unit, key head, row of 32
+  const int unit = static_cast<int>(at / (a.unit_rows * a.hkv)), rest = static_cast<int>(at % (a.unit_rows * a.hkv));
+  if (unit >= a.batch * a.tiles) return;
+  const Unit u = unit_of(a, unit);
+  const int hk = rest / a.unit_rows, row = u.first + rest % a.unit_rows;
+  if (row >= u.rows) return;
+  const Line line = line_of(a, unit);
+  const int first = line.before / line.share, last = (line.before + u.passes - 1) / line.share;
+  if (first == last) return;
+  const int64_t step = static_cast<int64_t>(a.hkv) * a.unit_rows;
+  const int64_t part = (static_cast<int64_t>(first + unit) * a.hkv + hk) * a.unit_rows + rest % a.unit_rows;
   float most = -INFINITY;
-  for (int i = lane; i < a.splits; i += kWave) most = fmaxf(most, lse[i]);
+  for (int i = lane; i <= last - first; i += kWave) most = fmaxf(most, a.part_lse[part + i * step]);
   most = across<6>(most, [](float x, float y) { return fmaxf(x, y); });
   const float base = most == -INFINITY ? 0.0f : most;
   float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-  for (int i = 0; i < a.splits; ++i) {
-    const float w = __builtin_amdgcn_exp2f((lse[i] - base) * kLog2e);
+#pragma unroll 4
+  for (int i = 0; i <= last - first; ++i) {
+    const float w = __builtin_amdgcn_exp2f((a.part_lse[part + i * step] - base) * kLog2e);
     sum += w;
-    if (lse[i] != -INFINITY && 2 * lane < a.d) {
-      const float* o = a.part_o + (at * a.splits + i) * a.d + 2 * lane;
+    if (2 * lane < a.d) {
+      const float* o = a.part_o + (part + i * step) * a.d + 2 * lane;
       o0 += w * o[0];
       o1 += w * o[1];
     }
   }
   const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  const int pos = row / a.g, head = hk * a.g + row % a.g;
   if (2 * lane < a.d) {
-    T* out = static_cast<T*>(a.o) + at * a.d + 2 * lane;
+    T* out = static_cast<T*>(a.o) + ((u.s.b * a.rows_q + pos) * a.hq + head) * a.d + 2 * lane;
     out[0] = static_cast<T>(o0 * inverse);
     out[1] = static_cast<T>(o1 * inverse);
   }
-  const int64_t row = at / a.hq, head = at % a.hq, b = row / a.rows_q;
-  if (lane == 0) a.lse[(b * a.hq + head) * a.rows_q + row % a.rows_q] = sum == 0.0f ? -INFINITY : base + logf(sum);
+  if (lane == 0) a.lse[(u.s.b * a.hq + head) * a.rows_q + pos] = sum == 0.0f ? -INFINITY : base + logf(sum);
 }
 
 // ---------------------------------------------------------------- backward
@@ -717,7 +835,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   const ColumnReader<DT, D> columns_at;
   f32x16 dq[D / 32] = {};
   const float scale2 = a.scale * kLog2e;
-  walk<true>(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+  walk(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
          keys.issue(stage, to.a, k0);
          values.issue(stage, to.b, k0);
@@ -901,7 +1019,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   // waves on tile i - 1
   const int begin = all.lo / kRowsPass * kRowsPass, tiles = all.hi > begin ? (all.hi - begin + kRowsPass - 1) / kRowsPass : 0;
   const auto turn = [&](Buffer& now, Buffer& before, Buffer& next, int i) {
-    landed();
+    landed<0>();
     __syncthreads();
     if (i + 1 < tiles) issue(next, begin + (i + 1) * kRowsPass);
     const int r0 = begin + i * kRowsPass;
@@ -963,19 +1081,27 @@ int64_t places_of(const fewbit_attn* a, int64_t rows, int64_t per) {
   return a->cu_q ? over(rows, per) + a->batch + 1 : over(rows, per) * a->batch;
 }
 
-// How the forward runs: keys of a split, and how many; 0: the kernel for many rows.
-struct Plan {
-  int64_t chunk, splits;
-};
-Plan plan_of(const fewbit_attn* a) {
+// Rows of a unit of the forward that splits keys.
+int64_t unit_rows(const fewbit_attn* a) { return std::min<int64_t>(kRowsWave, a->rows_q * (a->heads_q / a->heads_kv)); }
+
+// Shares per key head of the forward that splits keys; 0: the kernel for many rows.
+int64_t shares_of(const fewbit_attn* a) {
   const int64_t rows = a->rows_q * (a->heads_q / a->heads_kv);
-  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return {0, 0};
+  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return 0;
   const int64_t many = over(rows, kRowsGroup) * a->heads_kv * a->batch, cus = device_cus();
-  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return {0, 0};
-  const int64_t few = over(rows, kRowsWave) * a->heads_kv * a->batch;
-  const int64_t splits = std::max<int64_t>(1, std::min(over(4 * cus, few), over(a->rows_k, 2 * kKeysSplit)));
-  const int64_t chunk = over(over(a->rows_k, splits), kKeysSplit) * kKeysSplit;
-  return {chunk, over(a->rows_k, chunk)};
+  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return 0;
+  // as many workgroups as the chip holds at once, no more than there are passes
+  const int64_t units = over(rows, kRowsWave) * a->batch, passes = units * over(a->rows_k + 31, kKeysSplit);
+  if (units >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return 0;
+  return std::max<int64_t>(1, std::min((a->head_dim <= 64 ? 3 : 2) * cus / a->heads_kv, over(passes, kPassesShare)));
+}
+
+// Whether no unit is in two shares, as far as the host can tell.
+bool all_whole(const fewbit_attn* a, int64_t shares) {
+  if (a->k_len || a->rows_q * (a->heads_q / a->heads_kv) > kRowsWave) return false;
+  const int64_t lo = a->window ? std::max<int64_t>(0, a->rows_k - a->rows_q + 1 - a->window) / 32 * 32 : 0;
+  const int64_t each = std::max<int64_t>(1, over(a->rows_k - lo, kKeysSplit));
+  return std::max<int64_t>(kPassesShare, over(each * a->batch, shares)) % each == 0;
 }
 
 Args args_of(const fewbit_attn* a) {
@@ -1000,7 +1126,6 @@ Args args_of(const fewbit_attn* a) {
   r.window = a->window;
   r.scale = a->scale;
   r.by_g = {static_cast<uint32_t>(r.g), static_cast<uint32_t>(((uint64_t{1} << 32) + r.g - 1) / r.g)};
-  r.splits = 1;
   return r;
 }
 
@@ -1011,6 +1136,12 @@ bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // 
                           : launch(KERNEL<FEWBIT_F16, 64>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS))    \
                   : (bf16 ? launch(KERNEL<FEWBIT_BF16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)   \
                           : launch(KERNEL<FEWBIT_F16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)))
+
+template <bool ONCE>
+hipError_t start_split(const Args& r, bool bf16, unsigned groups, hipStream_t st) {
+  return r.d <= 64 ? launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 64, ONCE> : attn_split_kernel<FEWBIT_F16, 64, ONCE>, dim3(groups), kThreads, st, r)
+                   : launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 128, ONCE> : attn_split_kernel<FEWBIT_F16, 128, ONCE>, dim3(groups), kThreads, st, r);
+}
 
 // Runs of 64 keys where two of them and their gradients fit a wave's registers, else 32.
 int64_t keys_dkv(int d) { return kPairs * (d <= 64 ? 64 : 32); }
@@ -1027,8 +1158,8 @@ extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward)
   if (rc != FEWBIT_OK) return rc;
   const int64_t rows = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
   if (backward) return 2 * rows * static_cast<int64_t>(sizeof(float));
-  const Plan p = plan_of(a);
-  return p.splits > 1 ? rows * p.splits * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float)) : 0;
+  const int64_t shares = shares_of(a), units = over(a->rows_q * (a->heads_q / a->heads_kv), kRowsWave) * a->batch;
+  return shares > 0 ? (shares + units) * a->heads_kv * unit_rows(a) * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float)) : 0;
 }
 
 extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* k, const void* v, void* out, float* lse,
@@ -1055,24 +1186,23 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.o = out;
   r.lse = lse;
   const int64_t rows = a->rows_q * r.g;
-  const Plan plan = plan_of(a);
-  if (plan.splits == 0) {
+  r.shares = static_cast<int>(shares_of(a));
+  if (r.shares == 0) {
     r.tiles = static_cast<int>(over(rows, kRowsGroup));
     const int64_t groups = places_of(a, rows, kRowsGroup) * r.hkv;
     if (!fits_launch(groups)) return FEWBIT_E_INVALID;
     return launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_fwd_kernel, r, groups, st));
   }
   r.tiles = static_cast<int>(over(rows, kRowsWave));
-  r.chunk = static_cast<int>(plan.chunk);
-  r.splits = static_cast<int>(plan.splits);
-  if (r.splits > 1) {
-    r.part_o = static_cast<float*>(workspace);
-    r.part_lse = r.part_o + a->batch * a->rows_q * r.hq * plan.splits * r.d;
-  }
-  const int64_t groups = places_of(a, rows, kRowsWave) * r.hkv * plan.splits, joins = over(a->batch * a->rows_q * r.hq, kWaves);
+  const int64_t units = r.tiles * a->batch;
+  r.part_o = static_cast<float*>(workspace);
+  r.unit_rows = static_cast<int>(unit_rows(a));
+  r.part_lse = r.part_o + (r.shares + units) * r.hkv * r.unit_rows * r.d;
+  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = over(units * r.hkv * r.unit_rows, kWaves);
   if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
-  rc = launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_split_kernel, r, groups, st));
-  if (rc != FEWBIT_OK || r.splits == 1) return rc;
+  rc = launch_status("fewbit_attn_fwd", r.tiles == 1 ? start_split<true>(r, bf16, static_cast<unsigned>(groups), st)
+                                                     : start_split<false>(r, bf16, static_cast<unsigned>(groups), st));
+  if (rc != FEWBIT_OK || all_whole(a, r.shares)) return rc;
   return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_join_kernel<FEWBIT_BF16> : attn_join_kernel<FEWBIT_F16>,
                                                  dim3(static_cast<unsigned>(joins)), kThreads, st, r));
 }
