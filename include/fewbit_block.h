@@ -111,7 +111,8 @@ int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const void* q, const
  * head_dim]; the gradients of the weights are fp32.
  *
  * Everything is computed in fp32 and rounded once.  The weights' gradients
- * are summed in an order that depends on the sizes alone.
+ * are summed in an order that depends on the sizes alone.  batch * tokens *
+ * (heads + 1) stays below 2^31.
  */
 typedef struct fewbit_qk {
     int32_t dtype;                /* storage type of q, k and their weights    */
@@ -192,7 +193,7 @@ typedef struct fewbit_adamw {
 
 /* m, v: fp32 or 8-bit codes; m_scale, v_scale: one float per block with
  * 8-bit moments, else not used; master: fp32 or NULL.  `tensors` is a host
- * array, read before the call returns.  Takes one launch per 96 tensors; if
+ * array, read before the call returns.  Takes one launch per 256 tensors; if
  * one fails the earlier ones are done. */
 int fewbit_adamw_step(const fewbit_adamw* a, const fewbit_adamw_tensor* tensors, int32_t count,
                       void* m, void* v, float* m_scale, float* v_scale, float* master,

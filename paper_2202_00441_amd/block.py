@@ -145,7 +145,7 @@ def adamw_blocks(n: int) -> int:
 
 def adamw_step(params, grads, exp_avg, exp_avg_sq, exp_avg_scale=None, exp_avg_sq_scale=None, master=None, *,
                lr, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01, step, seed=None):
-    """One AdamW step over all tensors, in place, one launch for 96 of them.
+    """One AdamW step over all tensors, in place, one launch for 256 of them.
 
     params: tensors of one type (fp32, fp16 or bf16); grads: of that type or
     fp32, in the parameters' layout (None: that tensor is left as it is).

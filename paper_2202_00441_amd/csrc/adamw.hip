@@ -4,11 +4,11 @@
 // HBM: per element it reads and writes a parameter and two moments and reads a
 // gradient (bf16 with 8-bit moments: 10 bytes; fp32 with 32-bit ones: 28).
 //
-// A workgroup takes a run of 256-element blocks of one tensor, found in the list
-// that travels as kernel arguments; its waves take blocks in turn.  With 8-bit
-// moments 32 lanes hold a block, eight elements each (8 bytes of codes, 16 of a
-// 16-bit parameter), and find the block's largest magnitudes by cross-lane
-// steps; with 32-bit ones 64 lanes hold it, four elements each (16 bytes).
+// A workgroup takes 16 blocks of 256 elements of one tensor, found in the list that
+// travels as kernel arguments, and ends: the dispatcher balances the compute units.
+// With 8-bit moments 32 lanes hold a block, eight elements each (8 bytes of codes, 16 of
+// a 16-bit parameter), and find the block's largest magnitudes by cross-lane steps;
+// with 32-bit ones 64 lanes hold it, four elements each (16 bytes).
 //
 // Roundings.  Moments, root and update are fp32; sums of products are not fused,
 // so that the two moments are the same on every implementation of the formulas,
@@ -23,8 +23,10 @@ namespace {
 using namespace block;
 
 constexpr int kBlock = FEWBIT_ADAMW_BLOCK;
-constexpr int kThreads = 256;
-constexpr int kMaxTensors = 96;     // of one launch: their list is 3 KB of arguments
+constexpr int kThreads = 512;
+constexpr int kMaxTensors = 256;    // of one launch: their list is 9 KB of arguments
+constexpr int kRun = 16;            // blocks of a workgroup
+constexpr int kLoad = kNt, kStore = kNt;
 
 struct Tensor {
   void* p;
@@ -37,7 +39,6 @@ struct Args {
   Tensor t[kMaxTensors];
   uint32_t first[kMaxTensors];      // its first workgroup
   int count;
-  int run;              // blocks of a workgroup
   void *m, *v;
   float *ms, *vs, *master;
   float b1, a1, b2, a2;             // betas and 1 - beta
@@ -47,12 +48,19 @@ struct Args {
 
 // The update of N elements; codes and scales apart.
 template <int N>
-__device__ __forceinline__ void update(const Args& a, float (&w)[N], const float (&g)[N], float (&m)[N], float (&v)[N]) {
+__device__ __forceinline__ void moments(const Args& a, const float (&g)[N], float (&m)[N], float (&v)[N]) {
 #pragma clang fp contract(off)
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     m[i] = m[i] * a.b1 + g[i] * a.a1;
     v[i] = v[i] * a.b2 + (g[i] * g[i]) * a.a2;
+  }
+}
+template <int N>
+__device__ __forceinline__ void update(const Args& a, float (&w)[N], const float (&g)[N], float (&m)[N], float (&v)[N]) {
+  moments(a, g, m, v);
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
     const float d = __builtin_amdgcn_sqrtf(v[i]) * a.root + a.eps;
     w[i] = w[i] * a.keep - a.step * (m[i] * __builtin_amdgcn_rcpf(d));
   }
@@ -81,12 +89,15 @@ __device__ __forceinline__ uint32_t scale_field(float most) {
 }
 __device__ __forceinline__ float power(uint32_t field) { return __builtin_bit_cast(float, field << 23); }
 
-// y >= 0 (at most 448, or not finite) rounded to one of the two 8-bit numbers
-// around it, up with probability of its distance from the lower: u in [0, 1).
-// y is counted in steps of its binade (in steps of 2^-9 below 2^-6).
-__device__ __forceinline__ float dithered(float y, float u) {
-  const uint32_t e = max(__builtin_bit_cast(uint32_t, y) >> 23, 121u);
-  return floorf(y * power(257 - e) + u) * power(e - 3);
+// y >= 0 (at most 448, or not finite) rounded to one of the two 8-bit numbers around it,
+// up with the probability of its distance from the lower: u / 2^16 of that or more is
+// taken up.  The format keeps three bits of 23 behind the leading one; adding u to the
+// 16 bits below them carries into them as it should.  Below 2^-6 its numbers are 2^-9
+// apart, as those of the binade from 2^-6 on are: there y takes the detour through that.
+__device__ __forceinline__ float dithered(float y, uint32_t u) {
+  const float detour = y < 0x1p-6f ? 0x1p-6f : 0.0f;
+  const uint32_t bits = __builtin_bit_cast(uint32_t, y + detour) + (u << 4);
+  return __builtin_bit_cast(float, bits & 0xfff00000u) - detour;
 }
 
 __device__ __forceinline__ uint32_t pack4(float a, float b, float c, float d) {
@@ -106,85 +117,170 @@ __device__ __forceinline__ void unpack(const uint32_t (&c)[N / 4], float scale, 
   }
 }
 
-// N elements from p on, of which `left` are there; the others read as 0 and are
-// not written.  `whole`: all of them are, and p is aligned.
+// N elements from byte `at` on, of which `left` are there; the others read as 0 and are
+// not written.  `whole`: all of them are, and the address is aligned.
 template <class T, int N>
-__device__ __forceinline__ void load_some(const T* p, int64_t left, bool whole, float (&x)[N]) {
-  if (whole) return load(p, x);
+__device__ __forceinline__ void load_some(const Stream& s, const T* base, uint32_t at, int64_t left, bool whole, float (&x)[N]) {
+  if (whole) return s.load<T, kLoad>(at, x);
+  const T* p = reinterpret_cast<const T*>(reinterpret_cast<const char*>(base) + at);
 #pragma unroll
   for (int i = 0; i < N; ++i) x[i] = i < left ? static_cast<float>(p[i]) : 0.0f;
 }
 template <class T, int N>
-__device__ __forceinline__ void store_some(T* p, int64_t left, bool whole, const float (&x)[N]) {
-  if (whole) return store(p, x);
+__device__ __forceinline__ void store_some(const Stream& s, T* base, uint32_t at, int64_t left, bool whole, const float (&x)[N]) {
+  if (whole) return s.store<T, kStore>(at, x);
+  T* p = reinterpret_cast<T*>(reinterpret_cast<char*>(base) + at);
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (i < left) p[i] = static_cast<T>(x[i]);
+}
+
+// The moments of N elements, as codes of a block that 32 lanes hold; the second four of
+// a lane's elements lie `apart` elements behind its first.
+template <int N>
+__device__ __forceinline__ void encode(const Args& a, int64_t flat, int apart, const float (&m)[N], const float (&v)[N], uint32_t (&cm)[N / 4],
+                                       uint32_t (&cv)[N / 4], float& ms, float& vs) {
+  const uint32_t fm = scale_field(largest(m)), fv = scale_field(largest(v));
+  const float im = power(254 - fm), iv = power(254 - fv);
+  float rm[N], rv[N];
+  const uint32_t first = static_cast<uint32_t>(flat) * 0x9E3779B1u + a.key;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const uint32_t x = first + static_cast<uint32_t>(i / 4 * apart + i % 4) * 0x9E3779B1u;
+    uint32_t h = (x ^ x >> 15) * 0xBB67AE85u;
+    h ^= h >> 13;
+    rm[i] = copysignf(dithered(fabsf(m[i]) * im, h >> 16), m[i]);
+    rv[i] = dithered(v[i] * iv, h & 0xffff);
+    if (v[i] > 0.0f) rv[i] = fmaxf(rv[i], 0x1p-9f);
+  }
+#pragma unroll
+  for (int j = 0; j < N / 4; ++j) {
+    cm[j] = pack4(rm[4 * j], rm[4 * j + 1], rm[4 * j + 2], rm[4 * j + 3]);
+    cv[j] = pack4(rv[4 * j], rv[4 * j + 1], rv[4 * j + 2], rv[4 * j + 3]);
+  }
+  ms = power(fm);
+  vs = power(fv);
 }
 
 template <int PT, int GT, int BITS, bool MASTER>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
   using P = typename Store<PT>::type;
   using G = typename Store<GT>::type;
-  constexpr int N = BITS == 8 ? 8 : 4;              // elements of a lane
+  constexpr int N = BITS == 8 ? 8 : 4;              // elements of a lane in a row
   constexpr int kLanes = kBlock / N;                // lanes of a block
-  constexpr int kStep = kThreads / kLanes;          // blocks of a workgroup's pass
 
   // the tensor: the last whose first workgroup is not past this one
-  int lo = 0, hi = a.count;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) / 2;
-    (a.first[mid] <= blockIdx.x ? lo : hi) = mid;
-  }
-  const Tensor t = a.t[lo];
-  const int64_t start = static_cast<int64_t>(blockIdx.x - a.first[lo]) * a.run;     // in the tensor's blocks
-  const bool aligned = ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(t.g)) & 15) == 0;
-  const int lane = threadIdx.x % kLanes;
-  for (int64_t b = start + threadIdx.x / kLanes, end = start + a.run; b < end; b += kStep) {
-    const int64_t at = b * kBlock + lane * N, left = t.n - at;
-    if (b * kBlock >= t.n) break;                   // of all lanes of the block alike
-    const bool whole = aligned && left >= N;
-    const int64_t flat = (t.block0 + b) * kBlock + lane * N;
-    float w[N], g[N], m[N], v[N];
-    load_some(static_cast<const G*>(t.g) + at, left, whole, g);
-    if constexpr (MASTER)
-      load(a.master + flat, w);
-    else
-      load_some(static_cast<const P*>(t.p) + at, left, whole, w);
-    if constexpr (BITS == 32) {
-      load(static_cast<const float*>(a.m) + flat, m);
-      load(static_cast<const float*>(a.v) + flat, v);
-      update(a, w, g, m, v);
-      store(static_cast<float*>(a.m) + flat, m);
-      store(static_cast<float*>(a.v) + flat, v);
-    } else {
-      u32x2* cm = reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.m) + flat);
-      u32x2* cv = reinterpret_cast<u32x2*>(static_cast<uint8_t*>(a.v) + flat);
-      const u32x2 qm = *cm, qv = *cv;
-      unpack<N>({qm[0], qm[1]}, a.ms[t.block0 + b], m);
-      unpack<N>({qv[0], qv[1]}, a.vs[t.block0 + b], v);
-      update(a, w, g, m, v);
-      const uint32_t fm = scale_field(largest(m)), fv = scale_field(largest(v));
-      const float im = power(254 - fm), iv = power(254 - fv);
-      float rm[N], rv[N];
-      uint32_t x = static_cast<uint32_t>(flat) * 0x9E3779B1u + a.key;
+  const int l = threadIdx.x % kWave;
+  int before = 0;
 #pragma unroll
-      for (int i = 0; i < N; ++i, x += 0x9E3779B1u) {
-        uint32_t h = (x ^ x >> 15) * 0xBB67AE85u;
-        h ^= h >> 13;
-        rm[i] = copysignf(dithered(fabsf(m[i]) * im, static_cast<float>(h >> 16) * 0x1p-16f), m[i]);
-        rv[i] = dithered(v[i] * iv, static_cast<float>(h & 0xffff) * 0x1p-16f);
-        if (v[i] > 0.0f) rv[i] = fmaxf(rv[i], 0x1p-9f);
-      }
-      *cm = u32x2{pack4(rm[0], rm[1], rm[2], rm[3]), pack4(rm[4], rm[5], rm[6], rm[7])};
-      *cv = u32x2{pack4(rv[0], rv[1], rv[2], rv[3]), pack4(rv[4], rv[5], rv[6], rv[7])};
-      if (lane == 0) {
-        a.ms[t.block0 + b] = power(fm);
-        a.vs[t.block0 + b] = power(fv);
+  for (int i = 0; i < kMaxTensors; i += kWave) {
+    const uint32_t first = a.first[i + l];
+    before += __builtin_popcountll(__ballot(i + l < a.count && first <= blockIdx.x));
+  }
+  const Tensor t = a.t[__builtin_amdgcn_readfirstlane(before - 1)];
+  const int64_t block = static_cast<int64_t>(blockIdx.x - a.first[__builtin_amdgcn_readfirstlane(before - 1)]) * kRun;   // the first, of the tensor's
+  const bool aligned = ((reinterpret_cast<uintptr_t>(t.p) | reinterpret_cast<uintptr_t>(t.g)) & 15) == 0;
+  P* p = static_cast<P*>(t.p) + block * kBlock;
+  const G* g = static_cast<const G*>(t.g) + block * kBlock;
+  const int64_t flat = (t.block0 + block) * kBlock, left = t.n - block * kBlock;
+  constexpr uint32_t kAll = kRun * kBlock;
+  const Stream sp(p, kAll * sizeof(P)), sg(g, kAll * sizeof(G)), sw(a.master + flat, kAll * 4);
+  if constexpr (BITS == 32) {
+    // every lane has four elements in each of its wave's two blocks
+    const Stream sm(static_cast<float*>(a.m) + flat, kAll * 4), sv(static_cast<float*>(a.v) + flat, kAll * 4);
+    constexpr int kRows = kRun * kLanes / kThreads;
+    float w[kRows][N], gr[kRows][N], m[kRows][N], v[kRows][N];
+    uint32_t at[kRows];
+    bool whole[kRows], some[kRows];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      at[r] = ((threadIdx.x / kWave * kRows + r) * kWave + l) * N;
+      whole[r] = aligned && left - at[r] >= N;
+      some[r] = at[r] / kBlock * kBlock < left;       // of all lanes of the block alike
+      if (!some[r]) continue;
+      load_some(sg, g, at[r] * sizeof(G), left - at[r], whole[r], gr[r]);
+      sm.load<float, kLoad>(at[r] * 4, m[r]);
+      sv.load<float, kLoad>(at[r] * 4, v[r]);
+      if constexpr (MASTER)
+        sw.load<float, kLoad>(at[r] * 4, w[r]);
+      else
+        load_some<P>(sp, p, at[r] * sizeof(P), left - at[r], whole[r], w[r]);
+    }
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      if (!some[r]) continue;
+      update(a, w[r], gr[r], m[r], v[r]);
+      sm.store<float, kStore>(at[r] * 4, m[r]);
+      sv.store<float, kStore>(at[r] * 4, v[r]);
+      if constexpr (MASTER) sw.store<float, kStore>(at[r] * 4, w[r]);
+      store_some(sp, p, at[r] * sizeof(P), left - at[r], whole[r], w[r]);
+    }
+  } else {
+    // A lane's eight elements lie side by side where that is 16 bytes of everything;
+    // with a stream of fp32 in two rows of four, each of which 32 lanes fill.
+    constexpr int kApart = PT != FEWBIT_F32 && GT != FEWBIT_F32 && !MASTER ? 4 : kBlock / 2;
+    constexpr int kRow = kApart == 4 ? N : 4, kRows = N / kRow;
+    const uint32_t at = threadIdx.x / kLanes * kBlock + threadIdx.x % kLanes * kRow;
+    if (at / kBlock * kBlock >= left) return;         // all lanes of the block alike
+    const Stream sm(static_cast<uint8_t*>(a.m) + flat, kAll), sv(static_cast<uint8_t*>(a.v) + flat, kAll);
+    const int64_t b = t.block0 + block + at / kBlock;
+    float w[kRows][kRow], gr[N], m[N], v[N], wf[N];
+    uint32_t qm[N / 4], qv[N / 4];
+    bool whole[kRows];
+    if constexpr (kRows == 1) {
+      const u32x2 x = sm.get<kLoad, 8>(at), y = sv.get<kLoad, 8>(at);
+      qm[0] = x[0], qm[1] = x[1], qv[0] = y[0], qv[1] = y[1];
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        qm[r] = sm.get<kLoad, 4>(at + r * kApart);
+        qv[r] = sv.get<kLoad, 4>(at + r * kApart);
       }
     }
-    if constexpr (MASTER) store(a.master + flat, w);
-    store_some(static_cast<P*>(t.p) + at, left, whole, w);
+    const float oldm = a.ms[b], oldv = a.vs[b];
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const uint32_t here = at + r * kApart;
+      float x[kRow];
+      whole[r] = aligned && left - here >= kRow;
+      load_some(sg, g, here * sizeof(G), left - here, whole[r], x);
+      if constexpr (MASTER)
+        sw.load<float, kLoad>(here * 4, w[r]);
+      else
+        load_some<P>(sp, p, here * sizeof(P), left - here, whole[r], w[r]);
+#pragma unroll
+      for (int i = 0; i < kRow; ++i) {
+        gr[r * kRow + i] = x[i];
+        wf[r * kRow + i] = w[r][i];
+      }
+    }
+    unpack<N>(qm, oldm, m);
+    unpack<N>(qv, oldv, v);
+    update(a, wf, gr, m, v);
+#pragma unroll
+    for (int r = 0; r < kRows; ++r) {
+      const uint32_t here = at + r * kApart;
+#pragma unroll
+      for (int i = 0; i < kRow; ++i) w[r][i] = wf[r * kRow + i];
+      if constexpr (MASTER) sw.store<float, kStore>(here * 4, w[r]);
+      store_some(sp, p, here * sizeof(P), left - here, whole[r], w[r]);
+    }
+    float ms, vs;
+    encode(a, flat + at, kApart, m, v, qm, qv, ms, vs);
+    if constexpr (kRows == 1) {
+      sm.put<kStore>(at, u32x2{qm[0], qm[1]});
+      sv.put<kStore>(at, u32x2{qv[0], qv[1]});
+    } else {
+#pragma unroll
+      for (int r = 0; r < kRows; ++r) {
+        sm.put<kStore>(at + r * kApart, qm[r]);
+        sv.put<kStore>(at + r * kApart, qv[r]);
+      }
+    }
+    if (at % kBlock == 0) {
+      a.ms[b] = ms;
+      a.vs[b] = vs;
+    }
   }
 }
 
@@ -252,10 +348,6 @@ extern "C" int fewbit_adamw_step(const fewbit_adamw* h, const fewbit_adamw_tenso
   a.root = static_cast<float>(1.0 / std::sqrt(1.0 - std::pow(h->beta2, t)));
   a.eps = static_cast<float>(h->eps);
   a.key = static_cast<uint32_t>(h->seed) * 0x6A09E667u + 0x3C6EF372u;
-  // Blocks of a workgroup: enough for eight passes where that still gives the
-  // chip eight workgroups per CU, one pass at least.
-  const int64_t wanted = total / (8 * static_cast<int64_t>(device_cus()));
-  a.run = wanted >= 64 ? 64 : wanted >= 32 ? 32 : wanted >= 16 ? 16 : 8;
 
   int64_t block0 = 0;
   for (int i = 0; i < count;) {
@@ -267,7 +359,7 @@ extern "C" int fewbit_adamw_step(const fewbit_adamw* h, const fewbit_adamw_tenso
         block0 += blocks;
         continue;
       }
-      const uint64_t more = (blocks + a.run - 1) / a.run;
+      const uint64_t more = (blocks + kRun - 1) / kRun;
       if (groups + more >= uint64_t{1} << 24) {                      // fewer than 2^32 threads
         if (a.count == 0) return FEWBIT_E_INVALID;                   // more than any device's memory holds
         break;

@@ -51,17 +51,6 @@ struct Mma<FEWBIT_F16> {
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 
-// x / n for 0 <= x < 2^31: the high half of a product with 2^32 / n rounded up is at
-// most one too many.
-struct Divisor {
-  uint32_t n, inverse;
-  __device__ __forceinline__ int divide(int x) const {
-    if (n == 1) return x;
-    const uint32_t q = __umulhi(static_cast<uint32_t>(x), inverse);
-    return static_cast<int>(q * n > static_cast<uint32_t>(x) ? q - 1 : q);
-  }
-};
-
 struct Args {
   const void *q, *k, *v, *dout, *out;
   void *o, *dq, *dk, *dv;
@@ -1125,7 +1114,7 @@ Args args_of(const fewbit_attn* a) {
   r.causal = a->causal;
   r.window = a->window;
   r.scale = a->scale;
-  r.by_g = {static_cast<uint32_t>(r.g), static_cast<uint32_t>(((uint64_t{1} << 32) + r.g - 1) / r.g)};
+  r.by_g = divisor(r.g);
   return r;
 }
 

@@ -68,6 +68,62 @@ __device__ __forceinline__ void store(T* p, const float (&x)[N]) {
   }
 }
 
+// Streams: accesses relative to an address that is the same for the whole wave, through
+// buffer instructions, whose cache policy is explicit: 2 = nt (not kept in the caches),
+// 16 = sc1 (stores: written through the L2).
+constexpr int kNt = 2, kThrough = 16, kThroughNt = 18;
+
+struct Stream {
+  __amdgpu_buffer_rsrc_t r;
+  // 0x00020000: raw (unformatted) 32-bit buffer accesses on gfx9
+  __device__ __forceinline__ Stream(const void* base, uint32_t bytes)
+      : r(__builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(base), 0, static_cast<int>(bytes), 0x00020000)) {}
+
+  template <int P, int BYTES>
+  __device__ __forceinline__ auto get(uint32_t at) const {
+    if constexpr (BYTES == 16)
+      return __builtin_amdgcn_raw_buffer_load_b128(r, at, 0, P);
+    else if constexpr (BYTES == 8)
+      return __builtin_amdgcn_raw_buffer_load_b64(r, at, 0, P);
+    else
+      return __builtin_amdgcn_raw_buffer_load_b32(r, at, 0, P);
+  }
+  template <int P, class V>
+  __device__ __forceinline__ void put(uint32_t at, V v) const {
+    if constexpr (sizeof(V) == 16)
+      __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, v), r, at, 0, P);
+    else if constexpr (sizeof(V) == 8)
+      __builtin_amdgcn_raw_buffer_store_b64(__builtin_bit_cast(u32x2, v), r, at, 0, P);
+    else
+      __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, v), r, at, 0, P);
+  }
+
+  // N values of type T from byte `at` on, as fp32 and back
+  template <class T, int P, int N>
+  __device__ __forceinline__ void load(uint32_t at, float (&x)[N]) const {
+    constexpr int kPer = 16 / sizeof(T) < N ? 16 / sizeof(T) : N;
+    using V = typename Vec<T, kPer>::raw;
+#pragma unroll
+    for (int j = 0; j < N / kPer; ++j) {
+      const V v = __builtin_bit_cast(V, get<P, kPer * sizeof(T)>(at + j * kPer * sizeof(T)));
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) x[j * kPer + i] = static_cast<float>(v[i]);
+    }
+  }
+  template <class T, int P, int N>
+  __device__ __forceinline__ void store(uint32_t at, const float (&x)[N]) const {
+    constexpr int kPer = 16 / sizeof(T) < N ? 16 / sizeof(T) : N;
+    using V = typename Vec<T, kPer>::raw;
+#pragma unroll
+    for (int j = 0; j < N / kPer; ++j) {
+      V v;
+#pragma unroll
+      for (int i = 0; i < kPer; ++i) v[i] = static_cast<T>(x[j * kPer + i]);
+      put<P>(at + j * kPer * sizeof(T), v);
+    }
+  }
+};
+
 // ---------------------------------------------------------------- cross-lane steps
 template <int CTRL>
 __device__ __forceinline__ float dpp(float x) {
@@ -115,6 +171,19 @@ __device__ __forceinline__ float across(float x, F f) {
   }
   return x;
 }
+
+// x / n for 0 <= x < 2^31: the high half of a product with 2^32 / n rounded up is at
+// most one too many.
+struct Divisor {
+  uint32_t n, inverse;
+  __device__ __forceinline__ int divide(int x) const {
+    if (n == 1) return x;
+    const uint32_t q = __umulhi(static_cast<uint32_t>(x), inverse);
+    return static_cast<int>(q * n > static_cast<uint32_t>(x) ? q - 1 : q);
+  }
+};
+
+inline Divisor divisor(int n) { return {static_cast<uint32_t>(n), static_cast<uint32_t>(((uint64_t{1} << 32) + n - 1) / n)}; }
 
 // ---------------------------------------------------------------- host side
 inline bool misaligned(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) != 0; }

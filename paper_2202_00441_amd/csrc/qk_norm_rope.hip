@@ -5,12 +5,12 @@
 // element once; the backward reads the input and the incoming gradient and
 // writes the gradient, and recomputes the norm instead of keeping it.
 //
-// A row (one head of one token) is held by a group of 4, 8 or 16 lanes, 16
-// elements each: two 16-byte chunks that hold both elements of eight rotated
-// pairs, so that neither the rotation nor the tables' angles cross lanes, and
-// the row's sums take two to four cross-lane steps.  A group walks the heads of
-// one token (or a share of them): the token's angles are read once and stay in
-// registers.
+// A row (one head of one token) is held by a group of 4, 8 or 16 lanes, 16 elements
+// each: two 16-byte chunks that hold both elements of eight rotated pairs, so that
+// neither the rotation nor the tables' angles cross lanes, and the row's sums take two
+// to four cross-lane steps.  A group takes several heads of one token at once: the
+// token's angles are read once, and the rows are all on their way before the first is
+// worked on.
 //
 // Backward: with g the incoming gradient turned back, x the input, r = 1 /
 // sqrt(mean(x^2) + eps) and u = x r,
@@ -36,6 +36,8 @@ struct Side {
   void* y;              // forward: output; backward: gradient
   int64_t xs[3], ds[3];
   int heads;
+  Divisor shares;       // groups of a token
+  uint32_t units;       // groups of all tokens
 };
 
 struct Args {
@@ -43,12 +45,10 @@ struct Args {
   const float *cos, *sin;
   const int64_t* pos;
   int64_t ps[2];
-  int64_t tokens_all;   // batch * tokens
   int64_t table_rows;
-  uint32_t tokens;
+  Divisor tokens;
   int d, rot;
-  int share;            // heads of a group's walk
-  int shares;           // groups of a token
+  uint32_t first_k;     // forward: the first workgroup of the keys
   float eps;
   float* parts;         // backward: [workgroups][2][head_dim]
 };
@@ -80,6 +80,25 @@ __device__ __forceinline__ void turn(float (&x)[kN], const float (&c)[8], const 
   }
 }
 
+// A lane's part of a row as it lies in memory, and as fp32.
+template <class T>
+struct Raw {
+  static constexpr int kVecs = 8 * sizeof(T) / 16;      // 16-byte accesses of a chunk
+  typedef T V __attribute__((ext_vector_type(16 / sizeof(T))));
+  V v[2 * kVecs];
+
+  __device__ __forceinline__ void load(const T* row, const Chunks& at) {
+#pragma unroll
+    for (int j = 0; j < kVecs; ++j) {
+      v[j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(row + at.a) + j);
+      v[kVecs + j] = __builtin_nontemporal_load(reinterpret_cast<const V*>(row + at.b) + j);
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[kN]) const {
+#pragma unroll
+    for (int i = 0; i < kN; ++i) x[i] = static_cast<float>(v[i / (8 / kVecs)][i % (8 / kVecs)]);
+  }
+};
 template <class T>
 __device__ __forceinline__ void load_row(const T* row, const Chunks& at, float (&x)[kN]) {
   float a[8], b[8];
@@ -127,36 +146,38 @@ __device__ __forceinline__ void angles(const Args& a, int lane, bool turned, int
   }
 }
 
-// LEVELS: a group has 2^LEVELS lanes.
-template <int DT, bool INTER, int LEVELS>
+// LEVELS: a group has 2^LEVELS lanes.  HEADS: rows of a group.
+template <int DT, bool INTER, int LEVELS, int HEADS>
 __global__ __launch_bounds__(kThreads) void qk_fwd_kernel(const Args a) {
   using T = typename Store<DT>::type;
   constexpr int kLanes = 1 << LEVELS;
-  const int64_t unit = static_cast<int64_t>(blockIdx.x) * (kThreads / kLanes) + threadIdx.x / kLanes;
-  const int64_t token = unit / a.shares;
-  if (token >= a.tokens_all) return;
-  const int lane = threadIdx.x % kLanes, share = static_cast<int>(unit - token * a.shares);
+  const bool keys = blockIdx.x >= a.first_k;
+  const Side& side = a.s[keys];
+  const uint32_t place = (blockIdx.x - (keys ? a.first_k : 0)) * (kThreads / kLanes) + threadIdx.x / kLanes;
+  if (place >= side.units) return;
+  const int unit = static_cast<int>(place), token = side.shares.divide(unit), first = (unit - token * static_cast<int>(side.shares.n)) * HEADS;
+  const int lane = threadIdx.x % kLanes, b = a.tokens.divide(token), t = token - b * static_cast<int>(a.tokens.n);
   const Chunks at = chunks_of<INTER>(lane, a.d, a.rot);
-  const int64_t b = token / a.tokens, t = token - b * a.tokens;
-  float c[8], s[8];
-  angles(a, lane, at.turned, b, t, c, s);
-  const int last = min((share + 1) * a.share, a.s[0].heads + a.s[1].heads);
-  for (int head = share * a.share; head < last; ++head) {
-    const Side& side = a.s[head >= a.s[0].heads];
-    const int h = head >= a.s[0].heads ? head - a.s[0].heads : head;
-    float x[kN] = {}, w[kN] = {};
-    if (at.some) {
-      load_row(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at, x);
-      load_row(static_cast<const T*>(side.w), at, w);
-    }
-    float sum = 0.0f;
+  const T* x = static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1];
+  Raw<T> raw[HEADS] = {};
 #pragma unroll
-    for (int i = 0; i < kN; ++i) sum += x[i] * x[i];
+  for (int j = 0; j < HEADS; ++j)
+    if (at.some && first + j < side.heads) raw[j].load(x + (first + j) * side.xs[2], at);
+  float w[kN] = {}, c[8], s[8];
+  if (at.some) load_row(static_cast<const T*>(side.w), at, w);
+  angles(a, lane, at.turned, b, t, c, s);
+  T* y = static_cast<T*>(side.y) + (static_cast<int64_t>(token) * side.heads + first) * a.d;
+#pragma unroll
+  for (int j = 0; j < HEADS; ++j) {
+    float u[kN], sum = 0.0f;
+    raw[j].get(u);
+#pragma unroll
+    for (int i = 0; i < kN; ++i) sum += u[i] * u[i];
     const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) x[i] = x[i] * r * w[i];
-    if (at.turned) turn<INTER>(x, c, s);
-    if (at.some) store_row(static_cast<T*>(side.y) + (token * side.heads + h) * a.d, at, x);
+    for (int i = 0; i < kN; ++i) u[i] = u[i] * r * w[i];
+    if (at.turned) turn<INTER>(u, c, s);
+    if (at.some && first + j < side.heads) store_row(y + j * a.d, at, u);
   }
 }
 
@@ -167,55 +188,47 @@ __global__ __launch_bounds__(kThreads) void qk_bwd_kernel(const Args a) {
   __shared__ float sums[kGroups][kLanes * kN];
   const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
   const Chunks at = chunks_of<INTER>(lane, a.d, a.rot);
-  const int64_t units = a.tokens_all * a.shares, step = static_cast<int64_t>(gridDim.x) * kGroups;
-  float dw[2][kN] = {};
-  for (int64_t unit = static_cast<int64_t>(blockIdx.x) * kGroups + group; unit < units; unit += step) {
-    const int64_t token = unit / a.shares;
-    const int share = static_cast<int>(unit - token * a.shares);
-    const int64_t b = token / a.tokens, t = token - b * a.tokens;
-    float c[8], s[8];
-    angles(a, lane, at.turned, b, t, c, s);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) s[j] = -s[j];
-#pragma unroll
-    for (int kind = 0; kind < 2; ++kind) {
-      const Side& side = a.s[kind];
-      const int first = max(share * a.share - (kind ? a.s[0].heads : 0), 0);
-      const int last = min((share + 1) * a.share - (kind ? a.s[0].heads : 0), side.heads);
-      if (first >= last) continue;
-      float w[kN] = {};
-      if (at.some) load_row(static_cast<const T*>(side.w), at, w);
-      for (int h = first; h < last; ++h) {
-        float x[kN] = {}, g[kN] = {};
-        if (at.some) {
-          load_row(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at, x);
-          load_row(static_cast<const T*>(side.dy) + b * side.ds[0] + t * side.ds[1] + h * side.ds[2], at, g);
-        }
-        if (at.turned) turn<INTER>(g, c, s);
-        float sum = 0.0f, dot = 0.0f;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          sum += x[i] * x[i];
-          dot += g[i] * w[i] * x[i];
-        }
-        const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
-        const float mean = row_sum<LEVELS>(dot) * r / a.d;
-#pragma unroll
-        for (int i = 0; i < kN; ++i) {
-          const float u = x[i] * r;
-          dw[kind][i] += g[i] * u;
-          x[i] = r * (g[i] * w[i] - u * mean);
-        }
-        if (at.some) store_row(static_cast<T*>(side.y) + (token * side.heads + h) * a.d, at, x);
-      }
-    }
-  }
-  // the workgroup's sums: groups in pairs, then the next pairs
-#pragma unroll
+#pragma unroll 1
   for (int kind = 0; kind < 2; ++kind) {
+    const Side& side = a.s[kind];
+    float w[kN] = {}, dw[kN] = {};
+    if (at.some && side.units > 0) load_row(static_cast<const T*>(side.w), at, w);
+    for (uint32_t place = blockIdx.x * kGroups + group; place < side.units; place += gridDim.x * kGroups) {
+      const int unit = static_cast<int>(place), token = side.shares.divide(unit), h = unit - token * static_cast<int>(side.shares.n);
+      const int b = a.tokens.divide(token), t = token - b * static_cast<int>(a.tokens.n);
+      Raw<T> rx = {}, rg = {};
+      if (at.some) {
+        rx.load(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at);
+        rg.load(static_cast<const T*>(side.dy) + b * side.ds[0] + t * side.ds[1] + h * side.ds[2], at);
+      }
+      float c[8], s[8];
+      angles(a, lane, at.turned, b, t, c, s);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s[j] = -s[j];
+      float u[kN], g[kN];
+      rx.get(u);
+      rg.get(g);
+      if (at.turned) turn<INTER>(g, c, s);
+      float sum = 0.0f, dot = 0.0f;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        sum += u[i] * u[i];
+        dot += g[i] * w[i] * u[i];
+      }
+      const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
+      const float mean = row_sum<LEVELS>(dot) * r / a.d;
+#pragma unroll
+      for (int i = 0; i < kN; ++i) {
+        const float v = u[i] * r;
+        dw[i] += g[i] * v;
+        u[i] = r * (g[i] * w[i] - v * mean);
+      }
+      if (at.some) store_row(static_cast<T*>(side.y) + static_cast<int64_t>(unit) * a.d, at, u);
+    }
+    // the workgroup's sums: groups in pairs, then the next pairs
     if (kind) __syncthreads();
 #pragma unroll
-    for (int i = 0; i < kN; ++i) sums[group][i * kLanes + lane] = dw[kind][i];
+    for (int i = 0; i < kN; ++i) sums[group][i * kLanes + lane] = dw[i];
     for (int n = kGroups / 2; n > 0; n /= 2) {
       __syncthreads();
       for (int e = threadIdx.x; e < n * kLanes * kN; e += kThreads) {
@@ -262,7 +275,9 @@ int check(const fewbit_qk* a) {
   if (!(a->eps >= 0.0f && std::isfinite(a->eps))) return FEWBIT_E_INVALID;
   if (a->heads_q > 1 << 16 || a->heads_k > 1 << 16) return FEWBIT_E_INVALID;
   if (a->tokens >= int64_t{1} << 31 || a->batch >= int64_t{1} << 31) return FEWBIT_E_INVALID;
-  if (a->tokens > 0 && a->batch > (int64_t{1} << 34) / a->tokens) return FEWBIT_E_INVALID;
+  // rows are counted in 31 bits
+  if (a->tokens > 0 && a->batch > 0 && (std::max(a->heads_q, a->heads_k) + 1) * a->tokens >= (int64_t{1} << 31) / a->batch)
+    return FEWBIT_E_INVALID;
   return FEWBIT_OK;
 }
 
@@ -276,17 +291,23 @@ bool strides_fit(const fewbit_qk* a, const int64_t (&s)[3]) {
 
 int levels_of(int d) { return d <= 64 ? 2 : d <= 128 ? 3 : 4; }
 
-// Heads of a group's walk: all of a token's where that fills the chip (16 waves
-// per CU), fewer where there are few tokens.
-int share_of(const fewbit_qk* a) {
-  const int heads = a->heads_q + a->heads_k;
-  const int64_t groups = static_cast<int64_t>(device_cus()) * 16 * (kWave >> levels_of(a->head_dim));
-  const int64_t all = a->batch * a->tokens;
-  const int64_t shares = all >= groups ? 1 : (groups + all - 1) / all;
-  return shares >= heads ? 1 : static_cast<int>((heads + shares - 1) / shares);
+// Rows of a group of the forward: two where that leaves eight waves per CU, else one.
+// (32768 tokens of 20 heads in bf16: 63.7 us with two, 63.9 with four, 70.5 with one; 4096
+// tokens of 24 heads of 64: 9.0, 8.9 and 8.4.)  The backward's groups take one, and are
+// many (97 us; with two 107).
+constexpr int kHeads = 2;
+int heads_of(const fewbit_qk* a) {
+  const int64_t groups = a->batch * a->tokens * ((a->heads_q + kHeads - 1) / kHeads + (a->heads_k + kHeads - 1) / kHeads);
+  return groups >= static_cast<int64_t>(device_cus()) * 8 * (kWave >> levels_of(a->head_dim)) ? kHeads : 1;
 }
 
-Args args_of(const fewbit_qk* a, const float* cos, const float* sin, const int64_t* pos) {
+// Workgroups for so many groups of lanes.
+int64_t groups_of(const fewbit_qk* a, int64_t units) {
+  const int64_t per = kThreads >> levels_of(a->head_dim);
+  return (units + per - 1) / per;
+}
+
+Args args_of(const fewbit_qk* a, const float* cos, const float* sin, const int64_t* pos, bool back) {
   Args r{};
   for (int i = 0; i < 3; ++i) {
     r.s[0].xs[i] = a->q_stride[i];
@@ -301,40 +322,40 @@ Args args_of(const fewbit_qk* a, const float* cos, const float* sin, const int64
   r.pos = pos;
   r.ps[0] = a->position_stride[0];
   r.ps[1] = a->position_stride[1];
-  r.tokens_all = a->batch * a->tokens;
   r.table_rows = a->table_rows;
-  r.tokens = static_cast<uint32_t>(a->tokens);
+  r.tokens = divisor(static_cast<int>(a->tokens));
   r.d = a->head_dim;
   r.rot = a->rot;
-  r.share = share_of(a);
-  r.shares = (a->heads_q + a->heads_k + r.share - 1) / r.share;
   r.eps = a->eps;
+  const int heads = back ? 1 : heads_of(a);
+  for (Side& side : r.s) {
+    const int shares = (side.heads + heads - 1) / heads;
+    side.shares = divisor(std::max(shares, 1));
+    side.units = static_cast<uint32_t>(a->batch * a->tokens * shares);
+  }
+  r.first_k = static_cast<uint32_t>(groups_of(a, r.s[0].units));
   return r;
-}
-
-int64_t groups_of(const fewbit_qk* a, const Args& r) {
-  const int64_t per = kThreads >> levels_of(a->head_dim);
-  return (r.tokens_all * r.shares + per - 1) / per;
 }
 
 // Workgroups of the backward: what the chip holds at once, four per CU (each
 // leaves a row for the second kernel).
 int64_t parts_of(const fewbit_qk* a, const Args& r) {
   const int64_t most = std::min<int64_t>(kParts, 4 * static_cast<int64_t>(device_cus()));
-  return std::min(groups_of(a, r), most);
+  return std::min(groups_of(a, std::max(r.s[0].units, r.s[1].units)), most);
 }
 
 template <int DT, bool INTER, int LEVELS>
-hipError_t start_at(const Args& r, bool back, unsigned groups, hipStream_t s) {
-  return back ? launch(qk_bwd_kernel<DT, INTER, LEVELS>, dim3(groups), kThreads, s, r)
-              : launch(qk_fwd_kernel<DT, INTER, LEVELS>, dim3(groups), kThreads, s, r);
+hipError_t start_at(const fewbit_qk* a, const Args& r, bool back, unsigned groups, hipStream_t s) {
+  const bool several = heads_of(a) == kHeads;
+  auto fwd = several ? qk_fwd_kernel<DT, INTER, LEVELS, kHeads> : qk_fwd_kernel<DT, INTER, LEVELS, 1>;
+  return launch(back ? qk_bwd_kernel<DT, INTER, LEVELS> : fwd, dim3(groups), kThreads, s, r);
 }
 template <int DT, bool INTER>
 hipError_t start_inter(const fewbit_qk* a, const Args& r, bool back, unsigned groups, hipStream_t s) {
   switch (levels_of(a->head_dim)) {
-    case 2: return start_at<DT, INTER, 2>(r, back, groups, s);
-    case 3: return start_at<DT, INTER, 3>(r, back, groups, s);
-    default: return start_at<DT, INTER, 4>(r, back, groups, s);
+    case 2: return start_at<DT, INTER, 2>(a, r, back, groups, s);
+    case 3: return start_at<DT, INTER, 3>(a, r, back, groups, s);
+    default: return start_at<DT, INTER, 4>(a, r, back, groups, s);
   }
 }
 template <int DT>
@@ -374,14 +395,14 @@ extern "C" int fewbit_qk_fwd(const fewbit_qk* a, const void* q, const void* k, c
   if (misaligned(q_out) || misaligned(k_out)) return FEWBIT_E_ALIGN;
   rc = check_stream_device(static_cast<hipStream_t>(stream));
   if (rc != FEWBIT_OK) return rc;
-  Args r = args_of(a, cos, sin, positions);
+  Args r = args_of(a, cos, sin, positions, false);
   r.s[0].x = q;
   r.s[1].x = k;
   r.s[0].w = q_weight;
   r.s[1].w = k_weight;
   r.s[0].y = q_out;
   r.s[1].y = k_out;
-  const int64_t groups = groups_of(a, r);
+  const int64_t groups = r.first_k + groups_of(a, r.s[1].units);
   if (groups >= int64_t{1} << 24) return FEWBIT_E_INVALID;       // fewer than 2^32 threads: more than a device holds
   return launch_status("fewbit_qk_fwd", start(a, r, false, static_cast<unsigned>(groups), static_cast<hipStream_t>(stream)));
 }
@@ -390,7 +411,7 @@ extern "C" int64_t fewbit_qk_workspace(const fewbit_qk* a) {
   const int rc = check(a);
   if (rc != FEWBIT_OK) return rc;
   if (nothing(a)) return 0;
-  return parts_of(a, args_of(a, nullptr, nullptr, nullptr)) * 2 * a->head_dim * static_cast<int64_t>(sizeof(float));
+  return parts_of(a, args_of(a, nullptr, nullptr, nullptr, true)) * 2 * a->head_dim * static_cast<int64_t>(sizeof(float));
 }
 
 extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void* dk_out, const void* q, const void* k,
@@ -417,7 +438,7 @@ extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void*
   const hipStream_t s = static_cast<hipStream_t>(stream);
   int64_t parts = 0;
   if (!none) {
-    Args r = args_of(a, cos, sin, positions);
+    Args r = args_of(a, cos, sin, positions, true);
     r.s[0].x = q;
     r.s[1].x = k;
     r.s[0].w = q_weight;
