@@ -1,0 +1,173 @@
+"""The operators together: the example stack trains, its gradients are those of plain
+attention and torch's own activation rule, its cached generation agrees with the
+whole-sequence forward, and the optimizer class steps, saves and restores.
+"""
+import math
+
+import pytest
+import torch
+import torch.nn.functional as F
+
+import paper_2202_00441_amd as P
+from paper_2202_00441_amd import transformer as TR
+
+pytestmark = pytest.mark.gpu
+
+
+def plain_block(block, x, cos, sin):
+    """The block's formulas in the types of its parameters (fp64 here)."""
+    def norm(y, w):
+        return y * torch.rsqrt(y.square().mean(-1, keepdim=True) + 1e-6) * w
+
+    def turn(y):
+        h = cos.shape[-1]
+        c, s = cos[:y.shape[1]].double().unsqueeze(1), sin[:y.shape[1]].double().unsqueeze(1)
+        a, b = y[..., :h], y[..., h:]
+        return torch.cat((a * c - b * s, b * c + a * s), -1)
+
+    q, k, v = block._heads(x)
+    q, k = turn(norm(q, block.q_norm)), turn(norm(k, block.k_norm))
+    g = block.heads // block.kv_heads
+    q, k, v = (t.transpose(1, 2) for t in (q, k.repeat_interleave(g, 2), v.repeat_interleave(g, 2)))
+    s = q @ k.transpose(2, 3) / math.sqrt(block.head_dim)
+    s = s.masked_fill(torch.ones(s.shape[-2:], dtype=torch.bool, device=x.device).triu(1), -math.inf)
+    return block._rest(x, (torch.softmax(s, -1) @ v).transpose(1, 2))
+
+
+def test_block_against_plain_formulas():
+    """bf16 against fp64 on the same (bf16) weights: every product and every tensor between rounds to 2^-8 of
+    itself, about ten of them one after another with random signs, so 4 % of the norm is far outside chance."""
+    torch.manual_seed(0)
+    block = TR.Block(256, 4, 2, 512, torch.nn.GELU()).cuda().bfloat16()
+    cos, sin = P.rope_tables(100, 64)
+    x = torch.randn(2, 70, 256, device="cuda").bfloat16().requires_grad_()
+    dy = torch.randn(2, 70, 256, device="cuda").bfloat16()
+    y = block(x, cos, sin)
+    params = list(block.parameters())
+    grads = torch.autograd.grad(y, [x, *params], dy)
+    exact = TR.Block(256, 4, 2, 512, torch.nn.GELU()).cuda().double()
+    exact.load_state_dict({k: v.double() for k, v in block.state_dict().items()})
+    xd = x.detach().double().requires_grad_()
+    yd = plain_block(exact, xd, cos, sin)
+    want = torch.autograd.grad(yd, [xd, *exact.parameters()], dy.double())
+    assert float((y.double() - yd).norm() / yd.norm()) < 0.04
+    for g, w in zip(grads, want):
+        assert float((g.double() - w).norm() / w.norm()) < 0.04
+
+
+def test_training_learns_and_holds_less():
+    r = TR.train(steps=40, layers=2, width=256, heads=4, kv_heads=2, batch=8, length=128, tokens=32, lr=1e-3)
+    first, last = sum(r["losses"][:3]) / 3, sum(r["losses"][-3:]) / 3
+    assert first > 3.0 and last < 0.7 * first and all(math.isfinite(v) for v in r["losses"])
+    full = TR.train(steps=2, layers=2, width=256, heads=4, kv_heads=2, batch=8, length=128, tokens=32, bits=None, state_bits=32)
+    # per layer the activation's input of 8 x 128 x 1024 bf16 elements becomes 3 bits each
+    assert full["held_for_backward"] - r["held_for_backward"] >= 2 * 8 * 128 * 1024 * (2 - 3 / 8) * 0.9
+    moments = full["parameters"] * 8
+    assert full["optimizer_state"] - r["optimizer_state"] >= 0.7 * moments
+
+
+def test_generation_agrees_with_the_whole_forward():
+    """Logits of cached single tokens and of chunks against the whole-sequence forward: the same numbers but for the
+    order of sums and bf16's roundings."""
+    torch.manual_seed(1)
+    model = TR.Transformer(50, 256, 3, 4, 1, most=200).cuda().bfloat16()
+    tokens = torch.randint(0, 50, (3, 90), device="cuda")
+    with torch.no_grad():
+        whole = model(tokens).float()
+    cache = model.cache(3, 128)
+    parts = [model.extend(tokens[:, a:b], cache).float() for a, b in ((0, 40), (40, 41), (41, 42), (42, 75), (75, 90))]
+    got = torch.cat(parts, 1)
+    assert float((got - whole).norm() / whole.norm()) < 0.03
+    assert torch.equal(cache.lengths, torch.full((3,), 90, dtype=torch.int32, device="cuda"))
+    out = model.generate(tokens[:, :20], 5)
+    assert out.shape == (3, 5) and int(out.min()) >= 0 and int(out.max()) < 50
+    with pytest.raises(ValueError):
+        model.extend(tokens[:, :0], cache)
+
+
+# ---------------------------------------------------------------- the optimizer class
+def model_and_grads(dtype, seed=0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    params = [torch.nn.Parameter(torch.randn(s, generator=g, device="cuda").to(dtype)) for s in ((40, 30), (7,), (3, 5, 11), (1000,))]
+    params[0] = torch.nn.Parameter(params[0].detach().t())           # not contiguous
+    grads = [[torch.randn(p.shape, generator=g, device="cuda").to(dtype) for p in params] for _ in range(4)]
+    return params, grads
+
+
+@pytest.mark.parametrize("dtype", (torch.float32, torch.bfloat16))
+def test_optimizer_in_32_bits_is_torchs(dtype):
+    """Against torch.optim.AdamW in fp32 over four steps: a weight moves by the same update to a few roundings."""
+    params, grads = model_and_grads(dtype)
+    other = [torch.nn.Parameter(p.detach().float().clone()) for p in params]
+    opt = P.AdamW(params, lr=1e-2, betas=(0.9, 0.99), weight_decay=0.1, state_bits=32, master=dtype != torch.float32)
+    want = torch.optim.AdamW(other, lr=1e-2, betas=(0.9, 0.99), weight_decay=0.1, foreach=False)
+    for step in grads:
+        for p, o, g in zip(params, other, step):
+            p.grad, o.grad = g, g.float()
+        opt.step()
+        want.step()
+    for p, o in zip(params, other):
+        tol = 1e-6 if dtype == torch.float32 else 2.0 ** -8 * o.abs() + 1e-6
+        assert ((p.detach().float() - o.detach()).abs() <= tol).all()
+
+
+def test_optimizer_saves_and_restores():
+    params, grads = model_and_grads(torch.bfloat16)
+    opt = P.AdamW([{"params": params[:2]}, {"params": params[2:], "lr": 1e-4, "weight_decay": 0.0}], lr=1e-3, master=True)
+
+    def step(o, ps, gs):
+        for p, g in zip(ps, gs):
+            p.grad = g
+        o.step()
+
+    step(opt, params, grads[0])
+    saved = opt.state_dict()
+    saved = {**saved, "buffers": [{k: v.clone() if torch.is_tensor(v) else v for k, v in b.items()} for b in saved["buffers"]]}
+    again = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    other = P.AdamW([{"params": again[:2]}, {"params": again[2:]}], lr=5.0, master=True)
+    other.load_state_dict(saved)
+    for g in grads[1:]:
+        step(opt, params, g)
+        step(other, again, g)
+    assert all(torch.equal(a, b) for a, b in zip(params, again))
+    assert other.param_groups[1]["lr"] == 1e-4 and other.state_bytes() == opt.state_bytes() > 0
+    with pytest.raises(ValueError):
+        P.AdamW([{"params": again[:2]}, {"params": again[2:]}], master=False).load_state_dict(saved)
+    with pytest.raises(ValueError):
+        P.AdamW(again, master=True).load_state_dict(saved)
+
+
+def test_optimizer_leaves_out_what_has_no_gradient():
+    params, grads = model_and_grads(torch.float32)
+    extra = torch.nn.Parameter(torch.randn(9, device="cuda").half())
+    opt = P.AdamW([*params, extra], lr=1e-2)
+    before = [p.detach().clone() for p in params]
+    params[0].grad, params[3].grad, extra.grad = grads[0][0], grads[0][3], torch.ones(9, device="cuda").half()
+    assert opt.step(lambda: torch.tensor(2.0)) == 2.0
+    assert not torch.equal(params[0], before[0]) and not torch.equal(params[3], before[3])
+    assert torch.equal(params[1], before[1]) and torch.equal(params[2], before[2])
+    with pytest.raises(ValueError):
+        P.AdamW(params, state_bits=16)
+    opt.param_groups[0]["params"].append(torch.nn.Parameter(torch.zeros(5, device="cuda")))
+    opt.param_groups[0]["params"][-1].grad = torch.zeros(5, device="cuda")
+    with pytest.raises(RuntimeError):
+        opt.step()
+
+
+def test_losses_of_plain_adamw_are_followed():
+    """The same small regression by torch.optim.AdamW in 32 bits and by 8-bit moments: both come down alike."""
+    torch.manual_seed(3)
+    x = torch.randn(512, 64, device="cuda")
+    y = torch.tanh(x @ torch.randn(64, 8, device="cuda") / 8)
+    finals = []
+    for make in (lambda p: torch.optim.AdamW(p, lr=3e-3, weight_decay=0.0), lambda p: P.AdamW(p, lr=3e-3, weight_decay=0.0)):
+        torch.manual_seed(4)
+        net = torch.nn.Sequential(torch.nn.Linear(64, 128), torch.nn.Tanh(), torch.nn.Linear(128, 8)).cuda()
+        opt = make(net.parameters())
+        for _ in range(300):
+            loss = F.mse_loss(net(x), y)
+            opt.zero_grad()
+            loss.backward()
+            opt.step()
+        finals.append(float(loss.detach()))
+    assert finals[0] < 0.02 and finals[1] < 3 * finals[0] + 1e-3
