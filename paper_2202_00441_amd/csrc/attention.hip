@@ -57,16 +57,18 @@ struct Args {
   float* lse;
   float* stats;                       // backward: lse * log2(e) of every row (infinity if it is empty), then delta; lifted
   int64_t stats_delta;
-  float *part_o, *part_lse;           // split forward
+  float *part_o, *part_lse;           // forward: results that are to be joined
+  float *part_dq, *part_dkv;          // backward: the same
   const int32_t *cu_q, *cu_k, *k_len;
   int64_t qs[3], ks[3], vs[3], ds[3];
   int64_t rows_q, rows_k;
   int batch, hq, hkv, g, d;           // g: query heads to a key head
   int causal, window;
   float scale;
-  Divisor by_g;
+  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads;
   int tiles;                          // of a sequence (packed: places for tiles of all)
   int shares, unit_rows;              // split forward: workgroups of a key head, rows of a unit
+  int parts, parts_dkv;               // of a workgroup's walk (forward or dQ; dK and dV)
 };
 
 // One (sequence, key head): where its rows begin and how many there are.
@@ -139,14 +141,50 @@ __device__ __forceinline__ bool find(const Args& a, bool keys, int times, int ro
     tile = keys ? tile : tiles - 1 - tile;
     return true;
   }
-  s.b = place % a.batch;
-  tile = place / a.batch;
+  tile = a.by_batch.divide(place);
+  s.b = place - tile * a.batch;
   if (!keys) tile = a.tiles - 1 - tile;       // of keys the first are seen by the most rows
   s.q0 = s.k0 = 0;
   s.nq = static_cast<int>(a.rows_q);
   s.nk = a.k_len ? clamped(a.k_len[s.b], a.rows_k) : static_cast<int>(a.rows_k);
   return true;
 }
+
+// The first and one past the last key that query `pos` sees.
+struct Range {
+  int lo, hi;
+};
+__device__ __forceinline__ Range keys_of(const Args& a, const Seq& s, int pos) {
+  const int here = pos + s.nk - s.nq;           // below 2^30 either way, as the window is
+  Range r{0, s.nk};
+  if (a.causal) r.hi = min(max(here + 1, 0), s.nk);
+  if (a.window) r.lo = min(max(here + 1 - a.window, 0), s.nk);
+  return r;
+}
+
+// Keys that any of a workgroup's rows sees, and rows of all sequences and heads.
+constexpr int kThreads = 256, kWaves = kThreads / kWave;
+constexpr int kRowsWave = 32, kRowsGroup = kWaves * kRowsWave;      // rows of a wave and of a workgroup
+__device__ __forceinline__ Range keys_of_group(const Args& a, const Seq& s, int first, int rows) {
+  return {keys_of(a, s, a.by_g.divide(first)).lo, keys_of(a, s, a.by_g.divide(min(first + kRowsGroup, rows) - 1)).hi};
+}
+__device__ __forceinline__ int64_t rows_all(const Args& a) { return (a.cu_q ? 1 : a.batch) * a.rows_q * a.hq; }
+
+// Rows (query * G + head) that see key j, and that see any of a workgroup's keys; keys
+// of all sequences and heads.
+__device__ __forceinline__ Range rows_of_key(int g, int causal, int window, const Seq& s, int j) {
+  const int here = j - s.nk + s.nq;             // the query that stands at key j
+  Range r{0, s.nq * g};
+  if (causal) r.lo = min(max(here, 0), s.nq) * g;
+  if (window) r.hi = min(max(here + window, 0), s.nq) * g;
+  if (j >= s.nk) r.hi = 0;
+  return r;
+}
+__device__ __forceinline__ Range rows_of_keys(const Args& a, const Seq& s, int first, int n) {
+  if (first >= s.nk) return {0, 0};
+  return {rows_of_key(a.g, a.causal, a.window, s, first).lo, rows_of_key(a.g, a.causal, a.window, s, min(first + n, s.nk) - 1).hi};
+}
+__device__ __forceinline__ int64_t keys_all(const Args& a) { return (a.cu_q ? 1 : a.batch) * a.rows_k * a.hkv; }
 
 // Sixteen lanes that read a chunk each of rows one after another, and 32 lanes of a
 // transposing read, which take 64 bytes of four rows, then touch every bank once.
@@ -247,6 +285,30 @@ struct Rows {
   }
 };
 
+// Where there are few workgroups, several share one's walk: part `part` of `parts` of
+// the passes of `step` that it takes to get through `all`, two passes at least each; how
+// many parts there are then.
+constexpr int kPassesPart = 2;
+struct Slice {
+  Range r;
+  int used;
+};
+__device__ __forceinline__ Slice slice_of(Range all, int step, int parts, int part) {
+  const int begin = all.lo / step * step, n = all.hi > begin ? (all.hi - begin + step - 1) / step : 0;
+  if (parts == 1) return {{begin, all.hi}, 1};
+  const int per = max(kPassesPart, (n + parts - 1) / parts);
+  return {{begin + part * per * step, min(all.hi, begin + (part + 1) * per * step)}, max(1, (n + per - 1) / per)};
+}
+
+// A workgroup's key head, part of the walk and place.
+struct Spot {
+  int hk, part, place;
+};
+__device__ __forceinline__ Spot spot_of(const Divisor& by_hkv, const Divisor& by_parts) {
+  const int id = static_cast<int>(blockIdx.x), rest = by_hkv.divide(id), place = by_parts.divide(rest);
+  return {id - rest * static_cast<int>(by_hkv.n), rest - place * static_cast<int>(by_parts.n), place};
+}
+
 // Two tiles that come and are worked on together.
 template <class T, int N>
 struct Pair {
@@ -344,16 +406,25 @@ __device__ __forceinline__ typename Mma<DT>::V8 narrow(const f32x16& x, int step
   return r;
 }
 
-// A row of a tensor as second operand: elements 16 step + 8 (lane / 32) ..+7 of
-// lane's row, zeros for a row that is not there.
-template <int DT, int D>
-__device__ __forceinline__ void load_rows(const typename Mma<DT>::T* row, int d, typename Mma<DT>::V8 (&x)[D / 16]) {
+// A row of a tensor as second operand: elements 16 step + 8 (lane / 32) ..+7 of the
+// lane's row, zeros past head_dim (and, with ZERO, for a row that is not there).
+template <int DT, int D, bool ZERO = false>
+__device__ __forceinline__ void load_rows(const typename Mma<DT>::T* row, int d, typename Mma<DT>::V8 (&x)[D / 16], bool there = true) {
   using V8 = typename Mma<DT>::V8;
   const int c = threadIdx.x % kWave / 32 * 8;
+  if (d == D) {
 #pragma unroll
-  for (int s = 0; s < D / 16; ++s) {
-    x[s] = V8{};
-    if (row && 16 * s + c < d) x[s] = *reinterpret_cast<const V8*>(row + 16 * s + c);
+    for (int s = 0; s < D / 16; ++s) x[s] = *reinterpret_cast<const V8*>(row + 16 * s + c);
+  } else {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) {
+      x[s] = V8{};
+      if (16 * s + c < d) x[s] = *reinterpret_cast<const V8*>(row + 16 * s + c);
+    }
+  }
+  if (ZERO && !there) {
+#pragma unroll
+    for (int s = 0; s < D / 16; ++s) x[s] = V8{};
   }
 }
 
@@ -374,16 +445,17 @@ __device__ __forceinline__ void store_rows(typename Mma<DT>::T* row, int d, cons
     }
 }
 
-// The first and one past the last key that query `pos` sees.
-struct Range {
-  int lo, hi;
-};
-__device__ __forceinline__ Range keys_of(const Args& a, const Seq& s, int pos) {
-  const int64_t here = static_cast<int64_t>(pos) + s.nk - s.nq;
-  Range r{0, s.nk};
-  if (a.causal) r.hi = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(s.nk), here + 1)));
-  if (a.window) r.lo = static_cast<int>(max(static_cast<int64_t>(0), min(static_cast<int64_t>(s.nk), here + 1 - a.window)));
-  return r;
+// The same as fp32.
+template <int D>
+__device__ __forceinline__ void store_rows32(float* row, int d, const f32x16 (&x)[D / 32], float scale) {
+  const int c = threadIdx.x % kWave / 32 * 4;
+#pragma unroll
+  for (int t = 0; t < D / 32; ++t)
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int at = 32 * t + 8 * u + c;
+      if (at < d) *reinterpret_cast<f32x4*>(row + at) = f32x4{x[t][4 * u], x[t][4 * u + 1], x[t][4 * u + 2], x[t][4 * u + 3]} * scale;
+    }
 }
 
 __device__ __forceinline__ int key_of(int i) { return 8 * (i / 4) + i % 4; }      // plus 4 (lane / 32)
@@ -465,8 +537,6 @@ __device__ __forceinline__ void gather(const typename Mma<DT>::T* lv, const Colu
     }
 }
 
-constexpr int kThreads = 256, kWaves = kThreads / kWave;
-constexpr int kRowsWave = 32, kRowsGroup = kWaves * kRowsWave;      // rows of a wave and of a workgroup
 constexpr int kKeys = 64;                                           // keys of a pass
 constexpr int kPassesShare = 2;                                     // of a share of the split forward at least
 
@@ -474,24 +544,28 @@ template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   __shared__ Pair<T, kKeys * D> buf0, buf1;
-  const int hk = blockIdx.x % a.hkv, wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const int wave = threadIdx.x / kWave, lane = threadIdx.x % kWave;
+  const auto [hk, part, place] = spot_of(a.by_hkv, a.by_parts);
   Seq s;
   int tile;
-  if (!find(a, false, a.g, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  if (!find(a, false, a.g, kRowsGroup, place, s, tile)) return;
   const int rows = s.nq * a.g, first = tile * kRowsGroup;
   if (first >= rows) return;
   const int row = first + wave * kRowsWave + lane % 32;
   const bool there = row < rows;
-  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
+  const int pos = a.by_g.divide(min(row, rows - 1)), head = hk * a.g + min(row, rows - 1) - pos * a.g;
   typename Mma<DT>::V8 q[D / 16];
-  load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+  load_rows<DT, D>(static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2], a.d, q);
 
   // keys that any row of the workgroup sees, that this lane's row sees, and that
   // all rows of the wave see
-  const Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsGroup, rows) - 1) / a.g).hi};
+  const Slice slice = slice_of(keys_of_group(a, s, first, rows), kKeys, a.parts, part);
+  const Range all = slice.r;
+  if (part >= slice.used) return;
   const Range own = keys_of(a, s, pos);
   const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
-  const Range every{keys_of(a, s, max(w1, w0) / a.g).lo, keys_of(a, s, w0 / a.g).hi};
+  const int p0 = a.by_g.divide(w0), p1 = a.by_g.divide(max(w1, w0));
+  const Range every{keys_of(a, s, p1).lo, keys_of(a, s, p0).hi};
 
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
@@ -500,7 +574,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   const RowReader<DT, D> rr;
   const ColumnReader<DT, D> cr;
   Running<D> x;
-  walk(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+  walk(all.lo, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
          keys.issue(stage, to.a, k0);
          values.issue(stage, to.b, k0);
@@ -513,8 +587,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   if (!there) return;
   const Two both = halves32(x.sum);
   const float sum = both.a + both.b;
-  store_rows<DT, D>(static_cast<T*>(a.o) + ((s.b * a.rows_q + s.q0 + pos) * a.hq + head) * a.d, a.d, x.o, sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f);
-  if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = sum == 0.0f ? -INFINITY : x.most * a.scale + logf(sum);
+  const float lse = sum == 0.0f ? -INFINITY : x.most * a.scale + logf(sum);
+  const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head;
+  if (slice.used == 1) {
+    store_rows<DT, D>(static_cast<T*>(a.o) + at * a.d, a.d, x.o, inverse);
+    if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = lse;
+  } else {
+    const int64_t to = part * rows_all(a) + at;
+    store_rows32<D>(a.part_o + to * a.d, a.d, x.o, inverse);
+    if (lane < 32) a.part_lse[to] = lse;
+  }
 }
 
 // Few rows over many keys (single tokens over a cache).  Work is cut into units of 32
@@ -536,14 +619,15 @@ struct Unit {
 };
 __device__ __forceinline__ Unit unit_of(const Args& a, int unit) {
   Unit u;
-  u.s.b = unit / a.tiles;
+  const int b = a.tiles == 1 ? unit : unit / a.tiles;
+  u.s.b = b;
   u.s.q0 = u.s.k0 = 0;
   u.s.nq = static_cast<int>(a.rows_q);
   u.s.nk = a.k_len ? clamped(a.k_len[u.s.b], a.rows_k) : static_cast<int>(a.rows_k);
   u.rows = u.s.nq * a.g;
-  u.first = unit % a.tiles * kRowsWave;
-  u.keys.lo = keys_of(a, u.s, u.first / a.g).lo / 32 * 32;
-  u.keys.hi = max(u.keys.lo, keys_of(a, u.s, (min(u.first + kRowsWave, u.rows) - 1) / a.g).hi);
+  u.first = (unit - b * a.tiles) * kRowsWave;
+  u.keys.lo = keys_of(a, u.s, a.by_g.divide(u.first)).lo / 32 * 32;
+  u.keys.hi = max(u.keys.lo, keys_of(a, u.s, a.by_g.divide(min(u.first + kRowsWave, u.rows) - 1)).hi);
   u.passes = max(1, (u.keys.hi - u.keys.lo + kKeysSplit - 1) / kKeysSplit);
   return u;
 }
@@ -615,8 +699,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   __shared__ __attribute__((aligned(16))) T lk[kWaves][32 * D], lv[kWaves][32 * D];
   __shared__ float stats[kWaves][2][32];
-  const int hk = blockIdx.x % a.hkv, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
-  const int share = blockIdx.x / a.hkv;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int share = a.by_hkv.divide(blockIdx.x), hk = static_cast<int>(blockIdx.x) - share * a.hkv;
   const Line line = line_of(a, 0);
   if (share > (line.all - 1) / line.share) return;
   int at = share * line.share;
@@ -628,18 +712,28 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     const int passes = min(u.passes - pass, end - at);
     const bool whole = passes == u.passes;
     at += passes;
-    const int row = u.first + lane % 32;
-    const bool there = row < u.rows;
-    const int pos = min(row, u.rows - 1) / a.g, head = hk * a.g + min(row, u.rows - 1) % a.g;
+    // This lane's query and head; asked for again behind the loop, which has no registers
+    // to keep them in.
+    struct Mine {
+      int pos, head;
+      bool there;
+    };
+    const auto mine = [&]() __attribute__((always_inline)) {
+      int l = lane;
+      asm volatile("" : "+v"(l));
+      const int row = u.first + l % 32, some = min(row, u.rows - 1), pos = a.by_g.divide(some);
+      return Mine{pos, hk * a.g + some - pos * a.g, row < u.rows};
+    };
+    const auto [pos, head, there] = mine();
     const Range own = keys_of(a, s, pos);
-    const Range every{keys_of(a, s, (min(u.first + kRowsWave, u.rows) - 1) / a.g).lo, keys_of(a, s, u.first / a.g).hi};
+    const Range every{keys_of(a, s, a.by_g.divide(min(u.first + kRowsWave, u.rows) - 1)).lo, keys_of(a, s, a.by_g.divide(u.first)).hi};
     Range all;
     all.lo = u.keys.lo + pass * kKeysSplit;
     all.hi = min(u.keys.hi, all.lo + passes * kKeysSplit);
     Running<D> x;
     if (all.lo < all.hi) {
       typename Mma<DT>::V8 q[D / 16];
-      load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + pos * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
+      load_rows<DT, D>(static_cast<const T*>(a.q) + s.b * a.qs[0] + pos * a.qs[1] + head * a.qs[2], a.d, q);
       const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + hk * a.ks[2];
       const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + hk * a.vs[2];
       constexpr int kPolicy = ONCE ? 2 : 0;
@@ -667,6 +761,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
       }
       landed<0>();
     }
+    const auto [pos2, head2, there2] = mine();
     // The waves' results.  Wave t adds up all waves' columns 32 t ..+31 and writes them;
     // the others' come through LDS, three parts for each t.
     const Two both = halves32(x.sum);
@@ -695,7 +790,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const float lse = sum == 0.0f ? -INFINITY : most * a.scale + logf(sum);
     const int64_t part = (static_cast<int64_t>(share + unit) * a.hkv + hk) * a.unit_rows + lane % 32;
-    if (there && wave == 0 && lane < 32) (whole ? a.lse[(s.b * a.hq + head) * a.rows_q + pos] : a.part_lse[part]) = lse;
+    if (there2 && wave == 0 && lane < 32) (whole ? a.lse[(s.b * a.hq + head2) * a.rows_q + pos2] : a.part_lse[part]) = lse;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) {
       if (wave != t) continue;
@@ -707,10 +802,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
 #pragma unroll
       for (int c4 = 0; c4 < 4; ++c4) {
         const int c = 32 * t + 8 * c4 + lane / 32 * 4;
-        if (!there || c >= a.d) continue;
+        if (!there2 || c >= a.d) continue;
         const f32x4 y{o[4 * c4], o[4 * c4 + 1], o[4 * c4 + 2], o[4 * c4 + 3]};
         if (whole)
-          *reinterpret_cast<typename Mma<DT>::V4*>(static_cast<T*>(a.o) + ((s.b * a.rows_q + pos) * a.hq + head) * a.d + c) =
+          *reinterpret_cast<typename Mma<DT>::V4*>(static_cast<T*>(a.o) + ((s.b * a.rows_q + pos2) * a.hq + head2) * a.d + c) =
               __builtin_convertvector(y, typename Mma<DT>::V4);
         else
           *reinterpret_cast<f32x4*>(a.part_o + part * a.d + c) = y;
@@ -762,6 +857,46 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
   if (lane == 0) a.lse[(u.s.b * a.hq + head) * a.rows_q + pos] = sum == 0.0f ? -INFINITY : base + logf(sum);
 }
 
+// The same for the parts of a workgroup's walk over keys: a thread takes four elements of
+// a row; kJoins workgroups share the rows of one.
+constexpr int kPartsMost = 8;
+template <int DT>
+__global__ __launch_bounds__(kThreads) void attn_parts_kernel(const Args a, Divisor by_joins) {
+  using T = typename Mma<DT>::T;
+  const auto [hk, join, place] = spot_of(a.by_hkv, by_joins);
+  Seq s;
+  int tile;
+  if (!find(a, false, a.g, kRowsGroup, place, s, tile)) return;
+  const int rows = s.nq * a.g, first = tile * kRowsGroup, i = join * kThreads + static_cast<int>(threadIdx.x);
+  const int of = a.by_quads.divide(i), c = (i - of * static_cast<int>(a.by_quads.n)) * 4, row = first + of;
+  if (of >= kRowsGroup || row >= rows) return;
+  const int used = slice_of(keys_of_group(a, s, first, rows), kKeys, a.parts, 0).used;
+  if (used == 1) return;
+  const int pos = a.by_g.divide(row), head = hk * a.g + row - pos * a.g;
+  const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head, step = rows_all(a);
+  float lse[kPartsMost], most = -INFINITY, sum = 0.0f;
+  f32x4 parts[kPartsMost], o{};
+#pragma unroll
+  for (int k = 0; k < kPartsMost; ++k) {        // past the last: the last again, with weight 0
+    const int64_t from = min(k, used - 1) * step + at;
+    lse[k] = a.part_lse[from];
+    parts[k] = *reinterpret_cast<const f32x4*>(a.part_o + from * a.d + c);
+  }
+#pragma unroll
+  for (int k = 0; k < kPartsMost; ++k) most = fmaxf(most, lse[k]);
+  const float base = most == -INFINITY ? 0.0f : most;
+#pragma unroll
+  for (int k = 0; k < kPartsMost; ++k) {
+    if (k >= used) break;
+    const float w = __builtin_amdgcn_exp2f((lse[k] - base) * kLog2e);
+    sum += w;
+    o += parts[k] * w;
+  }
+  const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
+  *reinterpret_cast<typename Mma<DT>::V4*>(static_cast<T*>(a.o) + at * a.d + c) = __builtin_convertvector(o * inverse, typename Mma<DT>::V4);
+  if (c == 0) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = sum == 0.0f ? -INFINITY : base + logf(sum);
+}
+
 // ---------------------------------------------------------------- backward
 // The kernel for dK and dV hands P over in the storage type.  In fp16 it hands over
 // 2^15 P, for which small probabilities keep all of their bits too.
@@ -778,24 +913,28 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   using V8 = typename Mma<DT>::V8;
   __shared__ Pair<T, kKeys * D> buf0, buf1;
-  const int hk = blockIdx.x % a.hkv, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), lane = threadIdx.x % kWave;
+  const auto [hk, part, place] = spot_of(a.by_hkv, a.by_parts);
   Seq s;
   int tile;
-  if (!find(a, false, a.g, kRowsGroup, blockIdx.x / a.hkv, s, tile)) return;
+  if (!find(a, false, a.g, kRowsGroup, place, s, tile)) return;
   const int rows = s.nq * a.g, first = tile * kRowsGroup;
   if (first >= rows) return;
+  const Slice slice = slice_of(keys_of_group(a, s, first, rows), kKeys, a.parts, part);
+  const Range all = slice.r;
+  if (part >= slice.used) return;
   const int row = first + wave * kRowsWave + lane % 32;
   const bool there = row < rows;
-  const int pos = min(row, rows - 1) / a.g, head = hk * a.g + min(row, rows - 1) % a.g;
+  const int pos = a.by_g.divide(min(row, rows - 1)), head = hk * a.g + min(row, rows - 1) - pos * a.g;
   const int64_t at = ((s.b * a.rows_q + s.q0 + pos) * a.hq + head) * a.d;
   const int64_t stat = (s.b * a.hq + head) * a.rows_q + s.q0 + pos;
   V8 q[D / 16], dout[D / 16];
-  load_rows<DT, D>(there ? static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2] : nullptr, a.d, q);
-  load_rows<DT, D>(there ? static_cast<const T*>(a.dout) + s.b * a.ds[0] + (s.q0 + pos) * a.ds[1] + head * a.ds[2] : nullptr, a.d, dout);
+  load_rows<DT, D>(static_cast<const T*>(a.q) + s.b * a.qs[0] + (s.q0 + pos) * a.qs[1] + head * a.qs[2], a.d, q);
+  load_rows<DT, D>(static_cast<const T*>(a.dout) + s.b * a.ds[0] + (s.q0 + pos) * a.ds[1] + head * a.ds[2], a.d, dout);
   float delta = 0.0f;
   {
     V8 o[D / 16];
-    load_rows<DT, D>(there ? static_cast<const T*>(a.out) + at : nullptr, a.d, o);
+    load_rows<DT, D>(static_cast<const T*>(a.out) + at, a.d, o);
 #pragma unroll
     for (int i = 0; i < D / 16; ++i)
 #pragma unroll
@@ -805,16 +944,16 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   }
   float lse = there ? a.lse[stat] : -INFINITY;
   lse = lse == -INFINITY ? INFINITY : lse * kLog2e;           // of an empty row no key is seen
-  if (there && lane < 32) {
+  if (there && lane < 32 && part == 0) {
     a.stats[stat] = lse - kLift<DT>;
     a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift<DT>);
   }
 
-  const Range all{keys_of(a, s, first / a.g).lo, keys_of(a, s, (min(first + kRowsGroup, rows) - 1) / a.g).hi};
   const Range own = keys_of(a, s, pos);
   const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
-  const Range every{keys_of(a, s, max(w1, w0) / a.g).lo, keys_of(a, s, w0 / a.g).hi};
-  const Range any{keys_of(a, s, w0 / a.g).lo, keys_of(a, s, max(w1, w0) / a.g).hi};
+  const int p0 = a.by_g.divide(w0), p1 = a.by_g.divide(max(w1, w0));
+  const Range every{keys_of(a, s, p1).lo, keys_of(a, s, p0).hi};
+  const Range any{keys_of(a, s, p0).lo, keys_of(a, s, p1).hi};
 
   const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + s.k0 * a.ks[1] + hk * a.ks[2];
   const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2];
@@ -824,7 +963,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   const ColumnReader<DT, D> columns_at;
   f32x16 dq[D / 32] = {};
   const float scale2 = a.scale * kLog2e;
-  walk(all.lo / kKeys * kKeys, kKeys, all.hi, buf0, buf1,
+  walk(all.lo, kKeys, all.hi, buf0, buf1,
        [&](Pair<T, kKeys * D>& to, int k0) {
          keys.issue(stage, to.a, k0);
          values.issue(stage, to.b, k0);
@@ -859,7 +998,11 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
            }
          }
        });
-  if (there) store_rows<DT, D>(static_cast<T*>(a.dq) + at, a.d, dq, a.scale);
+  if (!there) return;
+  if (slice.used == 1)
+    store_rows<DT, D>(static_cast<T*>(a.dq) + at, a.d, dq, a.scale);
+  else
+    store_rows32<D>(a.part_dq + part * rows_all(a) * a.d + at, a.d, dq, a.scale);
 }
 
 // A workgroup takes 4 runs of 32 SUBS keys and walks the rows that see them, 32 at a
@@ -880,16 +1023,20 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   };
   __shared__ Buffer buf0, buf1, buf2;
   __shared__ V8 handed[2][kPairs][SUBS][kRowsPass / 16][kWave];
-  const int hk = blockIdx.x % a.hkv, lane = threadIdx.x % kWave;
+  const int lane = threadIdx.x % kWave;
+  const auto [hk, part, place] = spot_of(a.by_hkv, a.by_parts_dkv);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), pair = wave % kPairs;
   const bool second = wave >= kPairs;             // of a pair: dP, dS and dK
   Seq s;
   int tile;
-  if (!find(a, true, 1, kGroup, blockIdx.x / a.hkv, s, tile)) return;
+  if (!find(a, true, 1, kGroup, place, s, tile)) return;
   // keys past those that are there have gradients too: zeros
   const int keys = a.cu_k ? s.nk : static_cast<int>(a.rows_k), first = tile * kGroup;
   if (first >= keys) return;
   const int run = first + pair * kRun;
+  const Slice slice = slice_of(rows_of_keys(a, s, first, kGroup), kRowsPass, a.parts_dkv, part);
+  const Range all = slice.r;
+  if (part >= slice.used) return;
   V8 kv[SUBS][D / 16];
   {
     const T* base = second ? static_cast<const T*>(a.v) + s.b * a.vs[0] + s.k0 * a.vs[1] + hk * a.vs[2]
@@ -898,22 +1045,12 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
 #pragma unroll
     for (int u = 0; u < SUBS; ++u) {
       const int key = run + 32 * u + lane % 32;
-      load_rows<DT, D>(key < s.nk ? base + key * stride : nullptr, a.d, kv[u]);
+      load_rows<DT, D, true>(base + min(key, max(s.nk - 1, 0)) * stride, a.d, kv[u], key < s.nk);
     }
   }
 
-  // rows (query * G + head) that see a key: from lo to before hi
   const int rows = s.nq * a.g;
-  const auto rows_of = [&](int j) {
-    const int64_t here = static_cast<int64_t>(j) - s.nk + s.nq;        // the query that stands at key j
-    Range r{0, rows};
-    if (a.causal) r.lo = static_cast<int>(max(static_cast<int64_t>(0), min(here * a.g, static_cast<int64_t>(rows))));
-    if (a.window) r.hi = static_cast<int>(max(static_cast<int64_t>(0), min((here + a.window) * a.g, static_cast<int64_t>(rows))));
-    if (j >= s.nk) r.hi = 0;
-    return r;
-  };
-  Range all{0, 0};
-  if (first < s.nk) all = Range{rows_of(first).lo, rows_of(min(first + kGroup, s.nk) - 1).hi};
+  const auto rows_of = [g = a.g, causal = a.causal, window = a.window, s](int j) __attribute__((always_inline)) { return rows_of_key(g, causal, window, s, j); };
   const Range every{rows_of(run + kRun - 1).lo, run + kRun <= s.nk ? rows_of(run).hi : 0};      // that all keys of the run are seen by
   const Range any{rows_of(run).lo, run < s.nk ? rows_of(min(run + kRun, s.nk) - 1).hi : 0};      // that any is
 
@@ -928,7 +1065,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   const bool near = a.g == 1 << g_bits && a.g <= kRowsPass && pos_stride < kNear / 16 && head_stride < kNear / 16;
   uint32_t offset[decltype(stage)::kLoads];
   stage.offsets([&](int i) { return (i >> g_bits) * static_cast<int>(pos_stride) + (i & (a.g - 1)) * static_cast<int>(head_stride); }, offset);
-  const auto issue = [&](Buffer& to, int r0) {
+  const auto issue = [&](Buffer& to, int r0) __attribute__((always_inline)) {
     // the first waves of the pairs bring Q and lse, the second dO and delta
     T* lds = second ? to.b : to.a;
     if (near && r0 + kRowsPass <= rows)
@@ -952,7 +1089,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   const float scale2 = a.scale * kLog2e;
   // One side's part of a tile of rows: SECOND and MASKED are constants, so that each
   // is one run of code in which products and the rest overlap.
-  const auto work = [&](auto SECOND, auto MASKED, const Buffer& in, int r0, int slot) {
+  const auto work = [&](auto SECOND, auto MASKED, const Buffer& in, int r0, int slot) __attribute__((always_inline)) {
     const T *x = SECOND ? in.b : in.a, *y = SECOND ? in.a : in.b;
     const auto rr = rows_at.here();
     const auto cr = columns_at.here();
@@ -1006,8 +1143,8 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
 
   // turn i: tile i + 1 comes, the pairs' first waves work on tile i and their second
   // waves on tile i - 1
-  const int begin = all.lo / kRowsPass * kRowsPass, tiles = all.hi > begin ? (all.hi - begin + kRowsPass - 1) / kRowsPass : 0;
-  const auto turn = [&](Buffer& now, Buffer& before, Buffer& next, int i) {
+  const int begin = all.lo, tiles = all.hi > begin ? (all.hi - begin + kRowsPass - 1) / kRowsPass : 0;
+  const auto turn = [&](Buffer& now, Buffer& before, Buffer& next, int i) __attribute__((always_inline)) {
     landed<0>();
     __syncthreads();
     if (i + 1 < tiles) issue(next, begin + (i + 1) * kRowsPass);
@@ -1039,9 +1176,60 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   for (int u = 0; u < SUBS; ++u) {
     const int key = run + 32 * u + lane % 32;
     if (key >= keys) continue;
-    store_rows<DT, D>(static_cast<T*>(second ? a.dk : a.dv) + ((s.b * a.rows_k + s.k0 + key) * a.hkv + hk) * a.d, a.d, acc[u],
-                      second ? a.scale : lower);
+    const int64_t at = (s.b * a.rows_k + s.k0 + key) * a.hkv + hk;
+    const float scale = second ? a.scale : lower;
+    if (slice.used == 1)
+      store_rows<DT, D>(static_cast<T*>(second ? a.dk : a.dv) + at * a.d, a.d, acc[u], scale);
+    else
+      store_rows32<D>(a.part_dkv + ((part * keys_all(a) + at) * 2 + second) * a.d, a.d, acc[u], scale);
   }
+}
+
+// Sums of the parts of both kernels' walks, in their order, four elements a thread:
+// workgroups for rows, then workgroups for runs of `group` keys.
+__device__ __forceinline__ f32x4 sum_of(const float* parts, int64_t step, int used) {
+  f32x4 x[kPartsMost], sum{};
+#pragma unroll
+  for (int k = 0; k < kPartsMost; ++k) x[k] = *reinterpret_cast<const f32x4*>(parts + min(k, used - 1) * step);
+#pragma unroll
+  for (int k = 0; k < kPartsMost; ++k)
+    if (k < used) sum += x[k];
+  return sum;
+}
+template <int DT>
+__global__ __launch_bounds__(kThreads) void attn_sums_kernel(const Args a, Divisor by_joins_q, Divisor by_joins_k, int q_groups, int group,
+                                                             int tiles_k) {
+  using T = typename Mma<DT>::T;
+  using V4 = typename Mma<DT>::V4;
+  const bool keys = static_cast<int>(blockIdx.x) >= q_groups;
+  const int id = static_cast<int>(blockIdx.x) - (keys ? q_groups : 0), rest = a.by_hkv.divide(id), hk = id - rest * a.hkv;
+  const Divisor& by = keys ? by_joins_k : by_joins_q;
+  const int place = by.divide(rest), i = (rest - place * static_cast<int>(by.n)) * kThreads + static_cast<int>(threadIdx.x);
+  const int of = a.by_quads.divide(i), c = (i - of * static_cast<int>(a.by_quads.n)) * 4;
+  Seq s;
+  int tile;
+  if (!keys) {
+    if (!find(a, false, a.g, kRowsGroup, place, s, tile)) return;
+    const int rows = s.nq * a.g, first = tile * kRowsGroup, row = first + of;
+    if (of >= kRowsGroup || row >= rows) return;
+    const int used = slice_of(keys_of_group(a, s, first, rows), kKeys, a.parts, 0).used;
+    if (used == 1) return;
+    const int pos = a.by_g.divide(row);
+    const int64_t at = ((s.b * a.rows_q + s.q0 + pos) * a.hq + hk * a.g + row - pos * a.g) * a.d + c;
+    *reinterpret_cast<V4*>(static_cast<T*>(a.dq) + at) = __builtin_convertvector(sum_of(a.part_dq + at, rows_all(a) * a.d, used), V4);
+    return;
+  }
+  Args b = a;
+  b.tiles = tiles_k;
+  if (!find(b, true, 1, group, place, s, tile)) return;
+  const int all = a.cu_k ? s.nk : static_cast<int>(a.rows_k), first = tile * group, key = first + of;
+  if (of >= group || key >= all) return;
+  const int used = slice_of(rows_of_keys(a, s, first, group), kRowsPass, a.parts_dkv, 0).used;
+  if (used == 1) return;
+  const int64_t at = (s.b * a.rows_k + s.k0 + key) * a.hkv + hk, step = keys_all(a) * 2 * a.d;
+  const float* p = a.part_dkv + at * 2 * a.d + c;
+  *reinterpret_cast<V4*>(static_cast<T*>(a.dv) + at * a.d + c) = __builtin_convertvector(sum_of(p, step, used), V4);
+  *reinterpret_cast<V4*>(static_cast<T*>(a.dk) + at * a.d + c) = __builtin_convertvector(sum_of(p + a.d, step, used), V4);
 }
 
 // ---------------------------------------------------------------- host side
@@ -1093,6 +1281,37 @@ bool all_whole(const fewbit_attn* a, int64_t shares) {
   return std::max<int64_t>(kPassesShare, over(each * a->batch, shares)) % each == 0;
 }
 
+// Parts of every workgroup's walk of `passes` passes at most: as many as give every CU a
+// workgroup (under a causal mask two, for the walks' lengths differ), where that shortens
+// the walk by enough to pay for the join's launch and traffic, eight passes.  Forward and
+// backward in a row, one and divided: 2 sequences of 2352 rows and 1 head, 38 workgroups of
+// 37 passes, 191 and 96 us; 2 of 807 and 16 heads, causal, 224 workgroups of 13, 84 and 106 us
+// in two parts each, which the rule leaves whole.
+int64_t parts_of(int64_t groups, int64_t passes, int64_t cus, bool uneven) {
+  const int64_t parts = std::min({(uneven ? 2 * cus : cus) / std::max<int64_t>(groups, 1), passes / kPassesPart, int64_t{kPartsMost}});
+  return parts > 1 && passes - over(passes, parts) >= 8 ? parts : 1;
+}
+
+// Runs of 64 keys where two of them and their gradients fit a wave's registers, else 32.
+int64_t keys_dkv(int d) { return kPairs * (d <= 64 ? 64 : 32); }
+
+// Workgroups of the kernels, and parts of their walks.
+struct Grid {
+  int64_t q_places, k_places, parts, parts_dkv;
+};
+Grid grid_of(const fewbit_attn* a, bool back) {
+  const int64_t g = a->heads_q / a->heads_kv, cus = device_cus();
+  Grid r{places_of(a, a->rows_q * g, kRowsGroup), places_of(a, a->rows_k, keys_dkv(a->head_dim)), 1, 1};
+  const int64_t seqs = a->cu_q ? std::max<int64_t>(a->batch, 1) : 1;              // packed: lengths are not known here
+  const int64_t keys = a->rows_k / seqs, rows = a->rows_q * g / seqs;
+  const bool uneven = a->causal && !a->window && 2 * a->rows_q > a->rows_k;
+  const int64_t seen = a->window ? std::min<int64_t>(keys, int64_t{a->window} + kRowsGroup / g) : keys;
+  const int64_t seers = a->window ? std::min(rows, (a->window + keys_dkv(a->head_dim)) * g) : rows;
+  r.parts = parts_of(r.q_places * a->heads_kv, over(seen, kKeys), cus, uneven);
+  if (back) r.parts_dkv = parts_of(r.k_places * a->heads_kv, over(seers, kRowsPass), cus, uneven);
+  return r;
+}
+
 Args args_of(const fewbit_attn* a) {
   Args r{};
   r.cu_q = a->cu_q;
@@ -1112,11 +1331,17 @@ Args args_of(const fewbit_attn* a) {
   r.g = a->heads_q / a->heads_kv;
   r.d = a->head_dim;
   r.causal = a->causal;
-  r.window = a->window;
+  r.window = std::min(a->window, 1 << 30);
   r.scale = a->scale;
   r.by_g = divisor(r.g);
+  r.by_hkv = divisor(r.hkv);
+  r.by_batch = divisor(std::max(r.batch, 1));
+  r.by_parts = r.by_parts_dkv = divisor(1);
+  r.by_quads = divisor(r.d / 4);
   return r;
 }
+
+int64_t rounded(int64_t n) { return over(n, 4) * 4; }         // floats, to whole 16 bytes
 
 bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // fewer than 2^32 threads
 
@@ -1132,9 +1357,6 @@ hipError_t start_split(const Args& r, bool bf16, unsigned groups, hipStream_t st
                    : launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 128, ONCE> : attn_split_kernel<FEWBIT_F16, 128, ONCE>, dim3(groups), kThreads, st, r);
 }
 
-// Runs of 64 keys where two of them and their gradients fit a wave's registers, else 32.
-int64_t keys_dkv(int d) { return kPairs * (d <= 64 ? 64 : 32); }
-
 hipError_t start_dkv(const Args& r, bool bf16, unsigned groups, hipStream_t st) {
   return r.d <= 64 ? launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 64, 2> : attn_dkv_kernel<FEWBIT_F16, 64, 2>, dim3(groups), kThreadsPairs, st, r)
                    : launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 128, 1> : attn_dkv_kernel<FEWBIT_F16, 128, 1>, dim3(groups), kThreadsPairs, st, r);
@@ -1146,9 +1368,15 @@ extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward)
   const int rc = check(a);
   if (rc != FEWBIT_OK) return rc;
   const int64_t rows = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
-  if (backward) return 2 * rows * static_cast<int64_t>(sizeof(float));
+  const Grid g = grid_of(a, backward != 0);
+  if (backward) {
+    const int64_t keys = (a->cu_q ? 1 : a->batch) * a->rows_k * a->heads_kv;
+    return (2 * rounded(rows) + (g.parts > 1 ? g.parts * rows * a->head_dim : 0) + (g.parts_dkv > 1 ? g.parts_dkv * keys * 2 * a->head_dim : 0)) *
+           static_cast<int64_t>(sizeof(float));
+  }
   const int64_t shares = shares_of(a), units = over(a->rows_q * (a->heads_q / a->heads_kv), kRowsWave) * a->batch;
-  return shares > 0 ? (shares + units) * a->heads_kv * unit_rows(a) * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float)) : 0;
+  const int64_t left = shares > 0 ? (shares + units) * a->heads_kv * unit_rows(a) : g.parts > 1 ? g.parts * rows : 0;
+  return left * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float));
 }
 
 extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* k, const void* v, void* out, float* lse,
@@ -1177,10 +1405,20 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   const int64_t rows = a->rows_q * r.g;
   r.shares = static_cast<int>(shares_of(a));
   if (r.shares == 0) {
+    const Grid g = grid_of(a, false);
     r.tiles = static_cast<int>(over(rows, kRowsGroup));
-    const int64_t groups = places_of(a, rows, kRowsGroup) * r.hkv;
-    if (!fits_launch(groups)) return FEWBIT_E_INVALID;
-    return launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_fwd_kernel, r, groups, st));
+    r.parts = static_cast<int>(g.parts);
+    r.by_parts = divisor(r.parts);
+    if (r.parts > 1) {
+      r.part_o = static_cast<float*>(workspace);
+      r.part_lse = r.part_o + g.parts * (a->cu_q ? 1 : a->batch) * a->rows_q * r.hq * r.d;
+    }
+    const int64_t share = over(int64_t{kRowsGroup} * r.d / 4, kThreads), joins = g.q_places * r.hkv * share, groups = g.q_places * r.hkv * g.parts;
+    if (!fits_launch(groups) || (r.parts > 1 && !fits_launch(joins))) return FEWBIT_E_INVALID;
+    rc = launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_fwd_kernel, r, groups, st));
+    if (rc != FEWBIT_OK || r.parts == 1) return rc;
+    return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_parts_kernel<FEWBIT_BF16> : attn_parts_kernel<FEWBIT_F16>,
+                                                   dim3(static_cast<unsigned>(joins)), kThreads, st, r, divisor(static_cast<int>(share))));
   }
   r.tiles = static_cast<int>(over(rows, kRowsWave));
   const int64_t units = r.tiles * a->batch;
@@ -1222,21 +1460,38 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   r.dout = dout;
   r.lse = const_cast<float*>(lse);
   r.stats = static_cast<float*>(workspace);
-  r.stats_delta = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
+  const int64_t rows_all = (a->cu_q ? 1 : a->batch) * a->rows_q * a->heads_q;
+  r.stats_delta = rounded(rows_all);
   r.dq = dq;
   r.dk = dk;
   r.dv = dv;
-  const int64_t rows = a->rows_q * r.g;
-  const int64_t q_groups = places_of(a, rows, kRowsGroup) * r.hkv, k_groups = places_of(a, a->rows_k, keys_dkv(r.d)) * r.hkv;
+  const Grid g = grid_of(a, true);
+  const int64_t rows = a->rows_q * r.g, q_groups = g.q_places * r.hkv * g.parts, k_groups = g.k_places * r.hkv * g.parts_dkv;
   if (!fits_launch(q_groups) || !fits_launch(k_groups)) return FEWBIT_E_INVALID;
+  r.parts = static_cast<int>(g.parts);
+  r.parts_dkv = static_cast<int>(g.parts_dkv);
+  r.by_parts = divisor(r.parts);
+  r.by_parts_dkv = divisor(r.parts_dkv);
+  r.part_dq = r.stats + 2 * r.stats_delta;
+  r.part_dkv = r.part_dq + (g.parts > 1 ? g.parts * rows_all * r.d : 0);
+  const int tiles_q = static_cast<int>(over(rows, kRowsGroup)), tiles_k = static_cast<int>(over(a->rows_k, keys_dkv(r.d)));
   if (a->rows_q > 0) {
-    r.tiles = static_cast<int>(over(rows, kRowsGroup));
+    r.tiles = tiles_q;
     rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dq_kernel, r, q_groups, st));
     if (rc != FEWBIT_OK) return rc;
   }
   if (a->rows_k > 0) {
-    r.tiles = static_cast<int>(over(a->rows_k, keys_dkv(r.d)));
+    r.tiles = tiles_k;
     rc = launch_status("fewbit_attn_bwd", start_dkv(r, bf16, static_cast<unsigned>(k_groups), st));
   }
-  return rc;
+  const bool join_q = g.parts > 1 && a->rows_q > 0, join_k = g.parts_dkv > 1 && a->rows_k > 0;
+  if (rc != FEWBIT_OK || (!join_q && !join_k)) return rc;
+  r.tiles = tiles_q;
+  const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(keys_dkv(r.d) * r.d / 4, kThreads);
+  const int64_t joins_q = join_q ? g.q_places * r.hkv * share_q : 0, joins_k = join_k ? g.k_places * r.hkv * share_k : 0;
+  if (!fits_launch(joins_q + joins_k)) return FEWBIT_E_INVALID;
+  return launch_status("fewbit_attn_bwd",
+                       launch(bf16 ? attn_sums_kernel<FEWBIT_BF16> : attn_sums_kernel<FEWBIT_F16>, dim3(static_cast<unsigned>(joins_q + joins_k)),
+                              kThreads, st, r, divisor(static_cast<int>(share_q)), divisor(static_cast<int>(share_k)), static_cast<int>(joins_q),
+                              static_cast<int>(keys_dkv(r.d)), tiles_k));
 }

@@ -170,6 +170,31 @@ def test_packed(dtype, lens, extra, hq, hkv, d, causal, window):
         assert not x[at:].any()
 
 
+# few workgroups and long walks: the walks are divided and joined, forward, dQ and dK with dV
+@pytest.mark.parametrize("dtype,b,sq,sk,hq,hkv,d,causal,window,k_len", [
+    (BF16, 1, 700, 1500, 2, 1, 128, False, 0, None), (F16, 1, 1500, 1500, 1, 1, 64, True, 0, None),
+    (BF16, 2, 1400, 650, 2, 2, 80, True, 0, None), (F16, 1, 1900, 1999, 1, 1, 40, True, 700, None),
+    (BF16, 4, 900, 1100, 3, 1, 128, False, 0, (1100, 0, 1, 64)), (F16, 3, 333, 1777, 2, 1, 72, True, 0, (1000, 300, 5)),
+    (BF16, 1, 128, 2047, 8, 8, 128, True, 1200, None)])
+def test_walks_in_parts(dtype, b, sq, sk, hq, hkv, d, causal, window, k_len):
+    check(*make(dtype, b, sq, sk, hq, hkv, d), causal=causal, window=window, k_len=k_len)
+
+
+@pytest.mark.parametrize("dtype,causal,d", [(BF16, True, 128), (F16, False, 64)])
+def test_walks_in_parts_packed(dtype, causal, d):
+    lens = (1700, 0, 1, 900, 64, 65)
+    q, k, v, do = make(dtype, 1, sum(lens), sum(lens), 2, 1, d, packed=True)
+    cu = torch.tensor([sum(lens[:i]) for i in range(len(lens) + 1)], dtype=torch.int32, device="cuda")
+    out, lse = P.attention_fwd(q, k, v, cu_q=cu, cu_k=cu, causal=causal)
+    grads = P.attention_bwd(do, q, k, v, out, lse, cu_q=cu, cu_k=cu, causal=causal)
+    for i in range(len(lens)):
+        at = slice(int(cu[i]), int(cu[i + 1]))
+        ref, want = reference(q[at], k[at], v[at], do[at], causal, 0, 1 / math.sqrt(d))
+        assert torch.allclose(lse[:, at].double(), want, rtol=1e-5, atol=1e-5)
+        for x, n in zip((out, *grads), ("out", "dq", "dk", "dv")):
+            near(x[at], ref[n], f"{n} of {i}")
+
+
 def test_packed_with_other_keys():
     """Queries and keys of different lengths: some sequences have no keys, or no queries."""
     nq, nk = (10, 0, 70, 3, 200), (64, 5, 0, 300, 130)
