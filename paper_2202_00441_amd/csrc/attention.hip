@@ -65,7 +65,7 @@ struct Args {
   int batch, hq, hkv, g, d;           // g: query heads to a key head
   int causal, window;
   float scale;
-  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads;
+  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads, by_unit_rows;
   int tiles;                          // of a sequence (packed: places for tiles of all)
   int shares, unit_rows;              // split forward: workgroups of a key head, rows of a unit
   int parts, parts_dkv;               // of a workgroup's walk (forward or dQ; dK and dV)
@@ -816,43 +816,63 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
 }
 
 // Rows of units that several shares worked on: out = sum of their outputs, each by its
-// weight exp(lse_share - lse); a wave takes a row, two elements a lane.
+// weight exp(lse_share - lse).  A workgroup takes a row, each wave every fourth share, four
+// at a time so that their loads are on their way together, two elements a lane.
+constexpr int kSharesTurn = 4;
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
   using T = typename Mma<DT>::T;
+  __shared__ float2 sums[kWaves][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t at = static_cast<int64_t>(blockIdx.x) * kWaves + wave;       // unit, key head, row of 32
-  const int unit = static_cast<int>(at / (a.unit_rows * a.hkv)), rest = static_cast<int>(at % (a.unit_rows * a.hkv));
-  if (unit >= a.batch * a.tiles) return;
+  const int rest = a.by_unit_rows.divide(blockIdx.x), of = static_cast<int>(blockIdx.x) - rest * a.unit_rows;
+  const int unit = a.by_hkv.divide(rest), hk = rest - unit * a.hkv;
   const Unit u = unit_of(a, unit);
-  const int hk = rest / a.unit_rows, row = u.first + rest % a.unit_rows;
+  const int row = u.first + of;
   if (row >= u.rows) return;
   const Line line = line_of(a, unit);
-  const int first = line.before / line.share, last = (line.before + u.passes - 1) / line.share;
-  if (first == last) return;
+  const int first = line.before / line.share, n = (line.before + u.passes - 1) / line.share - first + 1;
+  if (n == 1) return;
   const int64_t step = static_cast<int64_t>(a.hkv) * a.unit_rows;
-  const int64_t part = (static_cast<int64_t>(first + unit) * a.hkv + hk) * a.unit_rows + rest % a.unit_rows;
+  const int64_t part = (static_cast<int64_t>(first + unit) * a.hkv + hk) * a.unit_rows + of;
   float most = -INFINITY;
-  for (int i = lane; i <= last - first; i += kWave) most = fmaxf(most, a.part_lse[part + i * step]);
+  for (int i = lane; i < n; i += kWave) most = fmaxf(most, a.part_lse[part + i * step]);
   most = across<6>(most, [](float x, float y) { return fmaxf(x, y); });
   const float base = most == -INFINITY ? 0.0f : most;
-  float sum = 0.0f, o0 = 0.0f, o1 = 0.0f;
-#pragma unroll 4
-  for (int i = 0; i <= last - first; ++i) {
-    const float w = __builtin_amdgcn_exp2f((a.part_lse[part + i * step] - base) * kLog2e);
-    sum += w;
-    if (2 * lane < a.d) {
-      const float* o = a.part_o + (part + i * step) * a.d + 2 * lane;
-      o0 += w * o[0];
-      o1 += w * o[1];
+  const float* o = a.part_o + part * a.d + (2 * lane < a.d ? 2 * lane : 0);
+  float sum = 0.0f;
+  float2 x{0.0f, 0.0f};
+  for (int i0 = 0; i0 < n; i0 += kWave) {
+    const float weight = i0 + lane < n ? __builtin_amdgcn_exp2f((a.part_lse[part + (i0 + lane) * step] - base) * kLog2e) : 0.0f;
+    sum += weight;
+    for (int i1 = wave; i1 < min(n - i0, kWave); i1 += kWaves * kSharesTurn) {
+      float2 y[kSharesTurn];
+#pragma unroll
+      for (int k = 0; k < kSharesTurn; ++k) y[k] = *reinterpret_cast<const float2*>(o + min(i0 + i1 + k * kWaves, n - 1) * step * a.d);
+#pragma unroll
+      for (int k = 0; k < kSharesTurn; ++k) {
+        const int i = i1 + k * kWaves;
+        if (i0 + i >= n || i >= kWave) break;
+        const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, weight), i));
+        x.x += w * y[k].x;
+        x.y += w * y[k].y;
+      }
     }
   }
+  sum = across<6>(sum, [](float x, float y) { return x + y; });
+  sums[wave][lane] = x;
+  __syncthreads();
+  if (wave != 0) return;
+#pragma unroll
+  for (int w = 1; w < kWaves; ++w) {
+    x.x += sums[w][lane].x;
+    x.y += sums[w][lane].y;
+  }
   const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-  const int pos = row / a.g, head = hk * a.g + row % a.g;
+  const int pos = a.by_g.divide(row), head = hk * a.g + row - pos * a.g;
   if (2 * lane < a.d) {
     T* out = static_cast<T*>(a.o) + ((u.s.b * a.rows_q + pos) * a.hq + head) * a.d + 2 * lane;
-    out[0] = static_cast<T>(o0 * inverse);
-    out[1] = static_cast<T>(o1 * inverse);
+    out[0] = static_cast<T>(x.x * inverse);
+    out[1] = static_cast<T>(x.y * inverse);
   }
   if (lane == 0) a.lse[(u.s.b * a.hq + head) * a.rows_q + pos] = sum == 0.0f ? -INFINITY : base + logf(sum);
 }
@@ -1292,8 +1312,14 @@ int64_t parts_of(int64_t groups, int64_t passes, int64_t cus, bool uneven) {
   return parts > 1 && passes - over(passes, parts) >= 8 ? parts : 1;
 }
 
-// Runs of 64 keys where two of them and their gradients fit a wave's registers, else 32.
-int64_t keys_dkv(int d) { return kPairs * (d <= 64 ? 64 : 32); }
+// Keys of a workgroup of the kernel for dK and dV: four runs of 64 where two of 32 and
+// their gradients fit a wave's registers and that leaves every second CU a workgroup, else
+// of 32 (3 packed sequences of 465 on average, 16 heads of 64, causal, forward and
+// backward, 96 workgroups of 256 keys: 59 us, of 128: 50 us).
+int64_t keys_dkv(const fewbit_attn* a) {
+  const int64_t most = kPairs * 64;
+  return a->head_dim <= 64 && 2 * places_of(a, a->rows_k, most) * a->heads_kv > device_cus() ? most : most / 2;
+}
 
 // Workgroups of the kernels, and parts of their walks.
 struct Grid {
@@ -1301,12 +1327,12 @@ struct Grid {
 };
 Grid grid_of(const fewbit_attn* a, bool back) {
   const int64_t g = a->heads_q / a->heads_kv, cus = device_cus();
-  Grid r{places_of(a, a->rows_q * g, kRowsGroup), places_of(a, a->rows_k, keys_dkv(a->head_dim)), 1, 1};
+  Grid r{places_of(a, a->rows_q * g, kRowsGroup), places_of(a, a->rows_k, keys_dkv(a)), 1, 1};
   const int64_t seqs = a->cu_q ? std::max<int64_t>(a->batch, 1) : 1;              // packed: lengths are not known here
   const int64_t keys = a->rows_k / seqs, rows = a->rows_q * g / seqs;
   const bool uneven = a->causal && !a->window && 2 * a->rows_q > a->rows_k;
   const int64_t seen = a->window ? std::min<int64_t>(keys, int64_t{a->window} + kRowsGroup / g) : keys;
-  const int64_t seers = a->window ? std::min(rows, (a->window + keys_dkv(a->head_dim)) * g) : rows;
+  const int64_t seers = a->window ? std::min(rows, (a->window + keys_dkv(a)) * g) : rows;
   r.parts = parts_of(r.q_places * a->heads_kv, over(seen, kKeys), cus, uneven);
   if (back) r.parts_dkv = parts_of(r.k_places * a->heads_kv, over(seers, kRowsPass), cus, uneven);
   return r;
@@ -1357,9 +1383,9 @@ hipError_t start_split(const Args& r, bool bf16, unsigned groups, hipStream_t st
                    : launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 128, ONCE> : attn_split_kernel<FEWBIT_F16, 128, ONCE>, dim3(groups), kThreads, st, r);
 }
 
+template <int D, int SUBS>
 hipError_t start_dkv(const Args& r, bool bf16, unsigned groups, hipStream_t st) {
-  return r.d <= 64 ? launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 64, 2> : attn_dkv_kernel<FEWBIT_F16, 64, 2>, dim3(groups), kThreadsPairs, st, r)
-                   : launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, 128, 1> : attn_dkv_kernel<FEWBIT_F16, 128, 1>, dim3(groups), kThreadsPairs, st, r);
+  return launch(bf16 ? attn_dkv_kernel<FEWBIT_BF16, D, SUBS> : attn_dkv_kernel<FEWBIT_F16, D, SUBS>, dim3(groups), kThreadsPairs, st, r);
 }
 
 }  // namespace
@@ -1424,8 +1450,9 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   const int64_t units = r.tiles * a->batch;
   r.part_o = static_cast<float*>(workspace);
   r.unit_rows = static_cast<int>(unit_rows(a));
+  r.by_unit_rows = divisor(r.unit_rows);
   r.part_lse = r.part_o + (r.shares + units) * r.hkv * r.unit_rows * r.d;
-  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = over(units * r.hkv * r.unit_rows, kWaves);
+  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = units * r.hkv * r.unit_rows;
   if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
   rc = launch_status("fewbit_attn_fwd", r.tiles == 1 ? start_split<true>(r, bf16, static_cast<unsigned>(groups), st)
                                                      : start_split<false>(r, bf16, static_cast<unsigned>(groups), st));
@@ -1474,7 +1501,7 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   r.by_parts_dkv = divisor(r.parts_dkv);
   r.part_dq = r.stats + 2 * r.stats_delta;
   r.part_dkv = r.part_dq + (g.parts > 1 ? g.parts * rows_all * r.d : 0);
-  const int tiles_q = static_cast<int>(over(rows, kRowsGroup)), tiles_k = static_cast<int>(over(a->rows_k, keys_dkv(r.d)));
+  const int tiles_q = static_cast<int>(over(rows, kRowsGroup)), group = static_cast<int>(keys_dkv(a)), tiles_k = static_cast<int>(over(a->rows_k, group));
   if (a->rows_q > 0) {
     r.tiles = tiles_q;
     rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dq_kernel, r, q_groups, st));
@@ -1482,16 +1509,17 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   }
   if (a->rows_k > 0) {
     r.tiles = tiles_k;
-    rc = launch_status("fewbit_attn_bwd", start_dkv(r, bf16, static_cast<unsigned>(k_groups), st));
+    const auto start = r.d > 64 ? start_dkv<128, 1> : group == kPairs * 64 ? start_dkv<64, 2> : start_dkv<64, 1>;
+    rc = launch_status("fewbit_attn_bwd", start(r, bf16, static_cast<unsigned>(k_groups), st));
   }
   const bool join_q = g.parts > 1 && a->rows_q > 0, join_k = g.parts_dkv > 1 && a->rows_k > 0;
   if (rc != FEWBIT_OK || (!join_q && !join_k)) return rc;
   r.tiles = tiles_q;
-  const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(keys_dkv(r.d) * r.d / 4, kThreads);
+  const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(int64_t{group} * r.d / 4, kThreads);
   const int64_t joins_q = join_q ? g.q_places * r.hkv * share_q : 0, joins_k = join_k ? g.k_places * r.hkv * share_k : 0;
   if (!fits_launch(joins_q + joins_k)) return FEWBIT_E_INVALID;
   return launch_status("fewbit_attn_bwd",
                        launch(bf16 ? attn_sums_kernel<FEWBIT_BF16> : attn_sums_kernel<FEWBIT_F16>, dim3(static_cast<unsigned>(joins_q + joins_k)),
                               kThreads, st, r, divisor(static_cast<int>(share_q)), divisor(static_cast<int>(share_k)), static_cast<int>(joins_q),
-                              static_cast<int>(keys_dkv(r.d)), tiles_k));
+                              group, tiles_k));
 }

@@ -170,6 +170,13 @@ def test_packed(dtype, lens, extra, hq, hkv, d, causal, window):
         assert not x[at:].any()
 
 
+# heads of at most 64 in many workgroups: the kernel for dK and dV takes 256 keys in each
+@pytest.mark.parametrize("dtype,b,sq,sk,hq,hkv,d,causal,window", [
+    (F16, 6, 65, 300, 24, 12, 64, True, 0), (BF16, 9, 70, 257, 16, 16, 40, False, 0), (BF16, 12, 190, 130, 12, 12, 64, True, 33)])
+def test_many_workgroups(dtype, b, sq, sk, hq, hkv, d, causal, window):
+    check(*make(dtype, b, sq, sk, hq, hkv, d), causal=causal, window=window)
+
+
 # few workgroups and long walks: the walks are divided and joined, forward, dQ and dK with dV
 @pytest.mark.parametrize("dtype,b,sq,sk,hq,hkv,d,causal,window,k_len", [
     (BF16, 1, 700, 1500, 2, 1, 128, False, 0, None), (F16, 1, 1500, 1500, 1, 1, 64, True, 0, None),
