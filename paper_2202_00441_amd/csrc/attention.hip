@@ -67,7 +67,7 @@ struct Args {
   float scale;
   Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads, by_unit_rows;
   int tiles;                          // of a sequence (packed: places for tiles of all)
-  int shares, unit_rows;              // split forward: workgroups of a key head, rows of a unit
+  int shares, share_least, unit_rows; // split forward: workgroups of a key head, passes of one at least, rows of a unit
   int parts, parts_dkv;               // of a workgroup's walk (forward or dQ; dK and dV)
 };
 
@@ -538,7 +538,6 @@ __device__ __forceinline__ void gather(const typename Mma<DT>::T* lv, const Colu
 }
 
 constexpr int kKeys = 64;                                           // keys of a pass
-constexpr int kPassesShare = 2;                                     // of a share of the split forward at least
 
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
@@ -659,7 +658,7 @@ __device__ __forceinline__ Line line_of(const Args& a, int stop) {
     l.all = __builtin_amdgcn_readfirstlane(all);
     l.before = __builtin_amdgcn_readfirstlane(before);
   }
-  l.share = max(kPassesShare, (l.all + a.shares - 1) / a.shares);
+  l.share = max(a.share_least, (l.all + a.shares - 1) / a.shares);
   return l;
 }
 
@@ -1281,24 +1280,30 @@ int64_t places_of(const fewbit_attn* a, int64_t rows, int64_t per) {
 // Rows of a unit of the forward that splits keys.
 int64_t unit_rows(const fewbit_attn* a) { return std::min<int64_t>(kRowsWave, a->rows_q * (a->heads_q / a->heads_kv)); }
 
-// Shares per key head of the forward that splits keys; 0: the kernel for many rows.
-int64_t shares_of(const fewbit_attn* a) {
+// The forward that splits keys: shares per key head (0: the kernel for many rows), passes
+// of a share at least, and whether no unit is in two shares, as far as the host can tell.
+struct Shares {
+  int64_t n, least;
+  bool whole;
+};
+Shares shares_of(const fewbit_attn* a) {
   const int64_t rows = a->rows_q * (a->heads_q / a->heads_kv);
-  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return 0;
+  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return {};
   const int64_t many = over(rows, kRowsGroup) * a->heads_kv * a->batch, cus = device_cus();
-  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return 0;
-  // as many workgroups as the chip holds at once, no more than there are passes
+  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return {};
   const int64_t units = over(rows, kRowsWave) * a->batch, passes = units * over(a->rows_k + 31, kKeysSplit);
-  if (units >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return 0;
-  return std::max<int64_t>(1, std::min((a->head_dim <= 64 ? 3 : 2) * cus / a->heads_kv, over(passes, kPassesShare)));
-}
-
-// Whether no unit is in two shares, as far as the host can tell.
-bool all_whole(const fewbit_attn* a, int64_t shares) {
-  if (a->k_len || a->rows_q * (a->heads_q / a->heads_kv) > kRowsWave) return false;
+  if (units >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return {};
+  // As many workgroups as the chip holds at once, or as it has CUs where that leaves one
+  // pass to each (one row on 16000 keys, 16 heads to 4: 20 us in 504 workgroups, 17 in 252);
+  // units of four passes are not worth a join (300 keys, 12 heads: 8.9 us joined, 7.1 whole).
   const int64_t lo = a->window ? std::max<int64_t>(0, a->rows_k - a->rows_q + 1 - a->window) / 32 * 32 : 0;
-  const int64_t each = std::max<int64_t>(1, over(a->rows_k - lo, kKeysSplit));
-  return std::max<int64_t>(kPassesShare, over(each * a->batch, shares)) % each == 0;
+  const int64_t each = std::max<int64_t>(1, over(a->rows_k - lo, kKeysSplit));         // passes of the last rows' unit
+  const auto per = [&](int64_t groups) { return over(passes, std::max<int64_t>(1, groups / a->heads_kv)); };
+  Shares r;
+  r.least = std::max(std::min<int64_t>(2, per(cus)), each <= 4 ? each : 1);
+  r.n = over(passes, std::max(r.least, per((a->head_dim <= 64 ? 3 : 2) * cus)));
+  r.whole = rows <= kRowsWave && !a->k_len && std::max(r.least, over(each * a->batch, r.n)) % each == 0;
+  return r;
 }
 
 // Parts of every workgroup's walk of `passes` passes at most: as many as give every CU a
@@ -1400,7 +1405,7 @@ extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward)
     return (2 * rounded(rows) + (g.parts > 1 ? g.parts * rows * a->head_dim : 0) + (g.parts_dkv > 1 ? g.parts_dkv * keys * 2 * a->head_dim : 0)) *
            static_cast<int64_t>(sizeof(float));
   }
-  const int64_t shares = shares_of(a), units = over(a->rows_q * (a->heads_q / a->heads_kv), kRowsWave) * a->batch;
+  const int64_t shares = shares_of(a).n, units = over(a->rows_q * (a->heads_q / a->heads_kv), kRowsWave) * a->batch;
   const int64_t left = shares > 0 ? (shares + units) * a->heads_kv * unit_rows(a) : g.parts > 1 ? g.parts * rows : 0;
   return left * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float));
 }
@@ -1429,7 +1434,9 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.o = out;
   r.lse = lse;
   const int64_t rows = a->rows_q * r.g;
-  r.shares = static_cast<int>(shares_of(a));
+  const Shares shares = shares_of(a);
+  r.shares = static_cast<int>(shares.n);
+  r.share_least = static_cast<int>(shares.least);
   if (r.shares == 0) {
     const Grid g = grid_of(a, false);
     r.tiles = static_cast<int>(over(rows, kRowsGroup));
@@ -1456,7 +1463,7 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
   rc = launch_status("fewbit_attn_fwd", r.tiles == 1 ? start_split<true>(r, bf16, static_cast<unsigned>(groups), st)
                                                      : start_split<false>(r, bf16, static_cast<unsigned>(groups), st));
-  if (rc != FEWBIT_OK || all_whole(a, r.shares)) return rc;
+  if (rc != FEWBIT_OK || shares.whole) return rc;
   return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_join_kernel<FEWBIT_BF16> : attn_join_kernel<FEWBIT_F16>,
                                                  dim3(static_cast<unsigned>(joins)), kThreads, st, r));
 }
