@@ -65,9 +65,10 @@ struct Args {
   int batch, hq, hkv, g, d;           // g: query heads to a key head
   int causal, window;
   float scale;
-  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads, by_unit_rows;
+  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads, by_rows;
   int tiles;                          // of a sequence (packed: places for tiles of all)
-  int shares, share_least, unit_rows; // split forward: workgroups of a key head, passes of one at least, rows of a unit
+  int rows;                           // split forward: of a sequence and key head
+  int shares, share_least;            // split forward: workgroups of a key head, passes of one at least
   int parts, parts_dkv;               // of a workgroup's walk (forward or dQ; dK and dV)
 };
 
@@ -208,7 +209,7 @@ __device__ __forceinline__ const T* uniform(const T* p) {
 // which chunk of its row a lane asks for.  Rows past the last are read as the last,
 // chunks past head_dim as the first: what multiplies them is 0 (masked scores; the
 // other operand's elements past head_dim) or is not stored.
-// POLICY: cache policy of the loads, 2 for what is read once (non-temporal).
+// POLICY: cache policy of the loads, kNt for what is read once.
 template <int DT, int D, int ROWS, int WAVES, int POLICY = 0>
 struct Stage {
   using T = typename Mma<DT>::T;
@@ -234,11 +235,12 @@ struct Stage {
     for (int j = 0; j < kLoads; ++j) load(at(row + row_of(j)) + chunk[j % kKinds], lds, j);
   }
   // The same for rows `stride` apart from `base` on (the same for all lanes), at most
-  // kNear: the address is a scalar and a lane's offset, which is there already.
-  __device__ __forceinline__ void issue(T* lds, const T* base, int64_t stride, const uint32_t (&offset)[kKinds]) const {
+  // kNear: the address is a scalar and a lane's offset, its row's and its chunk's.
+  __device__ __forceinline__ void issue(T* lds, const T* base, int64_t stride, uint32_t apart) const {
+    asm volatile("" : "+v"(apart));             // the sums are not kept in registers
 #pragma unroll
     for (int j = 0; j < kLoads; ++j)
-      load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(uniform(base + row_of(j) * stride)) + offset[j % kKinds]), lds, j);
+      load(reinterpret_cast<const T*>(reinterpret_cast<const char*>(uniform(base + row_of(j) * stride)) + (apart + chunk[j % kKinds] * 2)), lds, j);
   }
   // The same with an offset of its own for every load.
   __device__ __forceinline__ void issue(T* lds, const T* base, const uint32_t (&offset)[kLoads]) const {
@@ -249,10 +251,6 @@ struct Stage {
   __device__ __forceinline__ void offsets(F at, uint32_t (&offset)[kLoads]) const {
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) offset[j] = static_cast<uint32_t>(at(row + row_of(j)) + chunk[j % kKinds]) * 2;
-  }
-  __device__ __forceinline__ void offsets(int64_t stride, uint32_t (&offset)[kKinds]) const {
-#pragma unroll
-    for (int j = 0; j < kKinds; ++j) offset[j] = static_cast<uint32_t>(row * static_cast<int>(stride) + chunk[j]) * 2;
   }
 
  private:
@@ -272,14 +270,12 @@ struct Rows {
   int64_t stride;
   int last;             // the last row there is
   bool near;
-  uint32_t offset[S::kKinds];
+  uint32_t apart;       // bytes between the first row and this lane's of a load
   __device__ __forceinline__ Rows(const S& stage, const T* base_, int64_t stride_, int last_)
-      : base(base_), stride(stride_), last(last_), near(stride_ < kNear) {
-    stage.offsets(stride_, offset);
-  }
+      : base(base_), stride(stride_), last(last_), near(stride_ < kNear), apart(static_cast<uint32_t>(stage.row * static_cast<int>(stride_)) * 2) {}
   __device__ __forceinline__ void issue(const S& stage, T* lds, int first) const {
     if (near && first + ROWS - 1 <= last)
-      stage.issue(lds, base + first * stride, stride, offset);
+      stage.issue(lds, base + first * stride, stride, apart);
     else
       stage.issue(lds, [&](int i) { return base + min(first + i, last) * stride; });
   }
@@ -599,51 +595,49 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   }
 }
 
-// Few rows over many keys (single tokens over a cache).  Work is cut into units of 32
-// rows of one sequence and key head, and the units' passes of 128 keys, all in one line,
-// into equal shares, one to a workgroup: whatever the lengths of the caches, all
-// workgroups end at the same time.  A workgroup's waves take different keys of each pass
-// and add their results up at the end of the unit, or of the share; what belongs to a
-// unit that is not all in one share is left in the workspace and added by a second
-// kernel.  Share w and unit u meet at most once, and of all meetings in line each has
-// the next w or the next u: w + u numbers them.
+// Few rows over many keys (single tokens over a cache): a unit is a sequence and key head
+// of at most 32 rows, and its keys are taken in passes of 128.  The passes of all
+// sequences, in one line, are cut into equal shares, one to a workgroup: whatever the
+// lengths of the caches, all workgroups end at the same time.  A workgroup's waves take
+// different keys of each pass and add their results up at the end of the unit, or of the
+// share; what belongs to a unit that is not all in one share is left in the workspace and
+// added by a second kernel.  Share w and unit u meet at most once, and of all meetings in
+// line each has the next w or the next u: w + u numbers them.
 constexpr int kKeysSplit = 32 * kWaves;
 
 // Unit `unit`: its sequence, and the keys that its rows see, from a multiple of 32 on.
 struct Unit {
   Seq s;
-  int first, rows;      // of its rows, and of all rows of the sequence
+  int rows;
   Range keys;
   int passes;           // at least one
 };
 __device__ __forceinline__ Unit unit_of(const Args& a, int unit) {
   Unit u;
-  const int b = a.tiles == 1 ? unit : unit / a.tiles;
-  u.s.b = b;
+  u.s.b = unit;
   u.s.q0 = u.s.k0 = 0;
   u.s.nq = static_cast<int>(a.rows_q);
-  u.s.nk = a.k_len ? clamped(a.k_len[u.s.b], a.rows_k) : static_cast<int>(a.rows_k);
+  u.s.nk = a.k_len ? clamped(a.k_len[unit], a.rows_k) : static_cast<int>(a.rows_k);
   u.rows = u.s.nq * a.g;
-  u.first = (unit - b * a.tiles) * kRowsWave;
-  u.keys.lo = keys_of(a, u.s, a.by_g.divide(u.first)).lo / 32 * 32;
-  u.keys.hi = max(u.keys.lo, keys_of(a, u.s, a.by_g.divide(min(u.first + kRowsWave, u.rows) - 1)).hi);
+  u.keys.lo = keys_of(a, u.s, 0).lo / 32 * 32;
+  u.keys.hi = max(u.keys.lo, keys_of(a, u.s, u.s.nq - 1).hi);
   u.passes = max(1, (u.keys.hi - u.keys.lo + kKeysSplit - 1) / kKeysSplit);
   return u;
 }
 
 // All units' passes in line: passes of a share, and of all units, and those before unit
-// `stop`.  Units are alike where a sequence is one unit and none is shorter.
+// `stop`.  Units are alike where no sequence is shorter.
 struct Line {
   int share, all, before;
 };
 __device__ __forceinline__ Line line_of(const Args& a, int stop) {
   Line l;
-  if (!a.k_len && a.tiles == 1) {
+  if (!a.k_len) {
     const int each = unit_of(a, 0).passes;
     l.all = each * a.batch;
     l.before = each * stop;
   } else {
-    const int lane = threadIdx.x % kWave, units = a.batch * a.tiles;
+    const int lane = threadIdx.x % kWave, units = a.batch;
     int all = 0, before = 0;
     for (int u = lane; u < units; u += kWave) {
       const int n = unit_of(a, u).passes;
@@ -664,12 +658,12 @@ __device__ __forceinline__ Line line_of(const Args& a, int stop) {
 
 // The unit that pass `at` of the line is in, and which of its passes it is.
 __device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
-  if (!a.k_len && a.tiles == 1) {
+  if (!a.k_len) {
     const int each = unit_of(a, 0).passes, unit = at / each;
     pass = at - unit * each;
     return unit;
   }
-  const int lane = threadIdx.x % kWave, units = a.batch * a.tiles;
+  const int lane = threadIdx.x % kWave, units = a.batch;
   int before = 0;
   for (int u0 = 0; u0 < units; u0 += kWave) {
     const int own = u0 + lane < units ? unit_of(a, u0 + lane).passes : 0;
@@ -691,9 +685,9 @@ __device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
   return units;
 }
 
-// ONCE: all rows of a sequence are one unit, so keys are read once and not kept in the
-// caches (64 caches of 8192 keys, 16 heads to 4: 200 -> 177 us).
-template <int DT, int D, bool ONCE>
+// Keys are read once and not kept in the caches (64 caches of 8192 keys, 16 heads to 4:
+// 177 us, else 200).
+template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   __shared__ __attribute__((aligned(16))) T lk[kWaves][32 * D], lv[kWaves][32 * D];
@@ -720,12 +714,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     const auto mine = [&]() __attribute__((always_inline)) {
       int l = lane;
       asm volatile("" : "+v"(l));
-      const int row = u.first + l % 32, some = min(row, u.rows - 1), pos = a.by_g.divide(some);
+      const int row = l % 32, some = min(row, u.rows - 1), pos = a.by_g.divide(some);
       return Mine{pos, hk * a.g + some - pos * a.g, row < u.rows};
     };
     const auto [pos, head, there] = mine();
     const Range own = keys_of(a, s, pos);
-    const Range every{keys_of(a, s, a.by_g.divide(min(u.first + kRowsWave, u.rows) - 1)).lo, keys_of(a, s, a.by_g.divide(u.first)).hi};
+    const Range every{keys_of(a, s, s.nq - 1).lo, keys_of(a, s, 0).hi};
     Range all;
     all.lo = u.keys.lo + pass * kKeysSplit;
     all.hi = min(u.keys.hi, all.lo + passes * kKeysSplit);
@@ -735,9 +729,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
       load_rows<DT, D>(static_cast<const T*>(a.q) + s.b * a.qs[0] + pos * a.qs[1] + head * a.qs[2], a.d, q);
       const T* kb = static_cast<const T*>(a.k) + s.b * a.ks[0] + hk * a.ks[2];
       const T* vb = static_cast<const T*>(a.v) + s.b * a.vs[0] + hk * a.vs[2];
-      constexpr int kPolicy = ONCE ? 2 : 0;
-      const Stage<DT, D, 32, 1, kPolicy> stage(a.d, 0);
-      const Rows<DT, D, 32, 1, kPolicy> keys(stage, kb, a.ks[1], all.hi - 1), values(stage, vb, a.vs[1], all.hi - 1);
+      const Stage<DT, D, 32, 1, kNt> stage(a.d, 0);
+      const Rows<DT, D, 32, 1, kNt> keys(stage, kb, a.ks[1], all.hi - 1), values(stage, vb, a.vs[1], all.hi - 1);
       const RowReader<DT, D> rr;
       const ColumnReader<DT, D> cr;
       // Each wave has buffers of its own: while it works on keys the next keys, and while
@@ -788,7 +781,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
     __syncthreads();
     const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
     const float lse = sum == 0.0f ? -INFINITY : most * a.scale + logf(sum);
-    const int64_t part = (static_cast<int64_t>(share + unit) * a.hkv + hk) * a.unit_rows + lane % 32;
+    const int64_t part = (static_cast<int64_t>(share + unit) * a.hkv + hk) * a.rows + lane % 32;
     if (there2 && wave == 0 && lane < 32) (whole ? a.lse[(s.b * a.hq + head2) * a.rows_q + pos2] : a.part_lse[part]) = lse;
 #pragma unroll
     for (int t = 0; t < D / 32; ++t) {
@@ -823,16 +816,15 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
   using T = typename Mma<DT>::T;
   __shared__ float2 sums[kWaves][kWave];
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int rest = a.by_unit_rows.divide(blockIdx.x), of = static_cast<int>(blockIdx.x) - rest * a.unit_rows;
+  const int rest = a.by_rows.divide(blockIdx.x), of = static_cast<int>(blockIdx.x) - rest * a.rows;
   const int unit = a.by_hkv.divide(rest), hk = rest - unit * a.hkv;
   const Unit u = unit_of(a, unit);
-  const int row = u.first + of;
-  if (row >= u.rows) return;
+  if (of >= u.rows) return;
   const Line line = line_of(a, unit);
   const int first = line.before / line.share, n = (line.before + u.passes - 1) / line.share - first + 1;
   if (n == 1) return;
-  const int64_t step = static_cast<int64_t>(a.hkv) * a.unit_rows;
-  const int64_t part = (static_cast<int64_t>(first + unit) * a.hkv + hk) * a.unit_rows + of;
+  const int64_t step = static_cast<int64_t>(a.hkv) * a.rows;
+  const int64_t part = (static_cast<int64_t>(first + unit) * a.hkv + hk) * a.rows + of;
   float most = -INFINITY;
   for (int i = lane; i < n; i += kWave) most = fmaxf(most, a.part_lse[part + i * step]);
   most = across<6>(most, [](float x, float y) { return fmaxf(x, y); });
@@ -867,7 +859,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
     x.y += sums[w][lane].y;
   }
   const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
-  const int pos = a.by_g.divide(row), head = hk * a.g + row - pos * a.g;
+  const int pos = a.by_g.divide(of), head = hk * a.g + of - pos * a.g;
   if (2 * lane < a.d) {
     T* out = static_cast<T*>(a.o) + ((u.s.b * a.rows_q + pos) * a.hq + head) * a.d + 2 * lane;
     out[0] = static_cast<T>(x.x * inverse);
@@ -877,8 +869,8 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
 }
 
 // The same for the parts of a workgroup's walk over keys: a thread takes four elements of
-// a row; kJoins workgroups share the rows of one.
-constexpr int kPartsMost = 8;
+// a row, with the loads of four parts on their way together.
+constexpr int kPartsMost = 16, kPartsTurn = 4;
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_parts_kernel(const Args a, Divisor by_joins) {
   using T = typename Mma<DT>::T;
@@ -894,22 +886,24 @@ __global__ __launch_bounds__(kThreads) void attn_parts_kernel(const Args a, Divi
   const int pos = a.by_g.divide(row), head = hk * a.g + row - pos * a.g;
   const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head, step = rows_all(a);
   float lse[kPartsMost], most = -INFINITY, sum = 0.0f;
-  f32x4 parts[kPartsMost], o{};
 #pragma unroll
-  for (int k = 0; k < kPartsMost; ++k) {        // past the last: the last again, with weight 0
-    const int64_t from = min(k, used - 1) * step + at;
-    lse[k] = a.part_lse[from];
-    parts[k] = *reinterpret_cast<const f32x4*>(a.part_o + from * a.d + c);
-  }
+  for (int k = 0; k < kPartsMost; ++k) lse[k] = k < used ? a.part_lse[k * step + at] : -INFINITY;
 #pragma unroll
   for (int k = 0; k < kPartsMost; ++k) most = fmaxf(most, lse[k]);
   const float base = most == -INFINITY ? 0.0f : most;
+  f32x4 o{};
 #pragma unroll
-  for (int k = 0; k < kPartsMost; ++k) {
-    if (k >= used) break;
-    const float w = __builtin_amdgcn_exp2f((lse[k] - base) * kLog2e);
-    sum += w;
-    o += parts[k] * w;
+  for (int k0 = 0; k0 < kPartsMost; k0 += kPartsTurn) {
+    if (k0 >= used) break;
+    f32x4 parts[kPartsTurn];
+#pragma unroll
+    for (int k = 0; k < kPartsTurn; ++k) parts[k] = *reinterpret_cast<const f32x4*>(a.part_o + (min(k0 + k, used - 1) * step + at) * a.d + c);
+#pragma unroll
+    for (int k = 0; k < kPartsTurn; ++k) {
+      const float w = __builtin_amdgcn_exp2f((lse[k0 + k] - base) * kLog2e);
+      sum += w;
+      if (k0 + k < used) o += parts[k] * w;
+    }
   }
   const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
   *reinterpret_cast<typename Mma<DT>::V4*>(static_cast<T*>(a.o) + at * a.d + c) = __builtin_convertvector(o * inverse, typename Mma<DT>::V4);
@@ -1207,12 +1201,15 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
 // Sums of the parts of both kernels' walks, in their order, four elements a thread:
 // workgroups for rows, then workgroups for runs of `group` keys.
 __device__ __forceinline__ f32x4 sum_of(const float* parts, int64_t step, int used) {
-  f32x4 x[kPartsMost], sum{};
+  f32x4 sum{};
+  for (int k0 = 0; k0 < used; k0 += kPartsTurn) {
+    f32x4 x[kPartsTurn];
 #pragma unroll
-  for (int k = 0; k < kPartsMost; ++k) x[k] = *reinterpret_cast<const f32x4*>(parts + min(k, used - 1) * step);
+    for (int k = 0; k < kPartsTurn; ++k) x[k] = *reinterpret_cast<const f32x4*>(parts + min(k0 + k, used - 1) * step);
 #pragma unroll
-  for (int k = 0; k < kPartsMost; ++k)
-    if (k < used) sum += x[k];
+    for (int k = 0; k < kPartsTurn; ++k)
+      if (k0 + k < used) sum += x[k];
+  }
   return sum;
 }
 template <int DT>
@@ -1277,32 +1274,30 @@ int64_t places_of(const fewbit_attn* a, int64_t rows, int64_t per) {
   return a->cu_q ? over(rows, per) + a->batch + 1 : over(rows, per) * a->batch;
 }
 
-// Rows of a unit of the forward that splits keys.
-int64_t unit_rows(const fewbit_attn* a) { return std::min<int64_t>(kRowsWave, a->rows_q * (a->heads_q / a->heads_kv)); }
-
 // The forward that splits keys: shares per key head (0: the kernel for many rows), passes
 // of a share at least, and whether no unit is in two shares, as far as the host can tell.
+// It takes at most 32 rows to a sequence and key head.  One row on 64 caches of 8192 keys, 16
+// heads to 4: 105 us, the kernel for many rows 166; on 1 of 777, 12 heads: 10 and 10; but 16
+// rows on 8 of 4096, 16 heads to 4: 40 (32 rows at a time) and 21.
 struct Shares {
   int64_t n, least;
   bool whole;
 };
 Shares shares_of(const fewbit_attn* a) {
   const int64_t rows = a->rows_q * (a->heads_q / a->heads_kv);
-  if (a->cu_q || a->batch == 0 || rows == 0 || a->rows_k == 0) return {};
-  const int64_t many = over(rows, kRowsGroup) * a->heads_kv * a->batch, cus = device_cus();
-  if (rows > kRowsWave && (many >= cus / 2 || a->rows_k < 2048)) return {};
-  const int64_t units = over(rows, kRowsWave) * a->batch, passes = units * over(a->rows_k + 31, kKeysSplit);
-  if (units >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return {};
+  if (a->cu_q || a->batch == 0 || rows == 0 || rows > kRowsWave || a->rows_k == 0) return {};
+  const int64_t cus = device_cus(), passes = a->batch * over(a->rows_k + 31, kKeysSplit);
+  if (a->batch >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return {};
   // As many workgroups as the chip holds at once, or as it has CUs where that leaves one
   // pass to each (one row on 16000 keys, 16 heads to 4: 20 us in 504 workgroups, 17 in 252);
   // units of four passes are not worth a join (300 keys, 12 heads: 8.9 us joined, 7.1 whole).
   const int64_t lo = a->window ? std::max<int64_t>(0, a->rows_k - a->rows_q + 1 - a->window) / 32 * 32 : 0;
-  const int64_t each = std::max<int64_t>(1, over(a->rows_k - lo, kKeysSplit));         // passes of the last rows' unit
+  const int64_t each = std::max<int64_t>(1, over(a->rows_k - lo, kKeysSplit));         // passes of a unit
   const auto per = [&](int64_t groups) { return over(passes, std::max<int64_t>(1, groups / a->heads_kv)); };
   Shares r;
   r.least = std::max(std::min<int64_t>(2, per(cus)), each <= 4 ? each : 1);
   r.n = over(passes, std::max(r.least, per((a->head_dim <= 64 ? 3 : 2) * cus)));
-  r.whole = rows <= kRowsWave && !a->k_len && std::max(r.least, over(each * a->batch, r.n)) % each == 0;
+  r.whole = !a->k_len && std::max(r.least, over(each * a->batch, r.n)) % each == 0;
   return r;
 }
 
@@ -1382,10 +1377,9 @@ bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // 
                   : (bf16 ? launch(KERNEL<FEWBIT_BF16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)   \
                           : launch(KERNEL<FEWBIT_F16, 128>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)))
 
-template <bool ONCE>
 hipError_t start_split(const Args& r, bool bf16, unsigned groups, hipStream_t st) {
-  return r.d <= 64 ? launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 64, ONCE> : attn_split_kernel<FEWBIT_F16, 64, ONCE>, dim3(groups), kThreads, st, r)
-                   : launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 128, ONCE> : attn_split_kernel<FEWBIT_F16, 128, ONCE>, dim3(groups), kThreads, st, r);
+  return r.d <= 64 ? launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 64> : attn_split_kernel<FEWBIT_F16, 64>, dim3(groups), kThreads, st, r)
+                   : launch(bf16 ? attn_split_kernel<FEWBIT_BF16, 128> : attn_split_kernel<FEWBIT_F16, 128>, dim3(groups), kThreads, st, r);
 }
 
 template <int D, int SUBS>
@@ -1405,8 +1399,8 @@ extern "C" int64_t fewbit_attn_workspace(const fewbit_attn* a, int32_t backward)
     return (2 * rounded(rows) + (g.parts > 1 ? g.parts * rows * a->head_dim : 0) + (g.parts_dkv > 1 ? g.parts_dkv * keys * 2 * a->head_dim : 0)) *
            static_cast<int64_t>(sizeof(float));
   }
-  const int64_t shares = shares_of(a).n, units = over(a->rows_q * (a->heads_q / a->heads_kv), kRowsWave) * a->batch;
-  const int64_t left = shares > 0 ? (shares + units) * a->heads_kv * unit_rows(a) : g.parts > 1 ? g.parts * rows : 0;
+  const int64_t shares = shares_of(a).n, of = a->rows_q * (a->heads_q / a->heads_kv);
+  const int64_t left = shares > 0 ? (shares + a->batch) * a->heads_kv * of : g.parts > 1 ? g.parts * rows : 0;
   return left * (a->head_dim + 1) * static_cast<int64_t>(sizeof(float));
 }
 
@@ -1453,16 +1447,13 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
     return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_parts_kernel<FEWBIT_BF16> : attn_parts_kernel<FEWBIT_F16>,
                                                    dim3(static_cast<unsigned>(joins)), kThreads, st, r, divisor(static_cast<int>(share))));
   }
-  r.tiles = static_cast<int>(over(rows, kRowsWave));
-  const int64_t units = r.tiles * a->batch;
   r.part_o = static_cast<float*>(workspace);
-  r.unit_rows = static_cast<int>(unit_rows(a));
-  r.by_unit_rows = divisor(r.unit_rows);
-  r.part_lse = r.part_o + (r.shares + units) * r.hkv * r.unit_rows * r.d;
-  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = units * r.hkv * r.unit_rows;
+  r.rows = static_cast<int>(rows);
+  r.by_rows = divisor(r.rows);
+  r.part_lse = r.part_o + (r.shares + a->batch) * r.hkv * r.rows * r.d;
+  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = a->batch * r.hkv * r.rows;
   if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
-  rc = launch_status("fewbit_attn_fwd", r.tiles == 1 ? start_split<true>(r, bf16, static_cast<unsigned>(groups), st)
-                                                     : start_split<false>(r, bf16, static_cast<unsigned>(groups), st));
+  rc = launch_status("fewbit_attn_fwd", start_split(r, bf16, static_cast<unsigned>(groups), st));
   if (rc != FEWBIT_OK || shares.whole) return rc;
   return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_join_kernel<FEWBIT_BF16> : attn_join_kernel<FEWBIT_F16>,
                                                  dim3(static_cast<unsigned>(joins)), kThreads, st, r));

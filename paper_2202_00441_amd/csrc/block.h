@@ -69,9 +69,8 @@ __device__ __forceinline__ void store(T* p, const float (&x)[N]) {
 }
 
 // Streams: accesses relative to an address that is the same for the whole wave, through
-// buffer instructions, whose cache policy is explicit: 2 = nt (not kept in the caches),
-// 16 = sc1 (stores: written through the L2).
-constexpr int kNt = 2, kThrough = 16, kThroughNt = 18;
+// buffer instructions, whose cache policy is explicit: kNt is not kept in the caches.
+constexpr int kNt = 2;
 
 struct Stream {
   __amdgpu_buffer_rsrc_t r;
