@@ -15,8 +15,8 @@
 // Backward: with g the incoming gradient turned back, x the input, r = 1 /
 // sqrt(mean(x^2) + eps) and u = x r,
 //   dw = sum over rows of g u,   dx = r (g w - u mean(g w u)).
-// Lanes add dw up in registers over all their rows, workgroups in LDS, and a
-// second kernel adds the workgroups' sums, each in a fixed order.
+// Lanes add dw up in registers over all their rows, waves across lanes, workgroups in LDS,
+// and a second kernel adds the workgroups' sums, each in a fixed order.
 #include <algorithm>
 
 #include "block.h"
@@ -27,7 +27,6 @@ using namespace block;
 
 constexpr int kThreads = 256;
 constexpr int kN = 16;          // elements of a lane
-constexpr int kParts = 1024;    // workgroups of the backward at most: the rows the second kernel adds
 
 struct Side {
   const void* x;
@@ -48,9 +47,9 @@ struct Args {
   int64_t table_rows;
   Divisor tokens;
   int d, rot;
-  uint32_t first_k;     // forward: the first workgroup of the keys
+  uint32_t first_k;     // the first workgroup of the keys
   float eps;
-  float* parts;         // backward: [workgroups][2][head_dim]
+  float* parts;         // backward: [workgroups][head_dim]
 };
 
 // Where a lane's two chunks of eight elements begin in a row.
@@ -181,86 +180,94 @@ __global__ __launch_bounds__(kThreads) void qk_fwd_kernel(const Args a) {
   }
 }
 
+// The sum over a wave's groups of 2^LEVELS lanes, lane by lane.
+template <int LEVELS>
+__device__ __forceinline__ float group_sum(float x) {
+  if constexpr (LEVELS < 4) x += dpp<0x128 /* row_ror 8 */>(x);
+  if constexpr (LEVELS < 3) x += dpp<0x124 /* row_ror 4 */>(x);
+  const Two rows = halves16(x);
+  const Two both = halves32(rows.a + rows.b);
+  return both.a + both.b;
+}
+
 template <int DT, bool INTER, int LEVELS>
 __global__ __launch_bounds__(kThreads) void qk_bwd_kernel(const Args a) {
   using T = typename Store<DT>::type;
-  constexpr int kLanes = 1 << LEVELS, kGroups = kThreads / kLanes;
-  __shared__ float sums[kGroups][kLanes * kN];
-  const int lane = threadIdx.x % kLanes, group = threadIdx.x / kLanes;
+  constexpr int kLanes = 1 << LEVELS, kGroups = kThreads / kLanes, kWaves = kThreads / kWave;
+  __shared__ float sums[kWaves][kLanes * kN];
+  const int lane = threadIdx.x % kLanes;
   const Chunks at = chunks_of<INTER>(lane, a.d, a.rot);
-#pragma unroll 1
-  for (int kind = 0; kind < 2; ++kind) {
-    const Side& side = a.s[kind];
-    float w[kN] = {}, dw[kN] = {};
-    if (at.some && side.units > 0) load_row(static_cast<const T*>(side.w), at, w);
-    for (uint32_t place = blockIdx.x * kGroups + group; place < side.units; place += gridDim.x * kGroups) {
-      const int unit = static_cast<int>(place), token = side.shares.divide(unit), h = unit - token * static_cast<int>(side.shares.n);
-      const int b = a.tokens.divide(token), t = token - b * static_cast<int>(a.tokens.n);
-      Raw<T> rx = {}, rg = {};
-      if (at.some) {
-        rx.load(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at);
-        rg.load(static_cast<const T*>(side.dy) + b * side.ds[0] + t * side.ds[1] + h * side.ds[2], at);
-      }
-      float c[8], s[8];
-      angles(a, lane, at.turned, b, t, c, s);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) s[j] = -s[j];
-      float u[kN], g[kN];
-      rx.get(u);
-      rg.get(g);
-      if (at.turned) turn<INTER>(g, c, s);
-      float sum = 0.0f, dot = 0.0f;
-#pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        sum += u[i] * u[i];
-        dot += g[i] * w[i] * u[i];
-      }
-      const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
-      const float mean = row_sum<LEVELS>(dot) * r / a.d;
-#pragma unroll
-      for (int i = 0; i < kN; ++i) {
-        const float v = u[i] * r;
-        dw[i] += g[i] * v;
-        u[i] = r * (g[i] * w[i] - v * mean);
-      }
-      if (at.some) store_row(static_cast<T*>(side.y) + static_cast<int64_t>(unit) * a.d, at, u);
+  const bool keys = blockIdx.x >= a.first_k;
+  const Side& side = a.s[keys];
+  const uint32_t first = blockIdx.x - (keys ? a.first_k : 0), groups = keys ? gridDim.x - a.first_k : a.first_k;
+  float w[kN] = {}, dw[kN] = {};
+  if (at.some) load_row(static_cast<const T*>(side.w), at, w);
+  for (uint32_t place = first * kGroups + threadIdx.x / kLanes; place < side.units; place += groups * kGroups) {
+    const int unit = static_cast<int>(place), token = side.shares.divide(unit), h = unit - token * static_cast<int>(side.shares.n);
+    const int b = a.tokens.divide(token), t = token - b * static_cast<int>(a.tokens.n);
+    Raw<T> rx = {}, rg = {};
+    if (at.some) {
+      rx.load(static_cast<const T*>(side.x) + b * side.xs[0] + t * side.xs[1] + h * side.xs[2], at);
+      rg.load(static_cast<const T*>(side.dy) + b * side.ds[0] + t * side.ds[1] + h * side.ds[2], at);
     }
-    // the workgroup's sums: groups in pairs, then the next pairs
-    if (kind) __syncthreads();
+    float c[8], s[8];
+    angles(a, lane, at.turned, b, t, c, s);
 #pragma unroll
-    for (int i = 0; i < kN; ++i) sums[group][i * kLanes + lane] = dw[i];
-    for (int n = kGroups / 2; n > 0; n /= 2) {
-      __syncthreads();
-      for (int e = threadIdx.x; e < n * kLanes * kN; e += kThreads) {
-        const int g = e / (kLanes * kN), i = e % (kLanes * kN);
-        sums[g][i] += sums[g + n][i];
-      }
-    }
-    __syncthreads();
-    if (group == 0 && at.some) {
-      float* out = a.parts + (static_cast<int64_t>(blockIdx.x) * 2 + kind) * a.d;
+    for (int j = 0; j < 8; ++j) s[j] = -s[j];
+    float u[kN], g[kN];
+    rx.get(u);
+    rg.get(g);
+    if (at.turned) turn<INTER>(g, c, s);
+    float sum = 0.0f, dot = 0.0f;
 #pragma unroll
-      for (int i = 0; i < kN; ++i) out[i < 8 ? at.a + i : at.b + i - 8] = sums[0][i * kLanes + lane];
+    for (int i = 0; i < kN; ++i) {
+      sum += u[i] * u[i];
+      dot += g[i] * w[i] * u[i];
     }
+    const float r = 1.0f / sqrtf(row_sum<LEVELS>(sum) / a.d + a.eps);
+    const float mean = row_sum<LEVELS>(dot) * r / a.d;
+#pragma unroll
+    for (int i = 0; i < kN; ++i) {
+      const float v = u[i] * r;
+      dw[i] += g[i] * v;
+      u[i] = r * (g[i] * w[i] - v * mean);
+    }
+    if (at.some) store_row(static_cast<T*>(side.y) + static_cast<int64_t>(unit) * a.d, at, u);
   }
+#pragma unroll
+  for (int i = 0; i < kN; ++i) {
+    const float sum = group_sum<LEVELS>(dw[i]);
+    if (threadIdx.x % kWave < kLanes) sums[threadIdx.x / kWave][i * kLanes + lane] = sum;
+  }
+  __syncthreads();
+  if (threadIdx.x >= kLanes * kN || !at.some) return;
+  float sum = 0.0f;
+#pragma unroll
+  for (int i = 0; i < kWaves; ++i) sum += sums[i][threadIdx.x];
+  const int i = threadIdx.x / kLanes;
+  a.parts[static_cast<int64_t>(blockIdx.x) * a.d + (i < 8 ? at.a + i : at.b + i - 8)] = sum;
 }
 
-// The sum of `rows` rows of 2 * d floats: a workgroup takes 16 columns, 64 sums
-// of every 64th row each, then adds those in pairs.
+// The sums of the workgroups' rows of d floats, those of the queries and then those of the
+// keys: a workgroup takes 16 columns of one kind, 64 sums of every 64th row each, then adds
+// those in pairs.
 constexpr int kColumns = 16, kRows = 64;
-__global__ __launch_bounds__(kColumns* kRows) void qk_sum_kernel(const float* parts, int rows, int d, float* dq_w, float* dk_w) {
+__global__ __launch_bounds__(kColumns* kRows) void qk_sum_kernel(const float* parts, int rows_q, int rows_k, int d, float* dq_w, float* dk_w) {
   __shared__ float sums[kRows][kColumns];
-  const int col = blockIdx.x * kColumns + threadIdx.x % kColumns, row = threadIdx.x / kColumns;
+  const int first = blockIdx.x * kColumns, row = threadIdx.x / kColumns;
+  const bool keys = first >= d;
+  const int col = first - (keys ? d : 0) + threadIdx.x % kColumns, end = keys ? rows_q + rows_k : rows_q;
   float sum = 0.0f;
-  for (int r = row; r < rows; r += kRows) sum += parts[static_cast<int64_t>(r) * 2 * d + col];
+#pragma unroll 8
+  for (int r = (keys ? rows_q : 0) + row; r < end; r += kRows) sum += parts[static_cast<int64_t>(r) * d + col];
   sums[row][threadIdx.x % kColumns] = sum;
   for (int n = kRows / 2; n > 0; n /= 2) {
     __syncthreads();
     if (row < n) sums[row][threadIdx.x % kColumns] += sums[row + n][threadIdx.x % kColumns];
   }
   if (row == 0) {
-    float* out = col < d ? dq_w : dk_w;
-    if (out) out[col < d ? col : col - d] = sums[0][threadIdx.x];
+    float* out = keys ? dk_w : dq_w;
+    if (out) out[col] = sums[0][threadIdx.x];
   }
 }
 
@@ -337,11 +344,19 @@ Args args_of(const fewbit_qk* a, const float* cos, const float* sin, const int64
   return r;
 }
 
-// Workgroups of the backward: what the chip holds at once, four per CU (each
-// leaves a row for the second kernel).
-int64_t parts_of(const fewbit_qk* a, const Args& r) {
-  const int64_t most = std::min<int64_t>(kParts, 4 * static_cast<int64_t>(device_cus()));
-  return std::min(groups_of(a, std::max(r.s[0].units, r.s[1].units)), most);
+// Workgroups of the backward for the queries and for the keys: all take as many rows, and
+// there are at most as many as the chip holds at once, five per CU, for each leaves a row
+// for the second kernel.  (32768 tokens of 20 heads in bf16: 90 us; with four per CU 93, six
+// 102, eight 95.)
+struct Parts {
+  int64_t q, k;
+};
+Parts parts_of(const fewbit_qk* a, const Args& r) {
+  const int64_t q = groups_of(a, r.s[0].units), k = groups_of(a, r.s[1].units), most = 5 * static_cast<int64_t>(device_cus());
+  const auto over = [](int64_t n, int64_t by) { return (n + by - 1) / by; };
+  int64_t each = std::max<int64_t>(1, over(q + k, most));
+  if (over(q, each) + over(k, each) > most) ++each;
+  return {over(q, each), over(k, each)};
 }
 
 template <int DT, bool INTER, int LEVELS>
@@ -411,7 +426,8 @@ extern "C" int64_t fewbit_qk_workspace(const fewbit_qk* a) {
   const int rc = check(a);
   if (rc != FEWBIT_OK) return rc;
   if (nothing(a)) return 0;
-  return parts_of(a, args_of(a, nullptr, nullptr, nullptr, true)) * 2 * a->head_dim * static_cast<int64_t>(sizeof(float));
+  const Parts parts = parts_of(a, args_of(a, nullptr, nullptr, nullptr, true));
+  return (parts.q + parts.k) * a->head_dim * static_cast<int64_t>(sizeof(float));
 }
 
 extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void* dk_out, const void* q, const void* k,
@@ -436,7 +452,7 @@ extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void*
   rc = check_stream_device(static_cast<hipStream_t>(stream));
   if (rc != FEWBIT_OK) return rc;
   const hipStream_t s = static_cast<hipStream_t>(stream);
-  int64_t parts = 0;
+  Parts parts{0, 0};
   if (!none) {
     Args r = args_of(a, cos, sin, positions, true);
     r.s[0].x = q;
@@ -449,10 +465,11 @@ extern "C" int fewbit_qk_bwd(const fewbit_qk* a, const void* dq_out, const void*
     r.s[1].y = dk;
     r.parts = static_cast<float*>(workspace);
     parts = parts_of(a, r);
-    rc = launch_status("fewbit_qk_bwd", start(a, r, true, static_cast<unsigned>(parts), s));
+    r.first_k = static_cast<uint32_t>(parts.q);
+    rc = launch_status("fewbit_qk_bwd", start(a, r, true, static_cast<unsigned>(parts.q + parts.k), s));
     if (rc != FEWBIT_OK) return rc;
   }
   return launch_status("fewbit_qk_bwd", launch(qk_sum_kernel, dim3(2 * a->head_dim / kColumns), kColumns * kRows, s,
-                                               static_cast<const float*>(workspace), static_cast<int>(parts), a->head_dim,
-                                               dq_weight, dk_weight));
+                                               static_cast<const float*>(workspace), static_cast<int>(parts.q), static_cast<int>(parts.k),
+                                               a->head_dim, dq_weight, dk_weight));
 }

@@ -187,7 +187,7 @@ def test_qk_pointers_strides_and_workspace():
             assert qk_bwd(a, *p) == E_ALIGN, i
     assert qk_fwd(qk(q_stride=(5120, 516, 64))) == qk_bwd(qk(dk_stride=(5120, 512, 4))) == E_ALIGN
     need = LIB.fewbit_qk_workspace(C.byref(a))
-    assert need > 0 and need % (2 * 64 * 4) == 0
+    assert need > 0 and need % (64 * 4) == 0
     assert qk_bwd(a, work=None) == E_NULL and qk_bwd(a, size=need - 1) == E_INVALID
     assert qk_fwd(qk(tokens=0)) == qk_fwd(qk(batch=0)) == qk_bwd(qk(heads_q=0, heads_k=0), *[None] * 13) == OK
 
