@@ -911,10 +911,10 @@ __global__ __launch_bounds__(kThreads) void attn_parts_kernel(const Args a, Divi
 }
 
 // ---------------------------------------------------------------- backward
-// The kernel for dK and dV hands P over in the storage type.  In fp16 it hands over
-// 2^15 P, for which small probabilities keep all of their bits too.
-template <int DT>
-constexpr int kLift = DT == FEWBIT_F16 ? 15 : 0;
+// The kernel for dK and dV forms 2^15 P, which it hands over in fp16 whatever the storage
+// type: 11 bits, for small probabilities too (bf16's eight would be rounded a second time
+// in dS: dK's error 0.0030 of its norm instead of 0.0025).
+constexpr int kLift = 15;
 
 // With P from lse, delta_i = <dO_i, O_i>, dP = dO V^T and dS = P (dP - delta):
 //   dQ = scale dS K,  dK = scale dS^T Q,  dV = P^T dO.
@@ -958,8 +958,8 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   float lse = there ? a.lse[stat] : -INFINITY;
   lse = lse == -INFINITY ? INFINITY : lse * kLog2e;           // of an empty row no key is seen
   if (there && lane < 32 && part == 0) {
-    a.stats[stat] = lse - kLift<DT>;
-    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift<DT>);
+    a.stats[stat] = lse - kLift;
+    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift);
   }
 
   const Range own = keys_of(a, s, pos);
@@ -1035,7 +1035,8 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
     __attribute__((aligned(16))) float stats[2][kRowsPass];
   };
   __shared__ Buffer buf0, buf1, buf2;
-  __shared__ V8 handed[2][kPairs][SUBS][kRowsPass / 16][kWave];
+  using Handed = typename Mma<FEWBIT_F16>::V8;
+  __shared__ Handed handed[2][kPairs][SUBS][kRowsPass / 16][kWave];
   const int lane = threadIdx.x % kWave;
   const auto [hk, part, place] = spot_of(a.by_hkv, a.by_parts_dkv);
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave), pair = wave % kPairs;
@@ -1098,7 +1099,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   const RowReader<DT, D> rows_at;
   const ColumnReader<DT, D> columns_at;
   f32x16 acc[SUBS][D / 32] = {};
-  constexpr float lower = 1.0f / (1 << kLift<DT>);
+  constexpr float lower = 1.0f / (1 << kLift);
   const float scale2 = a.scale * kLog2e;
   // One side's part of a tile of rows: SECOND and MASKED are constants, so that each
   // is one run of code in which products and the rest overlap.
@@ -1129,7 +1130,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
 #pragma unroll
         for (int c = 0; c < 4; ++c) {
           const f32x4 stat = *reinterpret_cast<const f32x4*>(&in.stats[SECOND][32 * h + 8 * c + lane / 32 * 4]);
-          const V8 given = SECOND ? handed[slot][pair][u][2 * h + c / 2][lane] : V8{};
+          const Handed given = SECOND ? handed[slot][pair][u][2 * h + c / 2][lane] : Handed{};
 #pragma unroll
           for (int j = 0; j < 4; ++j) {
             const int i = 4 * c + j;
@@ -1140,7 +1141,7 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
 #pragma unroll
         for (int step = 0; step < 2; ++step) {
           n[u][step] = narrow<DT>(p[u], step);
-          if (!SECOND) handed[slot][pair][u][2 * h + step][lane] = n[u][step];
+          if (!SECOND) handed[slot][pair][u][2 * h + step][lane] = narrow<FEWBIT_F16>(p[u], step);
         }
       }
 #pragma unroll
