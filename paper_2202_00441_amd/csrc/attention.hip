@@ -65,8 +65,8 @@ struct Args {
   int batch, hq, hkv, g, d;           // g: query heads to a key head
   int causal, window;
   float scale;
-  Divisor by_g, by_hkv, by_batch, by_parts, by_parts_dkv, by_quads, by_rows;
-  int tiles;                          // of a sequence (packed: places for tiles of all)
+  Divisor by_g, by_hkv, by_place, by_parts, by_parts_dkv, by_quads, by_rows;
+  int tiles, tiles_first;             // of a sequence; whether all sequences' first tiles come first
   int rows;                           // split forward: of a sequence and key head
   int shares, share_least;            // split forward: workgroups of a key head, passes of one at least
   int parts, parts_dkv;               // of a workgroup's walk (forward or dQ; dK and dV)
@@ -133,8 +133,9 @@ __device__ __forceinline__ bool find_packed(const Args& a, bool keys, int times,
 
 // This workgroup's key head, sequence and tile.  Neighbouring workgroups have
 // different key heads, so those of one key head, which read the same keys, run on
-// one XCD where the heads are a multiple of eight; tiles come from the last, which
-// under a causal mask see the most keys, to the first.
+// one XCD where the heads are a multiple of eight.  Tiles come from the last, which under a
+// causal mask see the most keys, to the first: those of one sequence after another, so that
+// its keys are read from that XCD's L2, or (tiles_first) the last ones of all sequences first.
 __device__ __forceinline__ bool find(const Args& a, bool keys, int times, int rows, int place, Seq& s, int& tile) {
   if (a.cu_q) {
     int tiles;
@@ -142,8 +143,9 @@ __device__ __forceinline__ bool find(const Args& a, bool keys, int times, int ro
     tile = keys ? tile : tiles - 1 - tile;
     return true;
   }
-  tile = a.by_batch.divide(place);
-  s.b = place - tile * a.batch;
+  const int by = a.by_place.divide(place), rest = place - by * static_cast<int>(a.by_place.n);
+  s.b = a.tiles_first ? rest : by;
+  tile = a.tiles_first ? by : rest;
   if (!keys) tile = a.tiles - 1 - tile;       // of keys the first are seen by the most rows
   s.q0 = s.k0 = 0;
   s.nq = static_cast<int>(a.rows_q);
@@ -535,6 +537,14 @@ __device__ __forceinline__ void gather(const typename Mma<DT>::T* lv, const Colu
 
 constexpr int kKeys = 64;                                           // keys of a pass
 
+// The forward for many rows: a workgroup holds 128 rows of Q in registers, 32 to a wave,
+// and walks the keys they see in tiles of 64, one pass with a running maximum and sum; a
+// tile of K and V (32 KB at D = 128) serves all four waves, and two workgroups share a CU.
+// The maximum follows only when a row's scores pass it by 2^8, so the sums seldom have to
+// be scaled.  Bound by the matrix pipes, with the exponentials under them: 4 x 4096 rows, 16
+// heads of 128 in bf16, 533 us, 1030 TFLOP/s (a library product of 8192^3 reaches 1160); 16 x
+// 2048, causal, 365 us.  Of a workgroup's time 14 us pass outside the tiles.  Forming the
+// next tile's scores beside this tile's exponentials was slower, 625 us to 560.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -685,8 +695,10 @@ __device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
   return units;
 }
 
-// Keys are read once and not kept in the caches (64 caches of 8192 keys, 16 heads to 4:
-// 177 us, else 200).
+// Bound by HBM: one row on 64 caches of 8192 keys, 16 heads to 4 of 128 in bf16, 100 us,
+// 5.4 TB/s.  Each wave has two buffers of its own, so that it waits for no other.  Keys are
+// read once and not kept in the caches (64 caches of 8192 keys, 16 heads to 4, more of them
+// than the memory-side cache holds: 177 us, else 200).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -809,7 +821,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
 
 // Rows of units that several shares worked on: out = sum of their outputs, each by its
 // weight exp(lse_share - lse).  A workgroup takes a row, each wave every fourth share, four
-// at a time so that their loads are on their way together, two elements a lane.
+// at a time so that their loads are on their way together, two elements a lane.  Bound by
+// latency: 4 to 6 us (one row on 16000 keys in 63 shares: 17 us with the shares' kernel, with
+// one wave to a row 32).
 constexpr int kSharesTurn = 4;
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
@@ -869,7 +883,7 @@ __global__ __launch_bounds__(kThreads) void attn_join_kernel(const Args a) {
 }
 
 // The same for the parts of a workgroup's walk over keys: a thread takes four elements of
-// a row, with the loads of four parts on their way together.
+// a row, with the loads of four parts on their way together.  Bound by latency, 6 us.
 constexpr int kPartsMost = 16, kPartsTurn = 4;
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_parts_kernel(const Args a, Divisor by_joins) {
@@ -921,6 +935,11 @@ constexpr int kLift = 15;
 // dQ needs all keys of a row and dK, dV all rows of a key: one kernel for each,
 // both of which form S and dP (seven products where five would do, but no sums
 // across workgroups: nothing is added atomically, and no gradient waits in memory).
+//
+// dQ: 128 rows of Q and dO to a workgroup, which walks tiles of 64 keys as the forward does;
+// delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
+// type for its product with K.  Bound by the matrix pipes: 4 x 4096 rows, 16 heads of 128 in
+// bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 485 us.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1022,7 +1041,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
 // time.  Two waves share a run: one forms S, P and dV, the other dP, dS and dK, one
 // tile of rows behind, with P handed over in LDS.  So each wave holds one of K and V
 // and one of the two gradients, the same products run on both sides, and the two waves
-// of a SIMD are always one of either kind.  The tiles come through three buffers.
+// of a SIMD are always one of either kind.  The tiles come through three buffers.  P and
+// dS are rounded to the storage type for their products with dO and Q.
+// Bound by the matrix pipes at the clock the card holds under them, and by 12 us of a
+// workgroup's time outside the tiles, one workgroup to a CU: 4 x 4096 rows, 16 heads of 128 in
+// bf16, 1130 us, 970 TFLOP/s; 16 x 2048, causal, 811 us.  (Copies of the kernel without the
+// exponentials, without the reads of lse and delta, or with half of the reads from LDS take
+// 98% of the time.)  4 x 4096 rows, when these pairs took 1590 us: one wave for both sides,
+// with twice the registers, 2430; 64 keys to a pair, which spills at D = 128, 1700.
 constexpr int kRowsPass = 64;
 constexpr int kPairs = 4, kThreadsPairs = 2 * kPairs * kWave;
 
@@ -1199,7 +1225,8 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
   }
 }
 
-// Sums of the parts of both kernels' walks, in their order, four elements a thread:
+// Sums of the parts of both kernels' walks, in their order, four elements a thread, bound
+// by latency, 7 us:
 // workgroups for rows, then workgroups for runs of `group` keys.
 __device__ __forceinline__ f32x4 sum_of(const float* parts, int64_t step, int used) {
   f32x4 sum{};
@@ -1215,7 +1242,7 @@ __device__ __forceinline__ f32x4 sum_of(const float* parts, int64_t step, int us
 }
 template <int DT>
 __global__ __launch_bounds__(kThreads) void attn_sums_kernel(const Args a, Divisor by_joins_q, Divisor by_joins_k, int q_groups, int group,
-                                                             int tiles_k) {
+                                                             Divisor by_place_k, int tiles_first_k) {
   using T = typename Mma<DT>::T;
   using V4 = typename Mma<DT>::V4;
   const bool keys = static_cast<int>(blockIdx.x) >= q_groups;
@@ -1237,7 +1264,8 @@ __global__ __launch_bounds__(kThreads) void attn_sums_kernel(const Args a, Divis
     return;
   }
   Args b = a;
-  b.tiles = tiles_k;
+  b.by_place = by_place_k;
+  b.tiles_first = tiles_first_k;
   if (!find(b, true, 1, group, place, s, tile)) return;
   const int all = a.cu_k ? s.nk : static_cast<int>(a.rows_k), first = tile * group, key = first + of;
   if (of >= group || key >= all) return;
@@ -1302,6 +1330,17 @@ Shares shares_of(const fewbit_attn* a) {
   return r;
 }
 
+// The order of `tiles` tiles of every sequence.  Where walks differ in length and a CU gets
+// few of them the longest come first, else a sequence's tiles follow each other: 16 x 2048
+// rows, 16 heads of 128, causal, 4096 workgroups: the forward 388 us longest first, 365 so,
+// with 1.16 and 0.20 GB read past the L2 (dK and dV 846 and 811, and written 0.47 and 0.26);
+// 21 x 455 rows, 48 heads to 12, 1008 workgroups, dK and dV: 186 us longest first, 244 so.
+void set_order(Args& r, const fewbit_attn* a, int64_t tiles) {
+  r.tiles = static_cast<int>(tiles);
+  r.tiles_first = a->causal && !a->window && tiles * a->batch * a->heads_kv < 12 * static_cast<int64_t>(device_cus());
+  r.by_place = divisor(static_cast<int>(std::max<int64_t>(1, r.tiles_first ? a->batch : tiles)));
+}
+
 // Parts of every workgroup's walk of `passes` passes at most: as many as give every CU a
 // workgroup (under a causal mask two, for the walks' lengths differ), where that shortens
 // the walk by enough to pay for the join's launch and traffic, eight passes.  Forward and
@@ -1362,7 +1401,6 @@ Args args_of(const fewbit_attn* a) {
   r.scale = a->scale;
   r.by_g = divisor(r.g);
   r.by_hkv = divisor(r.hkv);
-  r.by_batch = divisor(std::max(r.batch, 1));
   r.by_parts = r.by_parts_dkv = divisor(1);
   r.by_quads = divisor(r.d / 4);
   return r;
@@ -1434,7 +1472,7 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.share_least = static_cast<int>(shares.least);
   if (r.shares == 0) {
     const Grid g = grid_of(a, false);
-    r.tiles = static_cast<int>(over(rows, kRowsGroup));
+    set_order(r, a, over(rows, kRowsGroup));
     r.parts = static_cast<int>(g.parts);
     r.by_parts = divisor(r.parts);
     if (r.parts > 1) {
@@ -1500,25 +1538,28 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   r.by_parts_dkv = divisor(r.parts_dkv);
   r.part_dq = r.stats + 2 * r.stats_delta;
   r.part_dkv = r.part_dq + (g.parts > 1 ? g.parts * rows_all * r.d : 0);
-  const int tiles_q = static_cast<int>(over(rows, kRowsGroup)), group = static_cast<int>(keys_dkv(a)), tiles_k = static_cast<int>(over(a->rows_k, group));
+  const int group = static_cast<int>(keys_dkv(a));
+  const int64_t tiles_q = over(rows, kRowsGroup), tiles_k = over(a->rows_k, group);
   if (a->rows_q > 0) {
-    r.tiles = tiles_q;
+    set_order(r, a, tiles_q);
     rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dq_kernel, r, q_groups, st));
     if (rc != FEWBIT_OK) return rc;
   }
   if (a->rows_k > 0) {
-    r.tiles = tiles_k;
+    set_order(r, a, tiles_k);
     const auto start = r.d > 64 ? start_dkv<128, 1> : group == kPairs * 64 ? start_dkv<64, 2> : start_dkv<64, 1>;
     rc = launch_status("fewbit_attn_bwd", start(r, bf16, static_cast<unsigned>(k_groups), st));
   }
   const bool join_q = g.parts > 1 && a->rows_q > 0, join_k = g.parts_dkv > 1 && a->rows_k > 0;
   if (rc != FEWBIT_OK || (!join_q && !join_k)) return rc;
-  r.tiles = tiles_q;
+  Args r_k = r;
+  set_order(r, a, tiles_q);
+  set_order(r_k, a, tiles_k);
   const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(int64_t{group} * r.d / 4, kThreads);
   const int64_t joins_q = join_q ? g.q_places * r.hkv * share_q : 0, joins_k = join_k ? g.k_places * r.hkv * share_k : 0;
   if (!fits_launch(joins_q + joins_k)) return FEWBIT_E_INVALID;
   return launch_status("fewbit_attn_bwd",
                        launch(bf16 ? attn_sums_kernel<FEWBIT_BF16> : attn_sums_kernel<FEWBIT_F16>, dim3(static_cast<unsigned>(joins_q + joins_k)),
                               kThreads, st, r, divisor(static_cast<int>(share_q)), divisor(static_cast<int>(share_k)), static_cast<int>(joins_q),
-                              group, tiles_k));
+                              group, r_k.by_place, r_k.tiles_first));
 }
