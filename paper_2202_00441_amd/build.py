@@ -13,12 +13,11 @@ Flags:
                                 its first loads wait for no load of their addresses (leading
                                 pointers and integers only; none if a structure comes first)
   constexpr steps               the bf16 output factors are evaluated at compile time
+  parallel jobs                 the sources are compiled at the same time
 """
 import os
 import subprocess
 import sys
-import tempfile
-from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
@@ -29,11 +28,11 @@ SOURCES = [os.path.join(CSRC, name) for name in
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
-    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC",
+    "--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-shared",
     "-fno-gpu-flush-denormals-to-zero", "-fno-fast-math", "-ffp-contract=on",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fconstexpr-steps=200000000", "-mllvm", "-amdgpu-kernarg-preload-count=16",
-    "-Wall", "-I", os.path.join(ROOT, "include"),
+    "-Wall", "-I", os.path.join(ROOT, "include"), "-parallel-jobs=5",
 ]
 
 
@@ -43,12 +42,7 @@ CXX = os.environ.get("CXX", "g++")
 
 
 def build(verbose: bool = False, extra=()) -> str:
-    # the sources apart and at the same time, then the library of their objects
-    with tempfile.TemporaryDirectory() as d, ThreadPoolExecutor(len(SOURCES)) as pool:
-        objects = [os.path.join(d, os.path.basename(src) + ".o") for src in SOURCES]
-        list(pool.map(lambda so: _compile([HIPCC, *FLAGS, *extra, "-c", so[0], "-o", so[1] + ".tmp"], so[1], verbose),
-                      zip(SOURCES, objects)))
-        _compile([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", OUT + ".tmp", *objects], OUT, verbose)
+    _compile([HIPCC, *FLAGS, *extra, "-o", OUT + ".tmp", *SOURCES], OUT, verbose)
     if _torch_headers():
         build_native(verbose)        # links libfewbit.so, so after it
     else:
