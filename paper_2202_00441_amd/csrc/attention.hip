@@ -426,24 +426,43 @@ __device__ __forceinline__ void load_rows(const typename Mma<DT>::T* row, int d,
   }
 }
 
-// Registers of D / 32 products whose lane is a row of the result, 32 elements each.
+// Registers of D / 32 products whose lane is a row of the result, 32 elements each, times
+// `scale`, to `offset` elements past `base`, the lane's row's; the first `rows` rows are there.
+// They go through 32 D elements of LDS of the wave's own, so that a store has whole rows, 16
+// bytes a lane: a lane's own elements lie in fours with another lane's between.  16 x 2048
+// rows, 16 heads of 128, on 64 keys: 71 us, stored from the registers 87.
 template <int DT, int D>
-__device__ __forceinline__ void store_rows(typename Mma<DT>::T* row, int d, const f32x16 (&x)[D / 32], float scale) {
+__device__ __forceinline__ void store_rows(typename Mma<DT>::T* lds, int d, const f32x16 (&x)[D / 32], float scale, typename Mma<DT>::T* base,
+                                           uint32_t offset, int rows) {
+  using T = typename Mma<DT>::T;
   using V4 = typename Mma<DT>::V4;
-  const int c = threadIdx.x % kWave / 32 * 4;
+  using V8 = typename Mma<DT>::V8;
+  constexpr int kChunks = D / 8, kRowsStore = kWave / kChunks;
+  // of 16 rows' chunks, no two in the same banks
+  const auto place = [](int row, int chunk) { return row * D + (chunk ^ (D == 128 ? row & 15 : row >> 1 & 7)) * 8; };
+  const int lane = threadIdx.x % kWave;
 #pragma unroll
   for (int t = 0; t < D / 32; ++t)
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
       V4 y;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) y[j] = static_cast<typename Mma<DT>::T>(x[t][4 * u + j] * scale);
-      const int at = 32 * t + 8 * u + c;
-      if (at < d) *reinterpret_cast<V4*>(row + at) = y;
+      for (int j = 0; j < 4; ++j) y[j] = static_cast<T>(x[t][4 * u + j] * scale);
+      *reinterpret_cast<V4*>(lds + place(lane % 32, 4 * t + u) + lane / 32 * 4) = y;
     }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  const int chunk = lane % kChunks;
+#pragma unroll
+  for (int i = 0; i < 32 / kRowsStore; ++i) {
+    const int r = i * kRowsStore + lane / kChunks;
+    const uint32_t row = __shfl(offset, r);
+    const V8 y = *reinterpret_cast<const V8*>(lds + place(r, chunk));
+    if (r < rows && chunk * 8 < d) *reinterpret_cast<V8*>(base + row + chunk * 8) = y;
+  }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 }
 
-// The same as fp32.
+// The lane's row as fp32, from the registers.
 template <int D>
 __device__ __forceinline__ void store_rows32(float* row, int d, const f32x16 (&x)[D / 32], float scale) {
   const int c = threadIdx.x % kWave / 32 * 4;
@@ -537,6 +556,18 @@ __device__ __forceinline__ void gather(const typename Mma<DT>::T* lv, const Colu
 
 constexpr int kKeys = 64;                                           // keys of a pass
 
+// store_rows for rows of a (sequence, key head) from row `first` of all `rows` on; the lane's
+// is head `head` of query `pos`.
+template <int DT, int D>
+__device__ __forceinline__ void store_queries(const Args& a, const Seq& s, void* out, typename Mma<DT>::T* lds, int hk, int first, int rows, int pos,
+                                              int head, const f32x16 (&x)[D / 32], float scale) {
+  const int pos0 = a.by_g.divide(first), head0 = hk * a.g;
+  // below 2^32: 32 queries of at most 2^20 heads
+  const uint32_t offset = (static_cast<uint32_t>(pos - pos0) * a.hq + (head - head0)) * a.d;
+  store_rows<DT, D>(lds, a.d, x, scale, static_cast<typename Mma<DT>::T*>(out) + ((s.b * a.rows_q + s.q0 + pos0) * a.hq + head0) * a.d, offset,
+                    rows - first);
+}
+
 // The forward for many rows: a workgroup holds 128 rows of Q in registers, 32 to a wave,
 // and walks the keys they see in tiles of 64, one pass with a running maximum and sum; a
 // tile of K and V (32 KB at D = 128) serves all four waves, and two workgroups share a CU.
@@ -590,16 +621,17 @@ __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
          score<DT, D, kKeys / 32>(in.a, k0, q, rr, k0 < every.lo || k0 + kKeys > every.hi, own, a.scale * kLog2e, x, p);
          gather<DT, D, kKeys / 32>(in.b, cr, p, x);
        });
-  if (!there) return;
   const Two both = halves32(x.sum);
   const float sum = both.a + both.b;
   const float lse = sum == 0.0f ? -INFINITY : x.most * a.scale + logf(sum);
   const float inverse = sum > 0.0f || sum != sum ? 1.0f / sum : 0.0f;
   const int64_t at = (s.b * a.rows_q + s.q0 + pos) * a.hq + head;
   if (slice.used == 1) {
-    store_rows<DT, D>(static_cast<T*>(a.o) + at * a.d, a.d, x.o, inverse);
-    if (lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = lse;
-  } else {
+    __syncthreads();                    // the tiles' buffers are free
+    const int w = __builtin_amdgcn_readfirstlane(wave);
+    store_queries<DT, D>(a, s, a.o, reinterpret_cast<T*>(&buf0) + w * 32 * D, hk, first + w * kRowsWave, rows, pos, head, x.o, inverse);
+    if (there && lane < 32) a.lse[(s.b * a.hq + head) * a.rows_q + s.q0 + pos] = lse;
+  } else if (there) {
     const int64_t to = part * rows_all(a) + at;
     store_rows32<D>(a.part_o + to * a.d, a.d, x.o, inverse);
     if (lane < 32) a.part_lse[to] = lse;
@@ -1031,11 +1063,12 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
            }
          }
        });
-  if (!there) return;
-  if (slice.used == 1)
-    store_rows<DT, D>(static_cast<T*>(a.dq) + at, a.d, dq, a.scale);
-  else
+  if (slice.used == 1) {
+    __syncthreads();                    // the tiles' buffers are free
+    store_queries<DT, D>(a, s, a.dq, reinterpret_cast<T*>(&buf0) + wave * 32 * D, hk, first + wave * kRowsWave, rows, pos, head, dq, a.scale);
+  } else if (there) {
     store_rows32<D>(a.part_dq + part * rows_all(a) * a.d + at, a.d, dq, a.scale);
+  }
 }
 
 // A workgroup takes 4 runs of 32 SUBS keys and walks the rows that see them, 32 at a
@@ -1213,16 +1246,19 @@ __global__ __launch_bounds__(kThreadsPairs, 2) void attn_dkv_kernel(const Args a
       turn(buf2, buf1, buf0, i + 2);
     }
   }
+  __syncthreads();                      // the tiles' buffers are free
+  T* own = reinterpret_cast<T*>(second ? &buf1 : &buf0) + pair * 32 * D;
 #pragma unroll
   for (int u = 0; u < SUBS; ++u) {
-    const int key = run + 32 * u + lane % 32;
-    if (key >= keys) continue;
+    const int key = run + 32 * u;
     const int64_t at = (s.b * a.rows_k + s.k0 + key) * a.hkv + hk;
     const float scale = second ? a.scale : lower;
-    if (slice.used == 1)
-      store_rows<DT, D>(static_cast<T*>(second ? a.dk : a.dv) + at * a.d, a.d, acc[u], scale);
-    else
-      store_rows32<D>(a.part_dkv + ((part * keys_all(a) + at) * 2 + second) * a.d, a.d, acc[u], scale);
+    if (slice.used == 1) {
+      store_rows<DT, D>(own, a.d, acc[u], scale, static_cast<T*>(second ? a.dk : a.dv) + at * a.d,
+                        static_cast<uint32_t>(lane % 32 * a.hkv) * a.d, keys - key);
+    } else if (key + lane % 32 < keys) {
+      store_rows32<D>(a.part_dkv + ((part * keys_all(a) + at + lane % 32 * a.hkv) * 2 + second) * a.d, a.d, acc[u], scale);
+    }
   }
 }
 
