@@ -573,9 +573,9 @@ __device__ __forceinline__ void store_queries(const Args& a, const Seq& s, void*
 // tile of K and V (32 KB at D = 128) serves all four waves, and two workgroups share a CU.
 // The maximum follows only when a row's scores pass it by 2^8, so the sums seldom have to
 // be scaled.  Bound by the products and the exponentials between them, which two waves a
-// SIMD overlap in part: 4 x 4096 rows, 16 heads of 128 in bf16, 533 us, 1030 TFLOP/s (a library
-// product of 8192^3 reaches 1160); 16 x 2048, causal, 365 us, matrix pipes busy for 44% of the
-// cycles.  Of a workgroup's time 14 us pass outside the tiles.  Forming the
+// SIMD overlap in part: 4 x 4096 rows, 16 heads of 128 in bf16, 528 us, 1040 TFLOP/s (a library
+// product of 8192^3 reaches 1160); 16 x 2048, causal, 357 us, matrix pipes busy for 44% of the
+// cycles.  Of a workgroup's time 10 us pass outside the tiles.  Forming the
 // next tile's scores beside this tile's exponentials was slower, 625 us to 560.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
@@ -972,7 +972,7 @@ constexpr int kLift = 15;
 // dQ: 128 rows of Q and dO to a workgroup, which walks tiles of 64 keys as the forward does;
 // delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
 // type for its product with K.  Bound as the forward is: 4 x 4096 rows, 16 heads of 128 in
-// bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 485 us, matrix pipes busy for 48%.
+// bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 493 us, matrix pipes busy for 48%.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1077,9 +1077,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
 // and one of the two gradients, the same products run on both sides, and the two waves
 // of a SIMD are always one of either kind.  The tiles come through three buffers.  P and
 // dS are rounded to the storage type for their products with dO and Q.
-// Bound by the products, the hand-over between them and 12 us of a workgroup's time outside
-// the tiles, one workgroup to a CU: 4 x 4096 rows, 16 heads of 128 in bf16, 1130 us, 970
-// TFLOP/s; 16 x 2048, causal, 811 us, matrix pipes busy for 36% of the cycles.  (Copies of the kernel without the
+// Bound by the products, the hand-over between them and 13 us of a workgroup's time outside
+// the tiles, one workgroup to a CU: 4 x 4096 rows, 16 heads of 128 in bf16, 1160 us, 950
+// TFLOP/s; 16 x 2048, causal, 793 us, matrix pipes busy for 36% of the cycles.  (Copies of the kernel without the
 // exponentials, without the reads of lse and delta, or with half of the reads from LDS take
 // 98% of the time.)  4 x 4096 rows, when these pairs took 1590 us: one wave for both sides,
 // with twice the registers, 2430; 64 keys to a pair, which spills at D = 128, 1700.
