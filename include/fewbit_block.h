@@ -50,8 +50,9 @@ extern "C" {
  *
  * Layouts.  q, k, v and dout have head_dim elements in a row and strides
  * {sequence, row, head} in elements (packed: the first is not used), each a
- * multiple of 8; pointers are 16-byte aligned.  out, dq, dk and dv are dense:
- * [batch,] rows, heads, head_dim.  lse is dense: [batch,] heads_q, rows_q.
+ * multiple of 8 and not negative; pointers are 16-byte aligned.  out, dq, dk
+ * and dv are dense: [batch,] rows, heads, head_dim.  lse is dense: [batch,]
+ * heads_q, rows_q.
  *
  * Values of k and v that no row of a sequence sees but that lie inside it
  * have to be finite.

@@ -1330,7 +1330,12 @@ int check(const fewbit_attn* a) {
   return FEWBIT_OK;
 }
 
-bool strides_fit(const int64_t (&s)[3]) { return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0; }
+// Rows start at multiples of 16 bytes, in ascending order: lanes' offsets inside a load have
+// no sign.
+int check_strides(const int64_t (&s)[3]) {
+  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return FEWBIT_E_INVALID;
+  return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 ? FEWBIT_OK : FEWBIT_E_ALIGN;
+}
 
 int64_t over(int64_t n, int64_t per) { return (n + per - 1) / per; }
 
@@ -1488,7 +1493,10 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   if (a->rows_q == 0) return FEWBIT_OK;
   if (!q || !out || !lse || (a->rows_k > 0 && (!k || !v))) return FEWBIT_E_NULL;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out)) return FEWBIT_E_ALIGN;
-  if (!strides_fit(a->q_stride) || !strides_fit(a->k_stride) || !strides_fit(a->v_stride)) return FEWBIT_E_ALIGN;
+  for (const auto* s : {&a->q_stride, &a->k_stride, &a->v_stride}) {
+    rc = check_strides(*s);
+    if (rc != FEWBIT_OK) return rc;
+  }
   const int64_t need = fewbit_attn_workspace(a, 0);
   if (need > 0 && !workspace) return FEWBIT_E_NULL;
   if (workspace_bytes < need) return FEWBIT_E_INVALID;
@@ -1546,8 +1554,10 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out) || misaligned(dout) || misaligned(dq) ||
       misaligned(dk) || misaligned(dv))
     return FEWBIT_E_ALIGN;
-  if (!strides_fit(a->q_stride) || !strides_fit(a->k_stride) || !strides_fit(a->v_stride) || !strides_fit(a->dout_stride))
-    return FEWBIT_E_ALIGN;
+  for (const auto* s : {&a->q_stride, &a->k_stride, &a->v_stride, &a->dout_stride}) {
+    rc = check_strides(*s);
+    if (rc != FEWBIT_OK) return rc;
+  }
   if (workspace_bytes < fewbit_attn_workspace(a, 1)) return FEWBIT_E_INVALID;
   rc = check_stream_device(static_cast<hipStream_t>(stream));
   if (rc != FEWBIT_OK) return rc;

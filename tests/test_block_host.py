@@ -125,6 +125,17 @@ def test_attention_pointers_strides_and_workspace():
     assert attn_fwd(long, work=ODD) == E_ALIGN
 
 
+def test_attention_strides_are_not_negative():
+    """A lane's offset inside a load is a number without a sign: rows in reverse order would be read far ahead."""
+    for i in range(3):
+        for name in ("q_stride", "k_stride", "v_stride", "dout_stride"):
+            stride = [5120, 512, 64]
+            stride[i] = -stride[i]
+            assert attn_bwd(attn(**{name: stride})) == E_INVALID, (name, i)
+            if name != "dout_stride":
+                assert attn_fwd(attn(**{name: stride})) == E_INVALID, (name, i)
+
+
 def test_attention_of_nothing():
     assert attn_fwd(attn(batch=0)) == attn_bwd(attn(batch=0)) == OK
     assert attn_fwd(attn(rows_q=0)) == OK
