@@ -81,21 +81,29 @@ struct Seq {
 
 __device__ __forceinline__ int clamped(int x, int64_t most) { return static_cast<int>(min(static_cast<int64_t>(max(x, 0)), most)); }
 
-// Rows of packed sequence b in one of the tensors; b = batch: those past the last.
-__device__ __forceinline__ void span(const int32_t* cu, int64_t rows, int batch, int b, int& at, int& n) {
-  at = b == 0 ? 0 : clamped(cu[b], rows);
-  const int end = b == batch ? static_cast<int>(rows) : clamped(cu[b + 1], rows);
-  n = max(end - at, 0);
-}
-
-__device__ __forceinline__ Seq packed_seq(const Args& a, int b) {
-  Seq s;
-  int q0, k0;
-  span(a.cu_q, a.rows_q, a.batch, b, q0, s.nq);
-  span(a.cu_k, a.rows_k, a.batch, b, k0, s.nk);
-  s.q0 = q0;
-  s.k0 = k0;
-  s.b = 0;
+// Rows of 64 packed sequences from b0 on in one of the tensors, one to a lane; sequence
+// `batch` are the rows past the last.  An offset below one before it counts as that one, so no
+// row is in two sequences.  `past`: where the sequence before b0 ended, and then where the last
+// of these did.
+struct Span {
+  int at, end;
+};
+__device__ __forceinline__ Span spans(const int32_t* cu, int64_t rows, int batch, int b0, int& past) {
+  const int lane = threadIdx.x % kWave, b = b0 + lane;
+  Span s{static_cast<int>(rows), static_cast<int>(rows)};
+  if (b <= batch) {
+    s.at = b == 0 ? 0 : max(clamped(cu[b], rows), past);
+    if (b < batch) s.end = max(clamped(cu[b + 1], rows), past);
+  }
+  if (__any(s.end < s.at)) {
+#pragma unroll
+    for (int step = 1; step < kWave; step *= 2) {
+      const int other = __shfl_up(s.at, step);
+      if (lane >= step) s.at = max(s.at, other);
+    }
+    s.end = max(s.at, s.end);
+  }
+  past = __builtin_amdgcn_readlane(s.end, kWave - 1);
   return s;
 }
 
@@ -104,29 +112,31 @@ __device__ __forceinline__ Seq packed_seq(const Args& a, int b) {
 // come last; they see, and are seen by, nothing.
 __device__ __forceinline__ bool find_packed(const Args& a, bool keys, int times, int rows, int at, Seq& s, int& tile, int& tiles) {
   const int lane = threadIdx.x % kWave;
-  int before = 0;
+  int before = 0, past_q = 0, past_k = 0;
   for (int b0 = 0; b0 <= a.batch; b0 += kWave) {
-    const int b = b0 + lane;
-    int at_b, n = 0;
-    if (b <= a.batch) span(keys ? a.cu_k : a.cu_q, keys ? a.rows_k : a.rows_q, a.batch, b, at_b, n);
-    const int own = static_cast<int>((static_cast<int64_t>(n) * times + rows - 1) / rows);
+    const Span q = spans(a.cu_q, a.rows_q, a.batch, b0, past_q), k = spans(a.cu_k, a.rows_k, a.batch, b0, past_k);
+    const int nq = q.end - q.at, nk = k.end - k.at;
+    const int own = static_cast<int>((static_cast<int64_t>(keys ? nk : nq) * times + rows - 1) / rows);
     int sum = own;                                            // of this lane's and all before it
 #pragma unroll
     for (int step = 1; step < kWave; step *= 2) {
       const int other = __shfl_up(sum, step);
       if (lane >= step) sum += other;
     }
-    const uint64_t past = __ballot(at < before + sum);
-    if (past) {
-      const int first = __builtin_ctzll(past);
-      const int b1 = __builtin_amdgcn_readfirstlane(b0 + first);
-      tiles = __builtin_amdgcn_readfirstlane(__shfl(own, first));
-      tile = at - before - __builtin_amdgcn_readfirstlane(__shfl(sum - own, first));
-      s = packed_seq(a, b1);
-      if (b1 == a.batch) (keys ? s.nq : s.nk) = 0;
+    const uint64_t here = __ballot(at < before + sum);
+    if (here) {
+      const int first = __builtin_ctzll(here);
+      tiles = __builtin_amdgcn_readlane(own, first);
+      tile = at - before - __builtin_amdgcn_readlane(sum - own, first);
+      s.b = 0;
+      s.q0 = __builtin_amdgcn_readlane(q.at, first);
+      s.k0 = __builtin_amdgcn_readlane(k.at, first);
+      s.nq = __builtin_amdgcn_readlane(nq, first);
+      s.nk = __builtin_amdgcn_readlane(nk, first);
+      if (b0 + first == a.batch) (keys ? s.nq : s.nk) = 0;
       return true;
     }
-    before += __builtin_amdgcn_readfirstlane(__shfl(sum, kWave - 1));
+    before += __builtin_amdgcn_readlane(sum, kWave - 1);
   }
   return false;
 }

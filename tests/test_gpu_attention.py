@@ -11,6 +11,7 @@ each doubled for the fp32 sums and the exponentials under them, plus 1e-6 of the
 largest magnitude of the row's terms.  lse is a sum of fp32 terms: 1e-5.
 """
 import math
+import random
 
 import pytest
 import torch
@@ -229,6 +230,42 @@ def test_packed_bounds_are_clamped():
         out, lse = P.attention_fwd(q, k, v, causal=True, cu_q=cu, cu_k=cu)
         P.attention_bwd(do, q, k, v, out, lse, causal=True, cu_q=cu, cu_k=cu)
     torch.cuda.synchronize()
+
+
+def effective(cu, rows):
+    """Where sequences begin: the first at 0, bounds inside the tensor, none before one ahead of it."""
+    r = [0]
+    for x in cu[1:]:
+        r.append(max(r[-1], min(max(x, 0), rows)))
+    return r
+
+
+@pytest.mark.parametrize("heads,d,causal,window", [((2, 2), 64, True, 0), ((8, 2), 128, False, 0), ((3, 1), 40, True, 17)])
+@pytest.mark.parametrize("cu_q,cu_k", [
+    ([90, 10, 40, 20], [90, 10, 40, 20]), ([0, 1000, 50, -3], [0, 3, 2, 290]), ([0, 60, 10, 60, 5, 200], [0, 10, 300, 20, 4, 1]),
+    ([7, 7, 7, 7], [300, 200, 100, 0]), (None, None)])
+def test_packed_offsets_out_of_order(heads, d, causal, window, cu_q, cu_k):
+    """An offset below one before it counts as that one: the same bits as with those offsets, and no row left out."""
+    nq, nk = 250, 300
+    if cu_q is None:                                        # more sequences than a wave looks at together
+        r = random.Random(3)
+        cu_q, cu_k = ([max(0, min(n, 2 * i + r.randint(-40, 40))) for i in range(140)] for n in (nq, nk))
+    q, _, _, do = make(BF16, 1, nq, 0, *heads, d, packed=True)
+    k, v = (make(BF16, 1, 0, nk, *heads, d, seed=s, packed=True)[1] for s in (1, 2))
+    results = []
+    for bounds in ((cu_q, cu_k), (effective(cu_q, nq), effective(cu_k, nk))):
+        bounds = [torch.tensor(x, dtype=torch.int32, device="cuda") for x in bounds]
+        kw = {"causal": causal, "window": window, "cu_q": bounds[0], "cu_k": bounds[1]}
+        out, lse = P.attention_fwd(q, k, v, **kw)
+        results.append((out, lse, *P.attention_bwd(do, q, k, v, out, lse, **kw)))
+    assert all(torch.equal(a, b) for a, b in zip(*results))
+    at_q, at_k = effective(cu_q, nq), effective(cu_k, nk)
+    for b in range(len(at_q) - 1):
+        i, j = slice(at_q[b], at_q[b + 1]), slice(at_k[b], at_k[b + 1])
+        ref, want = reference(q[i], k[j], v[j], do[i], causal, window, 1 / math.sqrt(d))
+        assert torch.equal(torch.isinf(want), torch.isinf(results[0][1][:, i]))
+        for x, name, rows in zip((results[0][0], *results[0][2:]), ("out", "dq", "dk", "dv"), (i, i, j, j)):
+            near(x[rows], ref[name], f"{name} of {b}")
 
 
 def test_no_keys_and_no_rows():
