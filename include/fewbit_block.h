@@ -52,7 +52,8 @@ extern "C" {
  * {sequence, row, head} in elements (packed: the first is not used), each a
  * multiple of 8 and not negative; pointers are 16-byte aligned.  out, dq, dk
  * and dv are dense: [batch,] rows, heads, head_dim.  lse is dense: [batch,]
- * heads_q, rows_q.
+ * heads_q, rows_q.  A launch has fewer than 2^32 threads: sizes that take more
+ * are refused (the backward takes 512 for 128 or 256 keys of a key head).
  *
  * Values of k and v that no row of a sequence sees but that lie inside it
  * have to be finite.
@@ -113,7 +114,8 @@ int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const void* q, const
  *
  * Everything is computed in fp32 and rounded once.  The weights' gradients
  * are summed in an order that depends on the sizes alone.  batch * tokens *
- * (heads + 1) stays below 2^31.
+ * (heads + 1) stays below 2^31, and the forward takes fewer than 2^32 threads: 4,
+ * 8 or 16 (head_dim up to 64, 128, 256) for two heads of a token.
  */
 typedef struct fewbit_qk {
     int32_t dtype;                /* storage type of q, k and their weights    */
@@ -194,8 +196,8 @@ typedef struct fewbit_adamw {
 
 /* m, v: fp32 or 8-bit codes; m_scale, v_scale: one float per block with
  * 8-bit moments, else not used; master: fp32 or NULL.  `tensors` is a host
- * array, read before the call returns.  Takes one launch per 256 tensors; if
- * one fails the earlier ones are done. */
+ * array, read before the call returns.  Takes one launch per 256 tensors (and
+ * per 3.4e10 elements); if one fails the earlier ones are done. */
 int fewbit_adamw_step(const fewbit_adamw* a, const fewbit_adamw_tensor* tensors, int32_t count,
                       void* m, void* v, float* m_scale, float* v_scale, float* master,
                       void* stream);

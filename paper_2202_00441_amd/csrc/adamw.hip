@@ -21,6 +21,8 @@
 // two where a largest magnitude crosses a bound.  The root and the quotient of
 // the update are the hardware's approximations (1 ulp each): what they feed is
 // added to a weight some thousand times as large.
+#include <algorithm>
+
 #include "block.h"
 
 namespace {
@@ -357,34 +359,38 @@ extern "C" int fewbit_adamw_step(const fewbit_adamw* h, const fewbit_adamw_tenso
   a.eps = static_cast<float>(h->eps);
   a.key = static_cast<uint32_t>(h->seed) * 0x6A09E667u + 0x3C6EF372u;
 
-  int64_t block0 = 0;
-  for (int i = 0; i < count;) {
-    uint64_t groups = 0;
-    a.count = 0;
-    for (; i < count && a.count < kMaxTensors; ++i) {
-      const int64_t blocks = blocks_of(tensors[i].n);
-      if (blocks == 0 || !tensors[i].grad) {
-        block0 += blocks;
-        continue;
-      }
-      const uint64_t more = (blocks + kRun - 1) / kRun;
-      if (groups + more >= uint64_t{1} << 24) {                      // fewer than 2^32 threads
-        if (a.count == 0) return FEWBIT_E_INVALID;                   // more than any device's memory holds
-        break;
-      }
-      a.t[a.count] = {tensors[i].param, tensors[i].grad, tensors[i].n, block0};
-      a.first[a.count++] = static_cast<uint32_t>(groups);
-      groups += more;
-      block0 += blocks;
-    }
-    if (a.count == 0) continue;
-    const hipStream_t s = static_cast<hipStream_t>(stream);
+  const hipStream_t s = static_cast<hipStream_t>(stream);
+  constexpr int64_t kGroupsMost = kThreadsLaunch / kThreads - 1;
+  int64_t groups = 0;
+  a.count = 0;
+  const auto start = [&]() {
+    if (a.count == 0) return static_cast<int>(FEWBIT_OK);
     const unsigned n = static_cast<unsigned>(groups);
     const hipError_t e = pt == FEWBIT_F32   ? start_grad<FEWBIT_F32>(a, gt, h->state_bits, n, s)
                          : pt == FEWBIT_F16 ? start_grad<FEWBIT_F16>(a, gt, h->state_bits, n, s)
                                             : start_grad<FEWBIT_BF16>(a, gt, h->state_bits, n, s);
-    const int status = launch_status("fewbit_adamw_step", e);
-    if (status != FEWBIT_OK) return status;
+    a.count = 0;
+    groups = 0;
+    return launch_status("fewbit_adamw_step", e);
+  };
+  // A tensor that the rest of a launch does not hold goes on in the next, after whole workgroups.
+  const int64_t p_size = pt == FEWBIT_F32 ? 4 : 2, g_size = gt == FEWBIT_F32 ? 4 : 2;
+  int64_t block0 = 0;
+  for (int i = 0; i < count; ++i) {
+    const int64_t blocks = blocks_of(tensors[i].n);
+    for (int64_t b = 0; b < blocks && tensors[i].grad;) {
+      if (a.count == kMaxTensors || groups == kGroupsMost) {
+        const int status = start();
+        if (status != FEWBIT_OK) return status;
+      }
+      const int64_t take = std::min(blocks - b, (kGroupsMost - groups) * kRun), at = b * kBlock;
+      a.t[a.count] = {static_cast<char*>(tensors[i].param) + at * p_size, static_cast<const char*>(tensors[i].grad) + at * g_size,
+                      tensors[i].n - at, block0 + b};
+      a.first[a.count++] = static_cast<uint32_t>(groups);
+      groups += (take + kRun - 1) / kRun;
+      b += take;
+    }
+    block0 += blocks;
   }
-  return FEWBIT_OK;
+  return start();
 }

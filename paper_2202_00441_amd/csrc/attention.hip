@@ -1336,6 +1336,9 @@ int check(const fewbit_attn* a) {
   if (a->batch < 0 || a->batch >= kMost || a->rows_q < 0 || a->rows_k < 0 || a->rows_k >= kMost || a->heads_q >= 1 << 20 ||
       a->rows_q >= kMost / (a->heads_q / a->heads_kv))
     return FEWBIT_E_INVALID;
+  // no more elements than there are addresses: all products of sizes below fit 64 bits
+  const double seqs = a->cu_q ? 1.0 : static_cast<double>(a->batch), most = 0x1p47;
+  if (seqs * a->rows_q * a->heads_q * a->head_dim >= most || seqs * a->rows_k * a->heads_kv * a->head_dim >= most) return FEWBIT_E_INVALID;
   if ((a->cu_q == nullptr) != (a->cu_k == nullptr) || (a->cu_q && a->k_len)) return FEWBIT_E_INVALID;
   return FEWBIT_OK;
 }
@@ -1460,8 +1463,6 @@ Args args_of(const fewbit_attn* a) {
 
 int64_t rounded(int64_t n) { return over(n, 4) * 4; }         // floats, to whole 16 bytes
 
-bool fits_launch(int64_t groups) { return groups < int64_t{1} << 24; }       // fewer than 2^32 threads
-
 #define FEWBIT_ATTN_START(KERNEL, ARGS, GROUPS, STREAM)                                                              \
   ((ARGS).d <= 64 ? (bf16 ? launch(KERNEL<FEWBIT_BF16, 64>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS)    \
                           : launch(KERNEL<FEWBIT_F16, 64>, dim3(static_cast<unsigned>(GROUPS)), kThreads, STREAM, ARGS))    \
@@ -1511,9 +1512,6 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   if (need > 0 && !workspace) return FEWBIT_E_NULL;
   if (workspace_bytes < need) return FEWBIT_E_INVALID;
   if (need > 0 && misaligned(workspace)) return FEWBIT_E_ALIGN;
-  rc = check_stream_device(static_cast<hipStream_t>(stream));
-  if (rc != FEWBIT_OK) return rc;
-  const hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = a->dtype == FEWBIT_BF16;
   Args r = args_of(a);
   r.q = q;
@@ -1521,6 +1519,7 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.v = v;
   r.o = out;
   r.lse = lse;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
   const int64_t rows = a->rows_q * r.g;
   const Shares shares = shares_of(a);
   r.shares = static_cast<int>(shares.n);
@@ -1535,7 +1534,9 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
       r.part_lse = r.part_o + g.parts * (a->cu_q ? 1 : a->batch) * a->rows_q * r.hq * r.d;
     }
     const int64_t share = over(int64_t{kRowsGroup} * r.d / 4, kThreads), joins = g.q_places * r.hkv * share, groups = g.q_places * r.hkv * g.parts;
-    if (!fits_launch(groups) || (r.parts > 1 && !fits_launch(joins))) return FEWBIT_E_INVALID;
+    if (!fits_launch(groups, kThreads) || (r.parts > 1 && !fits_launch(joins, kThreads))) return FEWBIT_E_INVALID;
+    rc = check_stream_device(st);
+    if (rc != FEWBIT_OK) return rc;
     rc = launch_status("fewbit_attn_fwd", FEWBIT_ATTN_START(attn_fwd_kernel, r, groups, st));
     if (rc != FEWBIT_OK || r.parts == 1) return rc;
     return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_parts_kernel<FEWBIT_BF16> : attn_parts_kernel<FEWBIT_F16>,
@@ -1546,7 +1547,9 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.by_rows = divisor(r.rows);
   r.part_lse = r.part_o + (r.shares + a->batch) * r.hkv * r.rows * r.d;
   const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = a->batch * r.hkv * r.rows;
-  if (!fits_launch(groups) || !fits_launch(joins)) return FEWBIT_E_INVALID;
+  if (!fits_launch(groups, kThreads) || !fits_launch(joins, kThreads)) return FEWBIT_E_INVALID;
+  rc = check_stream_device(st);
+  if (rc != FEWBIT_OK) return rc;
   rc = launch_status("fewbit_attn_fwd", start_split(r, bf16, static_cast<unsigned>(groups), st));
   if (rc != FEWBIT_OK || shares.whole) return rc;
   return launch_status("fewbit_attn_fwd", launch(bf16 ? attn_join_kernel<FEWBIT_BF16> : attn_join_kernel<FEWBIT_F16>,
@@ -1569,11 +1572,19 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
     if (rc != FEWBIT_OK) return rc;
   }
   if (workspace_bytes < fewbit_attn_workspace(a, 1)) return FEWBIT_E_INVALID;
-  rc = check_stream_device(static_cast<hipStream_t>(stream));
-  if (rc != FEWBIT_OK) return rc;
-  const hipStream_t st = static_cast<hipStream_t>(stream);
   const bool bf16 = a->dtype == FEWBIT_BF16;
   Args r = args_of(a);
+  const Grid g = grid_of(a, true);
+  const int group = static_cast<int>(keys_dkv(a));
+  const bool join_q = g.parts > 1 && a->rows_q > 0, join_k = g.parts_dkv > 1 && a->rows_k > 0;
+  const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(int64_t{group} * r.d / 4, kThreads);
+  const int64_t joins_q = join_q ? g.q_places * r.hkv * share_q : 0, joins_k = join_k ? g.k_places * r.hkv * share_k : 0;
+  const int64_t q_groups = g.q_places * r.hkv * g.parts, k_groups = g.k_places * r.hkv * g.parts_dkv;
+  if (!fits_launch(q_groups, kThreads) || !fits_launch(k_groups, kThreadsPairs) || !fits_launch(joins_q + joins_k, kThreads))
+    return FEWBIT_E_INVALID;
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  rc = check_stream_device(st);
+  if (rc != FEWBIT_OK) return rc;
   r.q = q;
   r.k = k;
   r.v = v;
@@ -1586,17 +1597,13 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
   r.dq = dq;
   r.dk = dk;
   r.dv = dv;
-  const Grid g = grid_of(a, true);
-  const int64_t rows = a->rows_q * r.g, q_groups = g.q_places * r.hkv * g.parts, k_groups = g.k_places * r.hkv * g.parts_dkv;
-  if (!fits_launch(q_groups) || !fits_launch(k_groups)) return FEWBIT_E_INVALID;
   r.parts = static_cast<int>(g.parts);
   r.parts_dkv = static_cast<int>(g.parts_dkv);
   r.by_parts = divisor(r.parts);
   r.by_parts_dkv = divisor(r.parts_dkv);
   r.part_dq = r.stats + 2 * r.stats_delta;
   r.part_dkv = r.part_dq + (g.parts > 1 ? g.parts * rows_all * r.d : 0);
-  const int group = static_cast<int>(keys_dkv(a));
-  const int64_t tiles_q = over(rows, kRowsGroup), tiles_k = over(a->rows_k, group);
+  const int64_t tiles_q = over(a->rows_q * r.g, kRowsGroup), tiles_k = over(a->rows_k, group);
   if (a->rows_q > 0) {
     set_order(r, a, tiles_q);
     rc = launch_status("fewbit_attn_bwd", FEWBIT_ATTN_START(attn_dq_kernel, r, q_groups, st));
@@ -1607,14 +1614,10 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
     const auto start = r.d > 64 ? start_dkv<128, 1> : group == kPairs * 64 ? start_dkv<64, 2> : start_dkv<64, 1>;
     rc = launch_status("fewbit_attn_bwd", start(r, bf16, static_cast<unsigned>(k_groups), st));
   }
-  const bool join_q = g.parts > 1 && a->rows_q > 0, join_k = g.parts_dkv > 1 && a->rows_k > 0;
   if (rc != FEWBIT_OK || (!join_q && !join_k)) return rc;
   Args r_k = r;
   set_order(r, a, tiles_q);
   set_order(r_k, a, tiles_k);
-  const int64_t share_q = over(int64_t{kRowsGroup} * r.d / 4, kThreads), share_k = over(int64_t{group} * r.d / 4, kThreads);
-  const int64_t joins_q = join_q ? g.q_places * r.hkv * share_q : 0, joins_k = join_k ? g.k_places * r.hkv * share_k : 0;
-  if (!fits_launch(joins_q + joins_k)) return FEWBIT_E_INVALID;
   return launch_status("fewbit_attn_bwd",
                        launch(bf16 ? attn_sums_kernel<FEWBIT_BF16> : attn_sums_kernel<FEWBIT_F16>, dim3(static_cast<unsigned>(joins_q + joins_k)),
                               kThreads, st, r, divisor(static_cast<int>(share_q)), divisor(static_cast<int>(share_k)), static_cast<int>(joins_q),

@@ -210,6 +210,10 @@ inline int check_stream_device(hipStream_t stream) {
   return owner == current ? FEWBIT_OK : FEWBIT_E_INVALID;
 }
 
+// A launch has fewer than 2^32 threads.
+constexpr int64_t kThreadsLaunch = int64_t{1} << 32;
+inline bool fits_launch(int64_t groups, int64_t threads) { return groups < kThreadsLaunch / threads; }
+
 // A launch by the runtime's own call, which returns its status.
 template <class T>
 struct Same {

@@ -413,8 +413,6 @@ extern "C" int fewbit_qk_fwd(const fewbit_qk* a, const void* q, const void* k, c
   if (rc != FEWBIT_OK) return rc;
   if ((a->heads_q > 0 && !q_out) || (a->heads_k > 0 && !k_out)) return FEWBIT_E_NULL;
   if (misaligned(q_out) || misaligned(k_out)) return FEWBIT_E_ALIGN;
-  rc = check_stream_device(static_cast<hipStream_t>(stream));
-  if (rc != FEWBIT_OK) return rc;
   Args r = args_of(a, cos, sin, positions, false);
   r.s[0].x = q;
   r.s[1].x = k;
@@ -423,7 +421,9 @@ extern "C" int fewbit_qk_fwd(const fewbit_qk* a, const void* q, const void* k, c
   r.s[0].y = q_out;
   r.s[1].y = k_out;
   const int64_t groups = r.first_k + groups_of(a, r.s[1].units);
-  if (groups >= int64_t{1} << 24) return FEWBIT_E_INVALID;       // fewer than 2^32 threads: more than a device holds
+  if (!fits_launch(groups, kThreads)) return FEWBIT_E_INVALID;
+  rc = check_stream_device(static_cast<hipStream_t>(stream));
+  if (rc != FEWBIT_OK) return rc;
   return launch_status("fewbit_qk_fwd", start(a, r, false, static_cast<unsigned>(groups), static_cast<hipStream_t>(stream)));
 }
 

@@ -136,6 +136,17 @@ def test_attention_strides_are_not_negative():
                 assert attn_fwd(attn(**{name: stride})) == E_INVALID, (name, i)
 
 
+def test_attention_grids_past_a_launch():
+    """A launch has fewer than 2^32 threads.  The kernel for dK and dV has 512 to a workgroup, here of one key head
+    each, 2^23 of them: refused before the kernel for dQ, of 256 threads, is launched.  Sizes whose products pass 64
+    bits are refused too."""
+    a = attn(batch=1 << 20, heads_q=8, heads_kv=8, head_dim=128, rows_q=1, rows_k=1)
+    assert attn_bwd(a) == E_INVALID
+    for most in ({"batch": (1 << 30) - 1, "rows_q": (1 << 30) - 1, "heads_q": 1 << 18, "heads_kv": 1 << 18},
+                 {"batch": 1 << 29, "rows_q": 1 << 29, "rows_k": 1 << 29, "heads_q": 1 << 19, "heads_kv": 1 << 19}):
+        assert attn_fwd(attn(**most), size=(1 << 63) - 1) == attn_bwd(attn(**most), size=(1 << 63) - 1) == E_INVALID
+
+
 def test_attention_of_nothing():
     assert attn_fwd(attn(batch=0)) == attn_bwd(attn(batch=0)) == OK
     assert attn_fwd(attn(rows_q=0)) == OK

@@ -168,6 +168,28 @@ def test_many_blocks():
     check(Case(BF16, 32, (20_000_003, 5)))
 
 
+def test_a_tensor_past_one_launch():
+    """2^35 elements and some take more than 2^32 threads: the step goes on in another launch.  Equal gradients at the
+    first step: every weight moves by lr but for a rounding, and every moment lies between two codes that are not 0."""
+    n = 2 ** 35 + 70001
+    blocks = P.adamw_blocks(n)
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < 6 * n + 8 * blocks + 2 ** 32:
+        pytest.skip("needs 212 GB of device memory")
+    w, g = (torch.full((n,), x, dtype=BF16, device="cuda") for x in (0.0, 1e-3))
+    m, v = (torch.zeros(256 * blocks, dtype=torch.uint8, device="cuda").view(F8) for _ in range(2))
+    ms, vs = (torch.ones(blocks, device="cuda") for _ in range(2))
+    P.adamw_step([w], [g], m, v, ms, vs, lr=0.25, weight_decay=0.0, step=1)
+    piece = 2 ** 30
+    for a in range(0, n, piece):
+        part = slice(a, min(n, a + piece))
+        assert bool((w[part] == -0.25).all()), a
+        assert bool((m.view(torch.uint8)[part] > 0).all()) and bool((v.view(torch.uint8)[part] > 0).all()), a
+    assert not m.view(torch.uint8)[n:].any() and bool((ms == ms[0]).all()) and bool((vs == vs[0]).all())
+    del w, g, m, v, ms, vs
+    torch.cuda.empty_cache()
+
+
 def test_step_by_step():
     """Ten steps in a row; each against the formula from the state before it."""
     c = Case(BF16, 8, master=True)
