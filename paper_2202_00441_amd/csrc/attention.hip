@@ -1382,6 +1382,8 @@ Shares shares_of(const fewbit_attn* a) {
   r.least = std::max(std::min<int64_t>(2, per(cus)), each <= 4 ? each : 1);
   r.n = over(passes, std::max(r.least, per((a->head_dim <= 64 ? 3 : 2) * cus)));
   r.whole = !a->k_len && std::max(r.least, over(each * a->batch, r.n)) % each == 0;
+  // a workgroup of the join takes a row; rows that are too many for it go to the tiled kernel
+  if (!fits_launch(r.n * a->heads_kv, kThreads) || (!r.whole && !fits_launch(a->batch * a->heads_kv * rows, kThreads))) return {};
   return r;
 }
 
@@ -1546,8 +1548,7 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   r.rows = static_cast<int>(rows);
   r.by_rows = divisor(r.rows);
   r.part_lse = r.part_o + (r.shares + a->batch) * r.hkv * r.rows * r.d;
-  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = a->batch * r.hkv * r.rows;
-  if (!fits_launch(groups, kThreads) || !fits_launch(joins, kThreads)) return FEWBIT_E_INVALID;
+  const int64_t groups = static_cast<int64_t>(r.shares) * r.hkv, joins = a->batch * r.hkv * r.rows;       // both fit a launch
   rc = check_stream_device(st);
   if (rc != FEWBIT_OK) return rc;
   rc = launch_status("fewbit_attn_fwd", start_split(r, bf16, static_cast<unsigned>(groups), st));

@@ -146,6 +146,24 @@ def test_cache(dtype, b, sq, hq, hkv, d, sk, lens, window):
     check(q, k, v, do, causal=True, window=window, k_len=list(lens))
 
 
+@pytest.mark.parametrize("lens", (False, True))
+def test_many_short_sequences(lens):
+    """Windows of a few rows: 2^24 rows of a sequence and key head, more than a launch has workgroups."""
+    b, n, h, d = 65536, 16, 16, 8
+    q, k, v, do = make(BF16, b, n, n, h, h, d)
+    k_len = torch.arange(b, dtype=torch.int32, device="cuda") % (n + 1) if lens else None
+    out, lse = P.attention_fwd(q, k, v, k_len=k_len)
+    dq, dk, dv = P.attention_bwd(do, q, k, v, out, lse, k_len=k_len)
+    for i in (0, 1, 7, 16, 17, 255, 4097, 32767, 32768, 65534, 65535):
+        ref, want = reference(q[i], k[i], v[i], do[i], False, 0, 1 / math.sqrt(d), i % (n + 1) if lens else None)
+        assert torch.equal(torch.isinf(want), torch.isinf(lse[i]))
+        for x, name in ((out, "out"), (dq, "dq"), (dk, "dk"), (dv, "dv")):
+            near(x[i], ref[name], f"{name} of {i}")
+    few = slice(60000, 60100)
+    o, _ = P.attention_fwd(q[few], k[few], v[few], k_len=None if k_len is None else k_len[few])
+    assert ((o.float() - out[few].float()).abs() <= 2.0 ** -6 * v[few].float().abs().amax((1, 3))[:, None, :, None]).all()
+
+
 @pytest.mark.parametrize("dtype,lens,extra,hq,hkv,d,causal,window", [
     (BF16, (5, 1, 0, 130, 64), 0, 4, 2, 64, True, 0), (F16, (129,), 7, 2, 2, 128, False, 0), (BF16, (0, 0), 3, 2, 1, 64, True, 0),
     (BF16, (300, 1, 255, 2), 5, 8, 1, 128, True, 100), (F16, tuple(range(90)), 0, 2, 2, 32, True, 0), (BF16, (), 9, 2, 2, 64, True, 0)])
