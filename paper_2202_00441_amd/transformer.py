@@ -24,12 +24,14 @@ from .optim import AdamW
 
 
 class Cache:
-    """Keys and values of every layer for up to `most` tokens of each sequence."""
+    """Keys and values of every layer for up to `most` tokens of each sequence.  `lengths` has how many
+    there are of each, on the device; `used`, known on the host, is what none of them passes."""
 
     def __init__(self, layers: int, batch: int, most: int, kv_heads: int, head_dim: int, dtype, device):
         shape = layers, batch, most, kv_heads, head_dim
         self.k, self.v = (torch.empty(shape, dtype=dtype, device=device) for _ in range(2))
         self.lengths = torch.zeros(batch, dtype=torch.int32, device=device)
+        self.batch, self.most, self.used = batch, most, 0
 
 
 class Block(torch.nn.Module):
@@ -81,12 +83,17 @@ class Transformer(torch.nn.Module):
         self.most = most
         self._tables = None
 
+    def _check_positions(self, n: int):
+        if n > self.most:
+            raise ValueError(f"the model has {self.most} positions, {n} are needed")
+
     def tables(self, device):
         if self._tables is None or self._tables[0].device != device:
             self._tables = rope_tables(self.most, self.blocks[0].head_dim, device=device)
         return self._tables
 
     def forward(self, tokens):
+        self._check_positions(tokens.shape[1])
         x = self.embed(tokens)
         cos, sin = self.tables(x.device)
         for b in self.blocks:
@@ -102,16 +109,24 @@ class Transformer(torch.nn.Module):
         """Logits of new tokens [batch, new] after those in the cache, which takes them up."""
         if tokens.shape[1] == 0:
             raise ValueError("no tokens to extend with")
+        if tokens.shape[0] != cache.batch:
+            raise ValueError(f"the cache is of {cache.batch} sequences, not {tokens.shape[0]}")
+        used = cache.used + tokens.shape[1]
+        if used > cache.most:
+            raise ValueError(f"the cache holds {cache.most} tokens of a sequence, {used} are needed")
+        self._check_positions(used)
         x = self.embed(tokens)
         cos, sin = self.tables(x.device)
         for i, b in enumerate(self.blocks):
             x = b.extend(x, cos, sin, cache, i, cache.lengths)
         cache.lengths += tokens.shape[1]
+        cache.used = used
         return self.head(self.norm(x))
 
     @torch.no_grad()
     def generate(self, tokens, new: int):
         """`new` tokens after each sequence of tokens [batch, prompt], greedily."""
+        self._check_positions(tokens.shape[1] + new - 1)
         cache = self.cache(tokens.shape[0], tokens.shape[1] + new)
         out = []
         for _ in range(new):

@@ -11,7 +11,7 @@ import pytest
 import torch
 
 import paper_2202_00441_amd as P
-from paper_2202_00441_amd import _lib
+from paper_2202_00441_amd import _lib, transformer
 from paper_2202_00441_amd._lib import E_ALIGN, E_BITS, E_DTYPE, E_INVALID, E_NULL, OK
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
@@ -273,6 +273,26 @@ def test_calls_refuse_tensors_that_are_not_on_a_device():
     with pytest.raises(ValueError, match="same length"):
         P.adamw_step([x], [], x, x, lr=0.1, step=1)
     P.adamw_step([], [], x, x, lr=0.1, step=1)
+
+
+def test_generation_stays_inside_the_cache_and_the_tables():
+    """A token past a cache, or past the positions there are angles for, is refused on the host."""
+    model = transformer.Transformer(10, 64, 1, 2, 1, bits=None, most=20)
+    tokens = torch.zeros(2, 6, dtype=torch.long)
+    with pytest.raises(ValueError, match="the cache holds 5 tokens"):
+        model.extend(tokens, model.cache(2, 5))
+    cache = model.cache(2, 9)
+    cache.used = 4                                          # as after four tokens
+    with pytest.raises(ValueError, match="the cache holds 9 tokens"):
+        model.extend(tokens, cache)
+    with pytest.raises(ValueError, match="the model has 20 positions"):
+        model.extend(torch.zeros(1, 21, dtype=torch.long), model.cache(1, 30))
+    with pytest.raises(ValueError, match="the model has 20 positions"):
+        model.generate(tokens, 16)                          # the last token has no position yet: 21 are needed
+    with pytest.raises(ValueError, match="the model has 20 positions"):
+        model(torch.zeros(1, 21, dtype=torch.long))
+    with pytest.raises(ValueError, match="sequences"):
+        model.extend(tokens, model.cache(3, 9))
 
 
 def test_blocks():
