@@ -128,7 +128,7 @@ class Transformer(torch.nn.Module):
         """`new` tokens after each sequence of tokens [batch, prompt], greedily."""
         self._check_positions(tokens.shape[1] + new - 1)
         cache = self.cache(tokens.shape[0], tokens.shape[1] + new)
-        out = []
+        out = [tokens[:, :0]]
         for _ in range(new):
             tokens = self.extend(tokens, cache)[:, -1:].float().argmax(-1)
             out.append(tokens)

@@ -295,6 +295,12 @@ def test_generation_stays_inside_the_cache_and_the_tables():
         model.extend(tokens, model.cache(3, 9))
 
 
+def test_generation_of_nothing():
+    model = transformer.Transformer(10, 64, 1, 2, 1, bits=None, most=20)
+    out = model.generate(torch.zeros(2, 6, dtype=torch.long), 0)
+    assert out.shape == (2, 0) and out.dtype == torch.long
+
+
 def test_blocks():
     assert [P.adamw_blocks(n) for n in (0, 1, 256, 257)] == [0, 1, 1, 2]
     assert _lib.strerror(E_ALIGN)
