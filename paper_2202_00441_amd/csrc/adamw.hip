@@ -76,17 +76,23 @@ __device__ __forceinline__ void update(const Args& a, float (&w)[N], const float
   }
 }
 
-// A block's largest magnitude over the 32 lanes that hold it, infinities and NaN
-// left out (they become NaN codes whatever the scale).
+// A block's largest magnitude over the 32 lanes that hold it.  Infinities and NaN are left
+// out: they become NaN codes whatever the scale, and infinities here, for adding the dither
+// to a NaN's mantissa may carry into its sign.
 template <int N>
-__device__ __forceinline__ float largest(const float (&x)[N]) {
+__device__ __forceinline__ float largest(float (&x)[N]) {
   float most = 0.0f;
 #pragma unroll
-  for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]));
+  for (int i = 0; i < N; ++i) most = __builtin_elementwise_maximum(most, fabsf(x[i]));      // a NaN stays one
   if (__builtin_expect(__any(!(most < INFINITY)), 0)) {
     most = 0.0f;
 #pragma unroll
-    for (int i = 0; i < N; ++i) most = fmaxf(most, fabsf(x[i]) < INFINITY ? fabsf(x[i]) : 0.0f);
+    for (int i = 0; i < N; ++i) {
+      if (fabsf(x[i]) < INFINITY)
+        most = fmaxf(most, fabsf(x[i]));
+      else
+        x[i] = INFINITY;
+    }
   }
   return across<5>(most, [](float p, float q) { return fmaxf(p, q); });
 }
@@ -99,7 +105,7 @@ __device__ __forceinline__ uint32_t scale_field(float most) {
 }
 __device__ __forceinline__ float power(uint32_t field) { return __builtin_bit_cast(float, field << 23); }
 
-// y >= 0 (at most 448, or not finite) rounded to one of the two 8-bit numbers around it,
+// y >= 0 (at most 448, or infinite) rounded to one of the two 8-bit numbers around it,
 // up with the probability of its distance from the lower: u / 2^16 of that or more is
 // taken up.  The format keeps three bits of 23 behind the leading one; adding u to the
 // 16 bits below them carries into them as it should.  Below 2^-6 its numbers are 2^-9
@@ -148,7 +154,7 @@ __device__ __forceinline__ void store_some(const Stream& s, T* base, uint32_t at
 // The moments of N elements, as codes of a block that 32 lanes hold; the second four of
 // a lane's elements lie `apart` elements behind its first.
 template <int N>
-__device__ __forceinline__ void encode(const Args& a, int64_t flat, int apart, const float (&m)[N], const float (&v)[N], uint32_t (&cm)[N / 4],
+__device__ __forceinline__ void encode(const Args& a, int64_t flat, int apart, float (&m)[N], float (&v)[N], uint32_t (&cm)[N / 4],
                                        uint32_t (&cv)[N / 4], float& ms, float& vs) {
   const uint32_t fm = scale_field(largest(m)), fv = scale_field(largest(v));
   const float im = power(254 - fm), iv = power(254 - fv);

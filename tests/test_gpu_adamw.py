@@ -234,6 +234,23 @@ def test_bad_gradients_stay_with_their_elements():
         assert torch.equal(c.params[0][fine], d.params[0][fine])
 
 
+@pytest.mark.parametrize("dtype,patterns", [
+    (BF16, (0x7fff, 0xffff, 0x7f81, 0x7fc0)), (F16, (0x7fff, 0xffff, 0x7c01, 0x7e00)), (F32, (0x7fffffff, 0xffffffff, 0x7f800001, 0x7fc00000))])
+def test_any_nan_stays_one_in_8_bits(dtype, patterns):
+    """Whatever its payload, and whatever the dither adds to it."""
+    bits = {2: torch.int16, 4: torch.int32}[dtype.itemsize]
+    places = [5 + 40 * i for i in range(len(patterns))]
+    for seed in range(12):
+        c = Case(dtype, 8, (1000,), seed=seed)
+        for at, x in zip(places, patterns):
+            c.grads[0].view(bits)[at] = x - (1 << 8 * dtype.itemsize if x >> 8 * dtype.itemsize - 1 else 0)
+        c.run(seed=seed)
+        bad = torch.zeros(1000, dtype=torch.bool, device="cuda")
+        bad[places] = True
+        assert torch.equal(torch.isnan(c.m[:1000].float()), bad) and torch.equal(torch.isnan(c.v[:1000].float()), bad)
+        assert torch.equal(torch.isnan(c.params[0]), bad)
+
+
 def test_second_moments_do_not_become_zero():
     c = Case(F32, 8, (256,))
     c.grads[0].zero_()
