@@ -66,12 +66,16 @@ __device__ __forceinline__ void moments(const Args& a, const float (&g)[N], floa
     v[i] = v[i] * a.b2 + (g[i] * g[i]) * a.a2;
   }
 }
-template <int N>
+// SMALL: what the hardware's root takes as 0, moments below the normal range, is brought into
+// its range first.
+template <bool SMALL, int N>
 __device__ __forceinline__ void update(const Args& a, float (&w)[N], const float (&g)[N], float (&m)[N], float (&v)[N]) {
   moments(a, g, m, v);
 #pragma unroll
   for (int i = 0; i < N; ++i) {
-    const float d = __builtin_amdgcn_sqrtf(v[i]) * a.root + a.eps;
+    const bool below = SMALL && v[i] < 0x1p-126f;
+    const float root = __builtin_amdgcn_sqrtf(below ? v[i] * 0x1p64f : v[i]) * (below ? 0x1p-32f : 1.0f);
+    const float d = root * a.root + a.eps;
     w[i] = w[i] * a.keep - a.step * (m[i] * __builtin_amdgcn_rcpf(d));
   }
 }
@@ -178,7 +182,7 @@ __device__ __forceinline__ void encode(const Args& a, int64_t flat, int apart, f
   vs = power(fv);
 }
 
-template <int PT, int GT, int BITS, bool MASTER>
+template <int PT, int GT, int BITS, bool MASTER, bool SMALL>
 __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
   using P = typename Store<PT>::type;
   using G = typename Store<GT>::type;
@@ -225,7 +229,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       if (!some[r]) continue;
-      update(a, w[r], gr[r], m[r], v[r]);
+      update<SMALL>(a, w[r], gr[r], m[r], v[r]);
       sm.store<float, kStore>(at[r] * 4, m[r]);
       sv.store<float, kStore>(at[r] * 4, v[r]);
       if constexpr (MASTER) sw.store<float, kStore>(at[r] * 4, w[r]);
@@ -272,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
     }
     unpack<N>(qm, oldm, m);
     unpack<N>(qv, oldv, v);
-    update(a, wf, gr, m, v);
+    update<SMALL>(a, wf, gr, m, v);
 #pragma unroll
     for (int r = 0; r < kRows; ++r) {
       const uint32_t here = at + r * kApart;
@@ -300,11 +304,20 @@ __global__ __launch_bounds__(kThreads) void adamw_kernel(const Args a) {
   }
 }
 
+template <int PT, int GT, int BITS, bool MASTER>
+hipError_t start_small(const Args& a, unsigned groups, hipStream_t s) {
+  // Roots that the hardware takes as 0 are below 2^-63: where the denominator's eps does not
+  // hide them they are formed with care.  (Always: 700 us where 684, 8 layers of width 2048 in
+  // bf16 with 8-bit moments.)
+  return a.root * 0x1p-63f > a.eps * 0x1p-24f ? launch(adamw_kernel<PT, GT, BITS, MASTER, true>, dim3(groups), kThreads, s, a)
+                                              : launch(adamw_kernel<PT, GT, BITS, MASTER, false>, dim3(groups), kThreads, s, a);
+}
+
 template <int PT, int GT, int BITS>
 hipError_t start(const Args& a, unsigned groups, hipStream_t s) {
   if constexpr (PT != FEWBIT_F32)
-    if (a.master) return launch(adamw_kernel<PT, GT, BITS, true>, dim3(groups), kThreads, s, a);
-  return launch(adamw_kernel<PT, GT, BITS, false>, dim3(groups), kThreads, s, a);
+    if (a.master) return start_small<PT, GT, BITS, true>(a, groups, s);
+  return start_small<PT, GT, BITS, false>(a, groups, s);
 }
 
 template <int PT, int GT>

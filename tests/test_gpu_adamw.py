@@ -260,6 +260,18 @@ def test_second_moments_do_not_become_zero():
     assert (c.v.float() > 0).all()
 
 
+@pytest.mark.parametrize("size", (1e-18, 1e-19, 1e-20))
+def test_second_moments_below_the_normal_range(size):
+    """eps = 0 at the first step: the update is lr times the gradient's sign.  The least second moment here, 0.05e-40,
+    is 3568 of the steps numbers lie apart there, so its root is right to 1.4e-4 / 2, and m's to 2^-23."""
+    c = Case(F32, 32, (1000,))
+    sign = torch.where(torch.arange(1000, device="cuda") % 2 == 0, 1.0, -1.0)
+    c.params[0].zero_(), c.m.zero_(), c.v.zero_()
+    c.grads[0].copy_(sign * size)
+    c.run(step=1, lr=0.5, eps=0.0, weight_decay=0.0)
+    assert ((c.params[0] + 0.5 * sign).abs() <= 0.5 * 1e-4).all()
+
+
 def test_mean_is_kept():
     """The same values rounded under 4096 seeds: the mean of n roundings between codes a step apart is within
     step / 2 / sqrt(n) of the value in the mean; six times that for the worst of 256 elements."""
