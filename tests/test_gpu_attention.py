@@ -124,6 +124,44 @@ def test_large_scores(dtype, d):
     check(q * 8, k * 8, v, do, causal=True)
 
 
+@pytest.mark.parametrize("b,sq,sk,hq,hkv,d,causal,window", [
+    (1, 2048, 2048, 2, 2, 64, False, 0), (2, 700, 900, 4, 2, 128, True, 0), (9, 70, 300, 16, 16, 40, False, 0), (1, 1500, 1500, 1, 1, 80, True, 300)])
+@pytest.mark.parametrize("size", (1.0, 1e-3, 1e-4, 1e-5))
+def test_small_gradients_in_fp16(b, sq, sk, hq, hkv, d, causal, window, size):
+    """Gradients of small dO, as without a loss scale: dS lies below fp16's normal range, the results need not.  In norm an
+    error of at most u = 2^-11 of the whole each from P, dS and delta, beside the rounding of the exact gradient, which at
+    these sizes is the largest part (a quarter more for it falls on other numbers)."""
+    q, k, v, do = make(F16, b, sq, sk, hq, hkv, d)
+    do = (do.float() * size).to(F16)
+    kw = {"causal": causal, "window": window}
+    out, lse = P.attention_fwd(q, k, v, **kw)
+    grads = dict(zip(("dq", "dk", "dv"), P.attention_bwd(do, q, k, v, out, lse, **kw)))
+    refs = [reference(q[i], k[i], v[i], do[i], causal, window, 1 / math.sqrt(d))[0] for i in range(b)]
+    for name, got in grads.items():
+        want = torch.stack([r[name][0] for r in refs])
+        rounding = (want.to(F16).double() - want).norm()
+        assert (got.double() - want).norm() <= 1.25 * rounding + 3 * 2.0 ** -11 * want.norm(), name
+
+
+def test_gradients_of_rows_of_different_sizes_in_fp16():
+    """Each row's dQ by itself, in norm, dO falling from row to row and values growing from key to key."""
+    q, k, v, do = make(F16, 1, 500, 900, 2, 1, 64)
+    do = (do.float() * 10.0 ** -(torch.arange(500, device="cuda") % 4)[:, None, None]).to(F16)
+    v = (v.float() * 2.0 ** (torch.arange(900, device="cuda") // 100 - 4)[:, None, None]).to(F16)
+    out, lse = P.attention_fwd(q, k, v)
+    dq = P.attention_bwd(do, q, k, v, out, lse)[0][0].double()
+    want = reference(q[0], k[0], v[0], do[0], False, 0, 1 / 8)[0]["dq"][0]
+    rounding = (want.to(F16).double() - want).norm(dim=-1)
+    assert ((dq - want).norm(dim=-1) <= 1.5 * rounding + 6 * 2.0 ** -11 * want.norm(dim=-1)).all()
+
+
+@pytest.mark.parametrize("sq,sk,d,causal", [(40, 16, 64, False), (200, 200, 128, True), (333, 33, 40, False)])
+def test_large_gradients_in_fp16(sq, sk, d, causal):
+    """dS past fp16's largest number, dQ and dK within it."""
+    q, k, v, do = make(F16, 1, sq, sk, 2, 1, d)
+    check(q * 0.01, k * 0.01, v * 100, do * 2000, causal=causal)
+
+
 def test_scale():
     q, k, v, do = make(BF16, 1, 70, 90, 2, 2, 64)
     check(q, k, v, do, scale=0.7)
