@@ -15,7 +15,8 @@ class AdamW(torch.optim.Optimizer):
     state_bits: 8 (a byte per moment and element, a power of two per 256, rounded
     with dither) or 32.  master: keep fp32 weights of 16-bit parameters, whose
     rounded copies the parameters then are.  Gradients have the parameters' type or
-    fp32; a parameter without one is left as it is.
+    fp32; a parameter without one is left as it is, and its steps, by whose number the
+    moments are corrected, are those in which it had one.
 
     The moments of a group's parameters of one type and device lie in flat buffers,
     made at the first step; adding a parameter group afterwards gives it buffers of
@@ -41,7 +42,7 @@ class AdamW(torch.optim.Optimizer):
             raise RuntimeError("the parameters of a group must stay as they were at its first step")
         blocks = [adamw_blocks(p.numel()) for p in params]
         n, moments = sum(blocks), _MOMENTS[self.state_bits]
-        b = {"params": params, "m": torch.zeros(n * ADAMW_BLOCK, device=device).to(moments)}
+        b = {"params": params, "counts": [0] * len(params), "m": torch.zeros(n * ADAMW_BLOCK, device=device).to(moments)}
         b["v"] = torch.zeros_like(b["m"])
         b["ms"] = b["vs"] = b["master"] = None
         if self.state_bits == 8:
@@ -66,9 +67,14 @@ class AdamW(torch.optim.Optimizer):
             kinds = dict.fromkeys((p.dtype, p.device) for p in group["params"] if p.grad is not None)
             for n, (dtype, device) in enumerate(kinds):
                 b = self._bucket(g, dtype, device)
-                adamw_step(b["params"], [_like(p.grad, p) for p in b["params"]], b["m"], b["v"], b["ms"], b["vs"], b["master"],
-                           lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"],
-                           weight_decay=group["weight_decay"], step=self._steps, seed=(self._steps << 8) + 16 * g + n)
+                grads, counts = [_like(p.grad, p) for p in b["params"]], tuple(b["counts"])
+                # one call for each number of steps that parameters have had: as a rule they all have as many
+                for count in dict.fromkeys(c for c, x in zip(counts, grads) if x is not None):
+                    these = [x if c == count else None for c, x in zip(counts, grads)]
+                    adamw_step(b["params"], these, b["m"], b["v"], b["ms"], b["vs"], b["master"],
+                               lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"],
+                               weight_decay=group["weight_decay"], step=count + 1, seed=(self._steps << 8) + 16 * g + n)
+                    b["counts"] = [c + (x is not None) for c, x in zip(b["counts"], these)]
         return loss
 
     def state_bytes(self) -> int:
@@ -77,10 +83,10 @@ class AdamW(torch.optim.Optimizer):
                    for t in (b["m"], b["v"], b["ms"], b["vs"], b["master"]) if t is not None)
 
     def state_dict(self) -> dict:
-        """Hyperparameters, the step count and the buffers as they are (8-bit moments in 8 bits)."""
+        """Hyperparameters, the step counts and the buffers as they are (8-bit moments in 8 bits)."""
         buffers = []
         for (g, dtype, _), b in self._buckets.items():
-            buffers.append({"group": g, "dtype": str(dtype), **{k: b[k] for k in ("m", "v", "ms", "vs", "master")}})
+            buffers.append({"group": g, "dtype": str(dtype), "counts": list(b["counts"]), **{k: b[k] for k in ("m", "v", "ms", "vs", "master")}})
         groups = [{k: v for k, v in group.items() if k != "params"} | {"params": [tuple(p.shape) for p in group["params"]]}
                   for group in self.param_groups]
         return {"steps": self._steps, "state_bits": self.state_bits, "master": self.master, "groups": groups, "buffers": buffers}
@@ -103,6 +109,8 @@ class AdamW(torch.optim.Optimizer):
                 raise ValueError("the state is of other parameters")
             wanted.append((b, saved))
         for b, saved in wanted:
+            # states without counts are of parameters that had a gradient in every step
+            b["counts"] = list(saved.get("counts", [state["steps"]] * len(b["params"])))
             for k in ("m", "v", "ms", "vs", "master"):
                 if b[k] is not None:
                     # codes go as bytes: a copy between 8-bit types would round

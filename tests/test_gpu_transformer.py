@@ -2,6 +2,7 @@
 attention and torch's own activation rule, its cached generation agrees with the
 whole-sequence forward, and the optimizer class steps, saves and restores.
 """
+import copy
 import math
 
 import pytest
@@ -152,6 +153,58 @@ def test_optimizer_leaves_out_what_has_no_gradient():
     opt.param_groups[0]["params"][-1].grad = torch.zeros(5, device="cuda")
     with pytest.raises(RuntimeError):
         opt.step()
+
+
+def both_optimizers(groups, **kw):
+    """P.AdamW in 32 bits over the parameters and torch's over copies of them."""
+    copies = [[torch.nn.Parameter(p.detach().clone()) for p in g] for g in groups]
+    return copies, P.AdamW([{"params": g} for g in groups], state_bits=32, **kw), torch.optim.AdamW([{"params": g} for g in copies], foreach=False, **kw)
+
+
+def agree(groups, copies):
+    for p, o in zip(sum(groups, []), sum(copies, [])):
+        assert ((p.detach() - o.detach()).abs() <= 1e-6 * (1 + o.detach().abs())).all()
+
+
+def test_steps_are_counted_for_each_parameter():
+    """A parameter whose gradients begin late, one that has them every third step, and a group added later move as
+    torch.optim.AdamW's do: each by the correction of its own count.  1e-6: ten steps of a few roundings of updates
+    below 0.02."""
+    params, _ = model_and_grads(torch.float32)
+    g = torch.Generator(device="cuda").manual_seed(5)
+    groups, added = [params[:3]], params[3:]
+    copies, opt, want = both_optimizers(groups, lr=1e-2, betas=(0.9, 0.999), weight_decay=0.1)
+    for step in range(12):
+        if step == 8:
+            groups.append(added)
+            copies.append([torch.nn.Parameter(p.detach().clone()) for p in added])
+            opt.add_param_group({"params": added})
+            want.add_param_group({"params": copies[1]})
+        for i, (p, o) in enumerate(zip(sum(groups, []), sum(copies, []))):
+            missing = i == 1 and step < 5 or i == 2 and step % 3 != 2
+            grad = torch.randn(p.shape, generator=g, device="cuda")
+            p.grad, o.grad = (None, None) if missing else (grad, grad)
+        opt.step()
+        want.step()
+        agree(groups, copies)
+
+
+def test_late_parameters_after_a_restart():
+    """Counts of their own are saved and restored."""
+    params, grads = model_and_grads(torch.float32)
+    opt = P.AdamW(params, lr=1e-2)
+    for i in range(3):
+        for j, p in enumerate(params):
+            p.grad = None if j == 1 and i < 2 else grads[i][j]
+        opt.step()
+    again = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    other = P.AdamW(again, lr=1.0)
+    other.load_state_dict(copy.deepcopy(opt.state_dict()))
+    for p, o, g in zip(params, again, grads[3]):
+        p.grad, o.grad = g, g
+    opt.step()
+    other.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, again))
 
 
 def test_losses_of_plain_adamw_are_followed():
