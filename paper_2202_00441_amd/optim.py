@@ -32,8 +32,9 @@ class AdamW(torch.optim.Optimizer):
         self._buckets = {}          # (group, dtype, device) -> buffers
         self._steps = 0
 
-    def _bucket(self, g: int, dtype, device) -> dict:
-        key = g, dtype, device
+    def _bucket(self, key) -> dict:
+        """The buffers of a key: those there are, or new ones, which the caller keeps."""
+        g, dtype, device = key
         params = [p for p in self.param_groups[g]["params"] if p.dtype == dtype and p.device == device]
         b = self._buckets.get(key)
         if b is not None and len(b["params"]) == len(params) and all(x is y for x, y in zip(b["params"], params)):
@@ -53,7 +54,6 @@ class AdamW(torch.optim.Optimizer):
             for p, k in zip(params, blocks):
                 b["master"][at:at + p.numel()] = _in_memory(p.detach())
                 at += k * ADAMW_BLOCK
-        self._buckets[key] = b
         return b
 
     @torch.no_grad()
@@ -66,7 +66,7 @@ class AdamW(torch.optim.Optimizer):
         for g, group in enumerate(self.param_groups):
             kinds = dict.fromkeys((p.dtype, p.device) for p in group["params"] if p.grad is not None)
             for n, (dtype, device) in enumerate(kinds):
-                b = self._bucket(g, dtype, device)
+                b = self._buckets[g, dtype, device] = self._bucket((g, dtype, device))
                 grads, counts = [_like(p.grad, p) for p in b["params"]], tuple(b["counts"])
                 # one call for each number of steps that parameters have had: as a rule they all have as many
                 for count in dict.fromkeys(c for c, x in zip(counts, grads) if x is not None):
@@ -93,22 +93,25 @@ class AdamW(torch.optim.Optimizer):
 
     @torch.no_grad()
     def load_state_dict(self, state: dict) -> None:
-        """The state of an optimizer over parameters of the same shapes and types in the same groups."""
+        """The state of an optimizer over parameters of the same shapes and types in the same groups.  Parameters of
+        a type that had not been stepped there begin anew here."""
         if state["state_bits"] != self.state_bits or state["master"] != self.master:
             raise ValueError("the state is of moments in another form")
         if [g["params"] for g in state["groups"]] != [[tuple(p.shape) for p in g["params"]] for g in self.param_groups]:
             raise ValueError("the state is of other parameters")
-        wanted = []
+        wanted = {}
         for saved in state["buffers"]:
             kinds = {(p.dtype, p.device) for p in self.param_groups[saved["group"]]["params"] if str(p.dtype) == saved["dtype"]}
             if len(kinds) != 1:
                 raise ValueError("the state is of parameters of other types")
-            b = self._bucket(saved["group"], *kinds.pop())
+            key = saved["group"], *kinds.pop()
+            b = self._bucket(key)
             if any((b[k] is None) != (saved[k] is None) or (b[k] is not None and b[k].shape != saved[k].shape)
                    for k in ("m", "v", "ms", "vs", "master")):
                 raise ValueError("the state is of other parameters")
-            wanted.append((b, saved))
-        for b, saved in wanted:
+            wanted[key] = b, saved
+        self._buckets = {key: b for key, (b, _) in wanted.items()}
+        for b, saved in wanted.values():
             # states without counts are of parameters that had a gradient in every step
             b["counts"] = list(saved.get("counts", [state["steps"]] * len(b["params"])))
             for k in ("m", "v", "ms", "vs", "master"):

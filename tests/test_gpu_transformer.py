@@ -207,6 +207,46 @@ def test_late_parameters_after_a_restart():
     assert all(torch.equal(a, b) for a, b in zip(params, again))
 
 
+def test_loading_a_state_before_the_first_step():
+    """Whatever the optimizer did before, it starts anew: as a fresh one does, bit for bit."""
+    params, grads = model_and_grads(torch.bfloat16)
+    start = P.AdamW(params, lr=1e-2, master=True).state_dict()
+    opt = P.AdamW(params, lr=1e-2, master=True)
+    for p, g in zip(params, grads[0]):
+        p.grad = g
+    opt.step()
+    opt.load_state_dict(start)
+    fresh = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    other = P.AdamW(fresh, lr=1e-2, master=True)
+    for o, ps in ((opt, params), (other, fresh)):
+        for p, g in zip(ps, grads[1]):
+            p.grad = g
+        o.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, fresh))
+    assert opt.state_bytes() == other.state_bytes()
+
+
+def test_a_state_without_counts():
+    """One saved when steps were counted together: every parameter had a gradient in each."""
+    params, grads = model_and_grads(torch.float32)
+    opt = P.AdamW(params, lr=1e-2)
+    for gs in grads[:2]:
+        for p, g in zip(params, gs):
+            p.grad = g
+        opt.step()
+    saved = copy.deepcopy(opt.state_dict())
+    for b in saved["buffers"]:
+        del b["counts"]
+    again = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    other = P.AdamW(again, lr=1.0)
+    other.load_state_dict(saved)
+    for p, o, g in zip(params, again, grads[2]):
+        p.grad, o.grad = g, g
+    opt.step()
+    other.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, again))
+
+
 def test_losses_of_plain_adamw_are_followed():
     """The same small regression by torch.optim.AdamW in 32 bits and by 8-bit moments: both come down alike."""
     torch.manual_seed(3)
