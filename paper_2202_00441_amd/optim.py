@@ -32,6 +32,21 @@ class AdamW(torch.optim.Optimizer):
         self._buckets = {}          # (group, dtype, device) -> buffers
         self._steps = 0
 
+    # Copies and pickles have the buffers and counts too; codes go as bytes, since a pickle of torch's
+    # does not hold tensors of an 8-bit floating-point type.
+    def __getstate__(self) -> dict:
+        own = {k: self.__dict__[k] for k in ("state_bits", "master", "_steps")}
+        return {**super().__getstate__(), **own, "_buckets": self._viewed(torch.uint8)}
+
+    def __setstate__(self, state: dict) -> None:
+        super().__setstate__(state)
+        self._buckets = self._viewed(_MOMENTS[8])
+
+    def _viewed(self, dtype) -> dict:
+        if self.state_bits != 8:
+            return self._buckets
+        return {key: {**b, "m": b["m"].view(dtype), "v": b["v"].view(dtype)} for key, b in self._buckets.items()}
+
     def _bucket(self, key) -> dict:
         """The buffers of a key: those there are, or new ones, which the caller keeps."""
         g, dtype, device = key

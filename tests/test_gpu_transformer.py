@@ -3,7 +3,9 @@ attention and torch's own activation rule, its cached generation agrees with the
 whole-sequence forward, and the optimizer class steps, saves and restores.
 """
 import copy
+import io
 import math
+import pickle
 
 import pytest
 import torch
@@ -245,6 +247,30 @@ def test_a_state_without_counts():
     opt.step()
     other.step()
     assert all(torch.equal(a, b) for a, b in zip(params, again))
+
+
+@pytest.mark.parametrize("bits", (8, 32))
+def test_optimizer_is_copied_and_pickled(bits):
+    params, grads = model_and_grads(torch.bfloat16)
+    opt = P.AdamW(params, lr=1e-2, state_bits=bits, master=True)
+
+    def step(o, gs):
+        for p, g in zip(o.param_groups[0]["params"], gs):
+            p.grad = g
+        o.step()
+
+    step(opt, grads[0])
+    file = io.BytesIO()
+    pickle.dump(opt, file)
+    file.seek(0)
+    others = copy.deepcopy(opt), pickle.load(file)
+    for g in grads[1:]:
+        for o in (opt, *others):
+            step(o, g)
+    for o in others:
+        copied = o.param_groups[0]["params"]
+        assert all(a is not b and torch.equal(a, b) for a, b in zip(params, copied))
+        assert o.state_bytes() == opt.state_bytes()
 
 
 def test_losses_of_plain_adamw_are_followed():
