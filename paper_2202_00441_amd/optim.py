@@ -77,7 +77,7 @@ class AdamW(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
-        self._steps += 1
+        step = self._steps + 1
         for g, group in enumerate(self.param_groups):
             kinds = dict.fromkeys((p.dtype, p.device) for p in group["params"] if p.grad is not None)
             for n, (dtype, device) in enumerate(kinds):
@@ -88,8 +88,9 @@ class AdamW(torch.optim.Optimizer):
                     these = [x if c == count else None for c, x in zip(counts, grads)]
                     adamw_step(b["params"], these, b["m"], b["v"], b["ms"], b["vs"], b["master"],
                                lr=group["lr"], beta1=group["betas"][0], beta2=group["betas"][1], eps=group["eps"],
-                               weight_decay=group["weight_decay"], step=count + 1, seed=(self._steps << 8) + 16 * g + n)
+                               weight_decay=group["weight_decay"], step=count + 1, seed=(step << 8) + 16 * g + n)
                     b["counts"] = [c + (x is not None) for c, x in zip(b["counts"], these)]
+        self._steps = step
         return loss
 
     def state_bytes(self) -> int:

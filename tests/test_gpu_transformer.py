@@ -273,6 +273,27 @@ def test_optimizer_is_copied_and_pickled(bits):
         assert o.state_bytes() == opt.state_bytes()
 
 
+def test_a_step_that_is_refused_does_not_count():
+    params, grads = model_and_grads(torch.float32)
+    again = [torch.nn.Parameter(p.detach().clone()) for p in params]
+    opt, other = P.AdamW(params, lr=1e-2), P.AdamW(again, lr=1e-2)
+    for p, o, g in zip(params, again, grads[0]):
+        p.grad, o.grad = g, g
+    opt.param_groups[0]["lr"] = -1.0
+    with pytest.raises(P.FewbitError):
+        opt.step()
+    opt.param_groups[0]["lr"] = 1e-2
+    opt.step()
+    other.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, again))
+    for p, o, g in zip(params, again, grads[1]):            # from moments rounded by the same dither
+        p.grad, o.grad = g, g
+    opt.step()
+    other.step()
+    assert all(torch.equal(a, b) for a, b in zip(params, again))
+    assert opt.state_dict()["steps"] == other.state_dict()["steps"] == 2
+
+
 def test_losses_of_plain_adamw_are_followed():
     """The same small regression by torch.optim.AdamW in 32 bits and by 8-bit moments: both come down alike."""
     torch.manual_seed(3)
