@@ -89,7 +89,8 @@ class Transformer(torch.nn.Module):
 
     def tables(self, device):
         if self._tables is None or self._tables[0].device != device:
-            self._tables = rope_tables(self.most, self.blocks[0].head_dim, device=device)
+            with torch.inference_mode(False):       # a later backward reads them too
+                self._tables = rope_tables(self.most, self.blocks[0].head_dim, device=device)
         return self._tables
 
     def forward(self, tokens):

@@ -88,6 +88,17 @@ def test_generation_agrees_with_the_whole_forward():
         model.extend(tokens[:, :0], cache)
 
 
+def test_training_after_generation_in_inference_mode():
+    """The tables made under torch.inference_mode() serve a training step afterwards."""
+    torch.manual_seed(2)
+    model = TR.Transformer(50, 256, 1, 4, 2, most=64).cuda().bfloat16()
+    tokens = torch.randint(0, 50, (2, 10), device="cuda")
+    with torch.inference_mode():
+        model.generate(tokens, 2)
+    model(tokens).float().sum().backward()
+    assert all(p.grad is not None for p in model.parameters())
+
+
 # ---------------------------------------------------------------- the optimizer class
 def model_and_grads(dtype, seed=0):
     g = torch.Generator(device="cuda").manual_seed(seed)
