@@ -152,10 +152,10 @@ def train(steps: int = 20, layers: int = 4, width: int = 1024, heads: int = 8, k
     generator = torch.Generator(device=device).manual_seed(seed)
     model = Transformer(tokens, width, layers, heads, kv_heads, bits=bits, most=length + 64).to(device=device, dtype=dtype)
     opt = AdamW(model.parameters(), lr=lr, betas=(0.9, 0.95), weight_decay=0.1, state_bits=state_bits, master=dtype != torch.float32)
-    losses, held, began = [], 0, 0.0
+    losses, held, began = [], 0, time.perf_counter()
     for i in range(steps):
         x = synthetic(batch, length, tokens, generator, device)
-        if i == 1:
+        if i < 2:                   # from the second step on, where there is one
             torch.cuda.synchronize()
             began = time.perf_counter()
         before = torch.cuda.memory_allocated()

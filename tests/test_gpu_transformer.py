@@ -6,6 +6,7 @@ import copy
 import io
 import math
 import pickle
+import time
 
 import pytest
 import torch
@@ -97,6 +98,13 @@ def test_training_after_generation_in_inference_mode():
         model.generate(tokens, 2)
     model(tokens).float().sum().backward()
     assert all(p.grad is not None for p in model.parameters())
+
+
+def test_time_of_a_single_step():
+    began = time.perf_counter()
+    r = TR.train(steps=1, layers=1, width=128, heads=2, kv_heads=1, batch=2, length=32, tokens=16)
+    assert 0.0 < r["ms_per_step"] <= (time.perf_counter() - began) * 1e3
+    assert TR.train(steps=0, layers=1, width=128, heads=2, kv_heads=1, batch=2, length=32, tokens=16)["losses"] == []
 
 
 # ---------------------------------------------------------------- the optimizer class
