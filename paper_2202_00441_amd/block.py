@@ -115,7 +115,7 @@ def qk_norm_rope_bwd(dq, dk, q, k, q_weight, k_weight, cos, sin, positions=None,
 class QkNormRope(torch.autograd.Function):
     @staticmethod
     def forward(ctx, q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved):
-        q, k = _rows(q), _rows(k)
+        q, k, q_weight, k_weight = (_rows(t) for t in (q, k, q_weight, k_weight))
         out = qk_norm_rope_fwd(q, k, q_weight, k_weight, cos, sin, positions, eps, interleaved)
         ctx.save_for_backward(q, k, q_weight, k_weight, cos, sin, positions)
         ctx.rest = eps, interleaved

@@ -132,6 +132,23 @@ def test_differentiable_call():
     assert torch.equal(grads[0], want[0]) and not grads[1].any() and not grads[3].any()
 
 
+def test_differentiable_call_takes_weights_anywhere():
+    """Weights that are views into one flat buffer, off any 16 bytes, or strided."""
+    q, k, qw, kw, dq, dk, cos, sin = inputs(BF16, 2, 30, 4, 2, 128, 128)
+    flat = torch.zeros(300, dtype=BF16, device="cuda")
+    flat[3:131], flat[131:259] = qw, kw
+    flat.requires_grad_()
+    wide = torch.stack((qw, kw), 1).requires_grad_()
+    want = P.qk_norm_rope_fwd(q, k, qw, kw, cos, sin)
+    grads = P.qk_norm_rope_bwd(dq, dk, q, k, qw, kw, cos, sin)[2:]
+    for base, a, b in ((flat, flat[3:131], flat[131:259]), (wide, wide[:, 0], wide[:, 1])):
+        y = P.qk_norm_rope(q, k, a, b, cos, sin)
+        assert all(torch.equal(s, t) for s, t in zip(y, want))
+        (g,) = torch.autograd.grad(y, base, (dq, dk))
+        got = (g[3:131], g[131:259]) if base is flat else (g[:, 0], g[:, 1])
+        assert all(torch.equal(s, t.to(BF16)) for s, t in zip(got, grads))
+
+
 @pytest.mark.parametrize("inter", (False, True))
 def test_gradient_against_differences(inter):
     """fp32, central differences of the formula in 64 bits along a random direction: exact to 1e-8 with h = 1e-5; the
