@@ -1012,6 +1012,7 @@ __device__ __forceinline__ void fit_half(f32x16& ds, f32x16 (&sums)[D / 32], int
 // delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
 // type for its product with K.  Bound as the forward is: 4 x 4096 rows, 16 heads of 128 in
 // bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 493 us, matrix pipes busy for 48%.
+constexpr int kFewKeys = 16;
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1048,10 +1049,6 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   }
   float lse = there ? a.lse[stat] : -INFINITY;
   lse = lse == -INFINITY ? INFINITY : lse * kLog2e;           // of an empty row no key is seen
-  if (there && lane < 32 && part == 0) {
-    a.stats[stat] = lse - kLift;
-    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift);
-  }
 
   const Range own = keys_of(a, s, pos);
   const int w0 = min(first + wave * kRowsWave, rows - 1), w1 = min(first + wave * kRowsWave + kRowsWave, rows) - 1;
@@ -1065,46 +1062,72 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   const Rows<DT, D, kKeys, kWaves> keys(stage, kb, a.ks[1], s.nk - 1), values(stage, vb, a.vs[1], s.nk - 1);
   const RowReader<DT, D> rows_at;
   const ColumnReader<DT, D> columns_at;
-  f32x16 dq[D / 32] = {};
   const float scale2 = a.scale * kLog2e;
+  const auto issue = [&](Pair<T, kKeys * D>& to, int k0) {
+    keys.issue(stage, to.a, k0);
+    values.issue(stage, to.b, k0);
+  };
+  // S (-infinity where the mask hides it) and dP of 32 keys of a tile
+  const auto products = [&](const Pair<T, kKeys * D>& in, int k0, int u, f32x16& p, f32x16& dp) __attribute__((always_inline)) {
+    const auto rr = rows_at.here();
+    p = dp = f32x16{};
+#pragma unroll
+    for (int step = 0; step < D / 16; ++step) {
+      p = Mma<DT>::mul(rr.read(in.a, 32 * u, step), q[step], p);
+      dp = Mma<DT>::mul(rr.read(in.b, 32 * u, step), dout[step], dp);
+    }
+    if (k0 < every.lo || k0 + kKeys > every.hi) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
+        if (key < own.lo || key >= own.hi) p[i] = -INFINITY;
+      }
+    }
+  };
+  // Rows that see few keys: the rounding of out is in delta, and not small beside their dS, which is
+  // 0 where a row sees one key.  Their delta is sum_j P_ij dP_ij, formed ahead.
+  const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
+  if (least.hi - least.lo <= kFewKeys && seen.lo < seen.hi) {
+    float sum = 0.0f;
+    walk(seen.lo / kKeys * kKeys, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
+      if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
+#pragma unroll
+      for (int u = 0; u < kKeys / 32; ++u) {
+        f32x16 p, dp;
+        products(in, k0, u, p, dp);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(p[i] * scale2 - lse) * dp[i];
+      }
+    });
+    const Two both = halves32(sum);
+    delta = both.a + both.b;
+    __syncthreads();                    // the tiles' buffers are free
+  }
+  if (there && lane < 32 && part == 0) {
+    a.stats[stat] = lse - kLift;
+    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift);
+  }
+  f32x16 dq[D / 32] = {};
   int lift = DT == FEWBIT_F16 ? kHalfLift : 0;
-  walk(all.lo, kKeys, all.hi, buf0, buf1,
-       [&](Pair<T, kKeys * D>& to, int k0) {
-         keys.issue(stage, to.a, k0);
-         values.issue(stage, to.b, k0);
-       },
-       [&](const Pair<T, kKeys * D>& in, int k0) {
-         if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
-         const auto rr = rows_at.here();
-         const auto cr = columns_at.here();
-         const bool masked = k0 < every.lo || k0 + kKeys > every.hi;
+  walk(all.lo, kKeys, all.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
+    if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
+    const auto cr = columns_at.here();
 #pragma unroll
-         for (int u = 0; u < kKeys / 32; ++u) {
-           const float from = lse - lift;
-           f32x16 p = {}, dp = {};
+    for (int u = 0; u < kKeys / 32; ++u) {
+      const float from = lse - lift;
+      f32x16 p, dp;
+      products(in, k0, u, p, dp);
 #pragma unroll
-           for (int step = 0; step < D / 16; ++step) {
-             p = Mma<DT>::mul(rr.read(in.a, 32 * u, step), q[step], p);
-             dp = Mma<DT>::mul(rr.read(in.b, 32 * u, step), dout[step], dp);
-           }
-           if (masked) {
+      for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - from) * (dp[i] - delta);
+      if constexpr (DT == FEWBIT_F16) fit_half<D>(p, dq, lift);
 #pragma unroll
-             for (int i = 0; i < 16; ++i) {
-               const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
-               if (key < own.lo || key >= own.hi) p[i] = -INFINITY;
-             }
-           }
+      for (int step = 0; step < 2; ++step) {
+        const V8 ds = narrow<DT>(p, step);
 #pragma unroll
-           for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - from) * (dp[i] - delta);
-           if constexpr (DT == FEWBIT_F16) fit_half<D>(p, dq, lift);
-#pragma unroll
-           for (int step = 0; step < 2; ++step) {
-             const V8 ds = narrow<DT>(p, step);
-#pragma unroll
-             for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), ds, dq[t]);
-           }
-         }
-       });
+        for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), ds, dq[t]);
+      }
+    }
+  });
   const float scale = ldexpf(a.scale, -lift);
   if (slice.used == 1) {
     __syncthreads();                    // the tiles' buffers are free

@@ -162,6 +162,28 @@ def test_large_gradients_in_fp16(sq, sk, d, causal):
     check(q * 0.01, k * 0.01, v * 100, do * 2000, causal=causal)
 
 
+@pytest.mark.parametrize("dtype", (BF16, F16))
+@pytest.mark.parametrize("b,sq,sk,hq,hkv,d,causal,window", [
+    (2, 30, 1, 2, 1, 64, False, 0), (1, 300, 300, 4, 2, 128, True, 1), (3, 70, 70, 8, 1, 40, True, 0), (1, 50, 20, 2, 2, 80, True, 0),
+    (1, 2100, 2100, 1, 1, 64, True, 0)])
+def test_gradient_of_rows_that_see_one_key(dtype, b, sq, sk, hq, hkv, d, causal, window):
+    """Softmax over one key is 1 whatever the scores: such a row gives queries and keys no gradient.  dP and delta are fp32
+    sums of d terms and P is off by what lse is, so 1e-5 of the sum of their terms' magnitudes."""
+    q, k, v, do = make(dtype, b, sq, sk, hq, hkv, d)
+    kw = {"causal": causal, "window": window}
+    out, lse = P.attention_fwd(q, k, v, **kw)
+    i = torch.arange(sq, device="cuda") + sk - sq                     # the key where a query stands
+    last = i.clamp(max=sk - 1) if causal else torch.full_like(i, sk - 1)
+    one = last == (i - window + 1).clamp(min=0) if window else last == 0
+    assert one.any()
+    do = do * one[None, :, None, None].to(dtype)                      # the other rows have none to give
+    dq, dk, _ = P.attention_bwd(do, q, k, v, out, lse, **kw)
+    most = [x.double().abs().amax() for x in (q, k)]
+    terms = float(do.double().abs().sum(-1).amax() * v.double().abs().amax()) / math.sqrt(d)
+    assert float(dq.double().abs().amax()) <= 1e-5 * terms * float(most[1])
+    assert float(dk.double().abs().amax()) <= 1e-5 * terms * float(most[0]) * int(one.sum()) * (hq // hkv)
+
+
 def test_scale():
     q, k, v, do = make(BF16, 1, 70, 90, 2, 2, 64)
     check(q, k, v, do, scale=0.7)
