@@ -1084,8 +1084,9 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
       }
     }
   };
-  // Rows that see few keys: the rounding of out is in delta, and not small beside their dS, which is
-  // 0 where a row sees one key.  Their delta is sum_j P_ij dP_ij, formed ahead.
+  // Rows that see few keys: the rounding of out is in delta, and the larger beside their dS the fewer
+  // they are.  Their delta is sum_j P_ij dP_ij, formed ahead.  (16 causal rows in bf16: dQ is 0.0030 of
+  // its norm off with delta from out, 0.0023 so, its rounding alone 0.0017.)
   const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
   if (least.hi - least.lo <= kFewKeys && seen.lo < seen.hi) {
     float sum = 0.0f;

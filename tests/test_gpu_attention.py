@@ -184,6 +184,23 @@ def test_gradient_of_rows_that_see_one_key(dtype, b, sq, sk, hq, hkv, d, causal,
     assert float(dk.double().abs().amax()) <= 1e-5 * terms * float(most[0]) * int(one.sum()) * (hq // hkv)
 
 
+@pytest.mark.parametrize("dtype", (BF16, F16))
+@pytest.mark.parametrize("b,n,hq,hkv,d,window", [(16, 16, 8, 8, 64, 0), (8, 24, 16, 4, 128, 0), (8, 40, 16, 16, 80, 8), (2, 200, 16, 16, 64, 2)])
+def test_gradients_of_rows_that_see_few_keys(dtype, b, n, hq, hkv, d, window):
+    """In norm, dQ is rounded twice, in dS and itself, by the same relative amount, and dK in fp16 a third time, in the P
+    that dS is formed from: sqrt(2) and sqrt(3) of the exact gradient's own rounding, and 6% for what fp32 adds.  Delta
+    from the rounded output would be another, the larger the fewer keys a row sees."""
+    q, k, v, do = make(dtype, b, n, n, hq, hkv, d)
+    kw = {"causal": True, "window": window}
+    out, lse = P.attention_fwd(q, k, v, **kw)
+    grads = P.attention_bwd(do, q, k, v, out, lse, **kw)
+    refs = [reference(q[i], k[i], v[i], do[i], True, window, 1 / math.sqrt(d))[0] for i in range(b)]
+    for name, got, roundings in (("dq", grads[0], 2), ("dk", grads[1], 3 if dtype is F16 else 2)):
+        want = torch.stack([r[name][0] for r in refs])
+        rounding = (want.to(dtype).double() - want).norm()
+        assert (got.double() - want).norm() <= 1.06 * math.sqrt(roundings) * rounding, name
+
+
 def test_scale():
     q, k, v, do = make(BF16, 1, 70, 90, 2, 2, 64)
     check(q, k, v, do, scale=0.7)
