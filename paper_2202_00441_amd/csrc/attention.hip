@@ -333,11 +333,11 @@ __device__ __forceinline__ void landed() {
 
 // Walks tiles at, at + step, .. < end through two buffers: while one is worked on the
 // next tile comes into the other.  (Buffers are apart so that the compiler does not make
-// reads of one wait for loads into the other.)
+// reads of one wait for loads into the other.)  `loaded`: the first tile is in its buffer.
 template <class Buffer, class Issue, class Work>
-__device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work) {
+__device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work, bool loaded = false) {
   if (at >= end) return;
-  issue(a, at);
+  if (!loaded) issue(a, at);
   for (; at < end; at += 2 * step) {
     landed<0>();
     __syncthreads();
@@ -1068,15 +1068,15 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
     values.issue(stage, to.b, k0);
   };
   // S (-infinity where the mask hides it) and dP of 32 keys of a tile
-  const auto products = [&](const Pair<T, kKeys * D>& in, int k0, int u, f32x16& p, f32x16& dp) __attribute__((always_inline)) {
-    const auto rr = rows_at.here();
+  const auto products = [&](const Pair<T, kKeys * D>& in, const RowReader<DT, D>& rr, int k0, int u, bool masked, f32x16& p,
+                            f32x16& dp) __attribute__((always_inline)) {
     p = dp = f32x16{};
 #pragma unroll
     for (int step = 0; step < D / 16; ++step) {
       p = Mma<DT>::mul(rr.read(in.a, 32 * u, step), q[step], p);
       dp = Mma<DT>::mul(rr.read(in.b, 32 * u, step), dout[step], dp);
     }
-    if (k0 < every.lo || k0 + kKeys > every.hi) {
+    if (masked) {
 #pragma unroll
       for (int i = 0; i < 16; ++i) {
         const int key = k0 + 32 * u + key_of(i) + lane / 32 * 4;
@@ -1084,18 +1084,24 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
       }
     }
   };
+  const auto hidden = [&](int k0) { return k0 < every.lo || k0 + kKeys > every.hi; };      // from some row of the wave
   // Rows that see few keys: the rounding of out is in delta, and the larger beside their dS the fewer
   // they are.  Their delta is sum_j P_ij dP_ij, formed ahead.  (16 causal rows in bf16: dQ is 0.0030 of
-  // its norm off with delta from out, 0.0023 so, its rounding alone 0.0017.)
+  // its norm off with delta from out, 0.0023 so, its rounding alone 0.0017.  The backward of 8 x 64
+  // causal rows, 12 heads of 64, takes 14.6 us so and 13.4 without; of long ones the same.)
   const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
-  if (least.hi - least.lo <= kFewKeys && seen.lo < seen.hi) {
+  const bool few = least.hi - least.lo <= kFewKeys && seen.lo < seen.hi;
+  const int begin = seen.lo / kKeys * kKeys;
+  if (few) {
     float sum = 0.0f;
-    walk(seen.lo / kKeys * kKeys, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
+    walk(begin, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
       if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
+      const auto rr = rows_at.here();
+      const bool masked = hidden(k0);
 #pragma unroll
       for (int u = 0; u < kKeys / 32; ++u) {
         f32x16 p, dp;
-        products(in, k0, u, p, dp);
+        products(in, rr, k0, u, masked, p, dp);
 #pragma unroll
         for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(p[i] * scale2 - lse) * dp[i];
       }
@@ -1112,12 +1118,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   int lift = DT == FEWBIT_F16 ? kHalfLift : 0;
   walk(all.lo, kKeys, all.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
     if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
+    const auto rr = rows_at.here();
     const auto cr = columns_at.here();
+    const bool masked = hidden(k0);
 #pragma unroll
     for (int u = 0; u < kKeys / 32; ++u) {
       const float from = lse - lift;
       f32x16 p, dp;
-      products(in, k0, u, p, dp);
+      products(in, rr, k0, u, masked, p, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - from) * (dp[i] - delta);
       if constexpr (DT == FEWBIT_F16) fit_half<D>(p, dq, lift);
@@ -1128,7 +1136,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
         for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), ds, dq[t]);
       }
     }
-  });
+  }, few && seen.hi - begin <= kKeys);        // a single tile is still there
   const float scale = ldexpf(a.scale, -lift);
   if (slice.used == 1) {
     __syncthreads();                    // the tiles' buffers are free
