@@ -1443,6 +1443,12 @@ Shares shares_of(const fewbit_attn* a) {
   if (a->cu_q || a->batch == 0 || rows == 0 || rows > kRowsWave || a->rows_k == 0) return {};
   const int64_t cus = device_cus(), passes = a->batch * over(a->rows_k + 31, kKeysSplit);
   if (a->batch >= int64_t{1} << 24 || passes >= int64_t{1} << 31) return {};
+  // Every workgroup here reads the lengths of all sequences, and so does the join's for every
+  // row.  Where a CU gets four sequences and key heads the tiled kernel, a workgroup to each,
+  // ends as evenly: one row on 256, 1024, 4096 and 16384 caches of up to 1024, 512, 256 and 128
+  // keys, 16 heads to 4 of 128: 69, 137, 301 and 819 us, here 74, 202, 1171 and 13871; on 128 of
+  // up to 4096 129, here 110.
+  if (a->k_len && a->batch * a->heads_kv >= 4 * cus) return {};
   // As many workgroups as the chip holds at once, or as it has CUs where that leaves one
   // pass to each (one row on 16000 keys, 16 heads to 4: 20 us in 504 workgroups, 17 in 252);
   // units of four passes are not worth a join (300 keys, 12 heads: 8.9 us joined, 7.1 whole).

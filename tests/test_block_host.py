@@ -136,6 +136,13 @@ def test_attention_strides_are_not_negative():
                 assert attn_fwd(attn(**{name: stride})) == E_INVALID, (name, i)
 
 
+def test_many_caches_are_not_divided():
+    """Shares of many caches with lengths of their own would have to be found from all lengths by each workgroup: where
+    every CU has several caches they are left whole, and need no room for joins."""
+    few, many = attn(batch=16, rows_q=1, rows_k=4096, k_len=16), attn(batch=4096, rows_q=1, rows_k=4096, k_len=16)
+    assert LIB.fewbit_attn_workspace(C.byref(few), 0) > 0 == LIB.fewbit_attn_workspace(C.byref(many), 0)
+
+
 def test_attention_grids_past_a_launch():
     """A launch has fewer than 2^32 threads.  The kernel for dK and dV has 512 to a workgroup, here of one key head
     each, 2^23 of them: refused before the kernel for dQ, of 256 threads, is launched.  Sizes whose products pass 64

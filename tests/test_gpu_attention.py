@@ -223,6 +223,18 @@ def test_cache(dtype, b, sq, hq, hkv, d, sk, lens, window):
     check(q, k, v, do, causal=True, window=window, k_len=list(lens))
 
 
+@pytest.mark.parametrize("dtype,b,hq,hkv,d,sq,window", [(BF16, 70, 32, 16, 128, 1, 0), (F16, 90, 12, 12, 40, 1, 50), (BF16, 130, 16, 8, 64, 3, 0)])
+def test_many_caches(dtype, b, hq, hkv, d, sq, window):
+    """Enough caches of different lengths, some of them empty, to give every CU several."""
+    sk = 200
+    q, k, v, do = make(dtype, b, sq, sk, hq, hkv, d)
+    lens = [(37 * i) % (sk + 1) for i in range(b)]
+    there = torch.arange(sk, device="cuda") < torch.tensor(lens, device="cuda")[:, None]
+    for x in (k, v):
+        x[~there] = math.nan
+    check(q, k, v, do, causal=True, window=window, k_len=lens, back=False)
+
+
 @pytest.mark.parametrize("lens", (False, True))
 def test_many_short_sequences(lens):
     """Windows of a few rows: 2^24 rows of a sequence and key head, more than a launch has workgroups."""
