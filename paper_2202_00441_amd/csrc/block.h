@@ -171,6 +171,14 @@ __device__ __forceinline__ float across(float x, F f) {
   return x;
 }
 
+// The sum over a wave, the same in every lane.
+__device__ __forceinline__ int wave_sum(int x) {
+  const float sum = across<6>(__builtin_bit_cast(float, x), [](float p, float q) {
+    return __builtin_bit_cast(float, __builtin_bit_cast(int, p) + __builtin_bit_cast(int, q));
+  });
+  return __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, sum));
+}
+
 // x / n for 0 <= x < 2^31: the high half of a product with 2^32 / n rounded up is at
 // most one too many.
 struct Divisor {
