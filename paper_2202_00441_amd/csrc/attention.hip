@@ -348,11 +348,11 @@ __device__ __forceinline__ void landed() {
 
 // Walks tiles at, at + step, .. < end through two buffers: while one is worked on the
 // next tile comes into the other.  (Buffers are apart so that the compiler does not make
-// reads of one wait for loads into the other.)  `loaded`: the first tile is in its buffer.
+// reads of one wait for loads into the other.)
 template <class Buffer, class Issue, class Work>
-__device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work, bool loaded = false) {
+__device__ __forceinline__ void walk(int at, int step, int end, Buffer& a, Buffer& b, Issue issue, Work work) {
   if (at >= end) return;
-  if (!loaded) issue(a, at);
+  issue(a, at);
   for (; at < end; at += 2 * step) {
     landed<0>();
     __syncthreads();
@@ -1100,38 +1100,77 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
     }
   };
   const auto hidden = [&](int k0) { return k0 < every.lo || k0 + kKeys > every.hi; };      // from some row of the wave
-  // Rows that see few keys: the rounding of out is in delta, and the larger beside their dS the fewer
-  // they are.  Their delta is sum_j P_ij dP_ij, formed ahead.  (16 causal rows in bf16: dQ is 0.0030 of
-  // its norm off with delta from out, 0.0023 so, its rounding alone 0.0017.  The backward of 8 x 64
-  // causal rows, 12 heads of 64, takes 14.6 us so and 13.4 without; of long ones the same.)
-  const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
-  const bool few = least.hi - least.lo <= kFewKeys && seen.lo < seen.hi;
-  const int begin = seen.lo / kKeys * kKeys;
-  if (few) {
-    float sum = 0.0f;
-    walk(begin, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
-      if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
-      const auto rr = rows_at.here();
-      const bool masked = hidden(k0);
-#pragma unroll
-      for (int u = 0; u < kKeys / 32; ++u) {
-        f32x16 p, dp;
-        products(in, rr, k0, u, masked, p, dp);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(p[i] * scale2 - lse) * dp[i];
-      }
-    });
-    const Two both = halves32(sum);
-    delta = both.a + both.b;
-    __syncthreads();                    // the tiles' buffers are free
-  }
-  if (there && lane < 32 && part == 0) {
-    a.stats[stat] = lse - kLift;
-    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift);
-  }
   f32x16 dq[D / 32] = {};
   int lift = DT == FEWBIT_F16 ? kHalfLift : 0;
-  walk(all.lo, kKeys, all.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
+  // dS (times 2^lift) of 32 keys into dQ
+  const auto add = [&](const Pair<T, kKeys * D>& in, const ColumnReader<DT, D>& cr, int u, f32x16& ds) __attribute__((always_inline)) {
+    if constexpr (DT == FEWBIT_F16) fit_half<D>(ds, dq, lift);
+#pragma unroll
+    for (int step = 0; step < 2; ++step) {
+      const V8 n = narrow<DT>(ds, step);
+#pragma unroll
+      for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), n, dq[t]);
+    }
+  };
+  // Rows that see few keys: the rounding of out is in delta, and the larger beside their dS the fewer
+  // they are.  Where a workgroup's first row sees at most kFewKeys, delta is sum_j P_ij dP_ij for all
+  // rows that see no key past the first tile, whose P and dP stay in registers meanwhile; with a
+  // window as small, for all rows, formed ahead.  (16 causal rows in bf16: dQ is 0.0030 of its norm
+  // off with delta from out, 0.0023 so, its rounding alone 0.0017; no shape takes longer for it.)
+  const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
+  const int begin = seen.lo / kKeys * kKeys;
+  int next = all.lo;
+  if (least.hi - least.lo <= kFewKeys && next == begin && next < all.hi) {
+    if (a.window > 0 && a.window <= kFewKeys) {
+      float sum = 0.0f;
+      walk(begin, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
+        if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
+        const auto rr = rows_at.here();
+        const bool masked = hidden(k0);
+#pragma unroll
+        for (int u = 0; u < kKeys / 32; ++u) {
+          f32x16 p, dp;
+          products(in, rr, k0, u, masked, p, dp);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum += __builtin_amdgcn_exp2f(p[i] * scale2 - lse) * dp[i];
+        }
+      });
+      const Two both = halves32(sum);
+      delta = both.a + both.b;
+    } else {
+      next += kKeys;
+      issue(buf0, begin);
+      landed<0>();
+      __syncthreads();
+      if (any.lo < next && any.hi > begin) {
+        f32x16 p[kKeys / 32], dp[kKeys / 32];
+        const auto rr = rows_at.here();
+        const auto cr = columns_at.here();
+        const bool masked = hidden(begin);
+        float sum = 0.0f;
+#pragma unroll
+        for (int u = 0; u < kKeys / 32; ++u) {
+          products(buf0, rr, begin, u, masked, p[u], dp[u]);
+#pragma unroll
+          for (int i = 0; i < 16; ++i) {
+            p[u][i] = __builtin_amdgcn_exp2f(p[u][i] * scale2 - lse);
+            sum += p[u][i] * dp[u][i];
+          }
+        }
+        const Two both = halves32(sum);
+        if (own.hi <= next) delta = both.a + both.b;
+#pragma unroll
+        for (int u = 0; u < kKeys / 32; ++u) {
+          const float up = DT == FEWBIT_F16 ? ldexpf(1.0f, lift) : 1.0f;
+#pragma unroll
+          for (int i = 0; i < 16; ++i) p[u][i] *= (dp[u][i] - delta) * up;
+          add(buf0, cr, u, p[u]);
+        }
+      }
+    }
+    __syncthreads();                    // the tiles' buffers are free
+  }
+  walk(next, kKeys, all.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
     if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
     const auto rr = rows_at.here();
     const auto cr = columns_at.here();
@@ -1143,15 +1182,13 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
       products(in, rr, k0, u, masked, p, dp);
 #pragma unroll
       for (int i = 0; i < 16; ++i) p[i] = __builtin_amdgcn_exp2f(p[i] * scale2 - from) * (dp[i] - delta);
-      if constexpr (DT == FEWBIT_F16) fit_half<D>(p, dq, lift);
-#pragma unroll
-      for (int step = 0; step < 2; ++step) {
-        const V8 ds = narrow<DT>(p, step);
-#pragma unroll
-        for (int t = 0; t < D / 32; ++t) dq[t] = Mma<DT>::mul(cr.read(in.a, 32 * u + 16 * step, t), ds, dq[t]);
-      }
+      add(in, cr, u, p);
     }
-  }, few && seen.hi - begin <= kKeys);        // a single tile is still there
+  });
+  if (there && lane < 32 && part == 0) {
+    a.stats[stat] = lse - kLift;
+    a.stats[a.stats_delta + stat] = ldexpf(delta, -kLift);
+  }
   const float scale = ldexpf(a.scale, -lift);
   if (slice.used == 1) {
     __syncthreads();                    // the tiles' buffers are free
