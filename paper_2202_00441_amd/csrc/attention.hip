@@ -1027,7 +1027,7 @@ __device__ __forceinline__ void fit_half(f32x16& ds, f32x16 (&sums)[D / 32], int
 // delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
 // type for its product with K.  Bound as the forward is: 4 x 4096 rows, 16 heads of 128 in
 // bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 493 us, matrix pipes busy for 48%.
-constexpr int kFewKeys = 16;
+constexpr int kFewKeys = 16, kThinWindow = 4;
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1115,13 +1115,14 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
   // Rows that see few keys: the rounding of out is in delta, and the larger beside their dS the fewer
   // they are.  Where a workgroup's first row sees at most kFewKeys, delta is sum_j P_ij dP_ij for all
   // rows that see no key past the first tile, whose P and dP stay in registers meanwhile; with a
-  // window as small, for all rows, formed ahead.  (16 causal rows in bf16: dQ is 0.0030 of its norm
-  // off with delta from out, 0.0023 so, its rounding alone 0.0017; no shape takes longer for it.)
+  // window of at most kThinWindow, for all rows, formed ahead.  (16 causal rows in bf16: dQ is 0.0030
+  // of its norm off with delta from out, 0.0023 so, its rounding alone 0.0017.  Only the thin windows
+  // take longer for it: 4 x 4096 rows, 16 heads of 128, forward apart, 251 us, else 226.)
   const Range seen = keys_of_group(a, s, first, rows), least = keys_of(a, s, a.by_g.divide(first));
   const int begin = seen.lo / kKeys * kKeys;
   int next = all.lo;
   if (least.hi - least.lo <= kFewKeys && next == begin && next < all.hi) {
-    if (a.window > 0 && a.window <= kFewKeys) {
+    if (a.window > 0 && a.window <= kThinWindow) {
       float sum = 0.0f;
       walk(begin, kKeys, seen.hi, buf0, buf1, issue, [&](const Pair<T, kKeys * D>& in, int k0) {
         if (k0 + kKeys <= any.lo || k0 >= any.hi) return;
