@@ -56,12 +56,17 @@ extern "C" {
  * are refused (the backward takes 512 for 128 or 256 keys of a key head).
  *
  * Values of k and v that no row of a sequence sees but that lie inside it
- * have to be finite.
+ * have to be finite, and so does dout: masked products are 0 times them.
  *
- * Sums, softmax statistics and gradients are accumulated in fp32; p and its
- * gradient are rounded to the storage type before the products with v, k and
- * q, as the matrix instructions take them.  Results do not depend on the
- * order in which anything runs.
+ * Sums, softmax statistics and gradients are accumulated in fp32.  What the
+ * matrix instructions take is rounded to 16 bits once: p and its gradient ds =
+ * p (<dout_i, v_j> - <dout_i, out_i>) to the storage type before the products
+ * with v and dout, and with k and q.  For dk the p in ds has the 11 bits of
+ * fp16, whatever the type, and is 0 below 2^-39.  In fp16 ds is multiplied by
+ * a power of two of each row's (dq) or key's (dk) own first, so that small
+ * gradients keep their bits and large ones do not pass its range.  <dout_i,
+ * out_i> is of out as it was rounded, but for rows that see few keys.  Results
+ * do not depend on the order in which anything runs.
  */
 typedef struct fewbit_attn {
     int32_t dtype;                /* FEWBIT_F16 / FEWBIT_BF16                  */

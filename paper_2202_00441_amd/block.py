@@ -7,8 +7,8 @@ adamw_step are the raw calls, in the library's HIP kernels on the current
 stream; they check every tensor (device, dtype, shape, layout) and raise
 TypeError or ValueError before anything is launched.  attention and
 qk_norm_rope are the same as differentiable functions: they keep their inputs
-(attention also its output and one number per row) and take any layout, copying
-tensors whose rows the kernels cannot read.
+(attention also its output and one number per row), take any layout, copying
+tensors whose rows the kernels cannot read, and form the gradients of all of them.
 """
 from __future__ import annotations
 
@@ -30,8 +30,9 @@ def attention_fwd(q, k, v, causal=False, window=0, scale=None, k_len=None, cu_q=
 
     q [batch, rows, heads, d], k and v [batch, keys, kv_heads, d], or, packed,
     [rows, heads, d] with cu_q and cu_k (int32, one entry more than sequences)
-    telling where sequences begin; fp16 or bf16, d a multiple of 8 up to 128.
-    Heads of q share heads of k and v in runs.  Any strides; rows contiguous.
+    telling where sequences begin (one below one before it counts as that one);
+    fp16 or bf16, d a multiple of 8 up to 128.  Heads of q share heads of k and v
+    in runs.  Any strides; rows contiguous, from multiples of 16 bytes on.
 
     causal: the last query sees the last key, each earlier one a key less.
     window (with causal): a query sees that many keys at most.  k_len (int32,
@@ -97,7 +98,8 @@ def qk_norm_rope_fwd(q, k, q_weight, k_weight, cos, sin, positions=None, eps=1e-
 
     q [batch, tokens, heads, d], k [batch, tokens, kv_heads, d] (or without the
     batch), fp32, fp16 or bf16 with weights [d] of the same type; d and the
-    rotated part multiples of 16, d up to 256; any strides, rows contiguous.
+    rotated part multiples of 16, d up to 256; any strides, rows contiguous,
+    from multiples of 16 bytes on.
     cos, sin: fp32 [positions, rotated elements / 2].  positions: int64
     [batch, tokens] or [tokens]; without, a token's place in its sequence.  A
     position that the tables do not hold gives NaN.  interleaved: the pairs are

@@ -19,6 +19,9 @@
 // in LDS by the transposing load, four rows at a time, in that order.
 //
 // Tiles lie in LDS row-major in 16-byte chunks, chunk c of row r at c ^ f(r) (swizzle).
+//
+// Times of long walks differ by 5% from card to card, with the clock that the matrix cores
+// hold: ranges are those of several.
 #include <algorithm>
 #include <type_traits>
 
@@ -455,7 +458,8 @@ __device__ __forceinline__ void load_rows(const typename Mma<DT>::T* row, int d,
 // `scale`, to `offset` elements past `base`, the lane's row's; the first `rows` rows are there.
 // They go through 32 D elements of LDS of the wave's own, so that a store has whole rows, 16
 // bytes a lane: a lane's own elements lie in fours with another lane's between.  16 x 2048
-// rows, 16 heads of 128, on 64 keys: 71 us, stored from the registers 87.
+// rows, 16 heads of 128, on 64 keys: 71 us, stored from the registers 87; 16 x 2048 causal rows,
+// forward 373 us to 381, dK and dV 831 to 838, dQ 510 to 503.
 template <int DT, int D>
 __device__ __forceinline__ void store_rows(typename Mma<DT>::T* lds, int d, const f32x16 (&x)[D / 32], float scale, typename Mma<DT>::T* base,
                                            uint32_t offset, int rows) {
@@ -598,10 +602,10 @@ __device__ __forceinline__ void store_queries(const Args& a, const Seq& s, void*
 // tile of K and V (32 KB at D = 128) serves all four waves, and two workgroups share a CU.
 // The maximum follows only when a row's scores pass it by 2^8, so the sums seldom have to
 // be scaled.  Bound by the products and the exponentials between them, which two waves a
-// SIMD overlap in part: 4 x 4096 rows, 16 heads of 128 in bf16, 528 us, 1040 TFLOP/s (a library
-// product of 8192^3 reaches 1160); 16 x 2048, causal, 357 us, matrix pipes busy for 44% of the
-// cycles.  Of a workgroup's time 10 us pass outside the tiles.  Forming the
-// next tile's scores beside this tile's exponentials was slower, 625 us to 560.
+// SIMD overlap in part: 4 x 4096 rows, 16 heads of 128 in bf16, 554 to 579 us, 950 to 990
+// TFLOP/s (a library product of 8192^3 reaches 1160), matrix pipes busy for 53% of the cycles;
+// 16 x 2048, causal, 358 to 376 us, 45%.  Of a workgroup's time 10 us pass outside the tiles.
+// Forming the next tile's scores beside this tile's exponentials was slower, 625 us to 560.
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_fwd_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -753,10 +757,10 @@ __device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
   return units;
 }
 
-// Bound by HBM: one row on 64 caches of 8192 keys, 16 heads to 4 of 128 in bf16, 100 us,
-// 5.4 TB/s.  Each wave has two buffers of its own, so that it waits for no other.  Keys are
-// read once and not kept in the caches (64 caches of 8192 keys, 16 heads to 4, more of them
-// than the memory-side cache holds: 177 us, else 200).
+// Bound by HBM: one row on 64 caches of up to 8192 keys, 270000 in all, 16 heads to 4 of 128
+// in bf16, 553 MB, 100 us, 5.5 TB/s.  Each wave has two buffers of its own, so that it waits for no other.  Keys are
+// read once and not kept in the caches (64 caches of 8192 keys each, more than the memory-side
+// cache holds: 177 us, else 200).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1026,7 +1030,8 @@ __device__ __forceinline__ void fit_half(f32x16& ds, f32x16 (&sums)[D / 32], int
 // dQ: 128 rows of Q and dO to a workgroup, which walks tiles of 64 keys as the forward does;
 // delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
 // type for its product with K.  Bound as the forward is: 4 x 4096 rows, 16 heads of 128 in
-// bf16, 714 us, 1150 TFLOP/s; 16 x 2048, causal, 493 us, matrix pipes busy for 48%.
+// bf16, 742 to 791 us, 1040 to 1110 TFLOP/s, matrix pipes busy for 58%; 16 x 2048, causal, 488
+// to 516 us, 46%.
 constexpr int kFewKeys = 16, kThinWindow = 4;
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
@@ -1206,11 +1211,10 @@ __global__ __launch_bounds__(kThreads, 2) void attn_dq_kernel(const Args a) {
 // of a SIMD are always one of either kind.  The tiles come through three buffers.  P and
 // dS are rounded to the storage type for their products with dO and Q.
 // Bound by the products, the hand-over between them and 13 us of a workgroup's time outside
-// the tiles, one workgroup to a CU: 4 x 4096 rows, 16 heads of 128 in bf16, 1160 us, 950
-// TFLOP/s; 16 x 2048, causal, 793 us, matrix pipes busy for 36% of the cycles.  (Copies of the kernel without the
-// exponentials, without the reads of lse and delta, or with half of the reads from LDS take
-// 98% of the time.)  4 x 4096 rows, when these pairs took 1590 us: one wave for both sides,
-// with twice the registers, 2430; 64 keys to a pair, which spills at D = 128, 1700.
+// the tiles, one workgroup to a CU: 4 x 4096 rows, 16 heads of 128 in bf16, 1210 to 1300 us,
+// 850 to 910 TFLOP/s, matrix pipes busy for 45% of the cycles; 16 x 2048, causal, 784 to 823 us,
+// 37%.  4 x 4096 rows, when these pairs took 1590 us: one wave for both sides, with twice the
+// registers, 2430; 64 keys to a pair, which spills at D = 128, 1700.
 constexpr int kRowsPass = 64;
 constexpr int kPairs = 4, kThreadsPairs = 2 * kPairs * kWave;
 
@@ -1484,8 +1488,8 @@ int64_t places_of(const fewbit_attn* a, int64_t rows, int64_t per) {
 
 // The forward that splits keys: shares per key head (0: the kernel for many rows), passes
 // of a share at least, and whether no unit is in two shares, as far as the host can tell.
-// It takes at most 32 rows to a sequence and key head.  One row on 64 caches of 8192 keys, 16
-// heads to 4: 105 us, the kernel for many rows 166; on 1 of 777, 12 heads: 10 and 10; but 16
+// It takes at most 32 rows to a sequence and key head.  One row on 64 caches of up to 8192
+// keys, 16 heads to 4: 105 us, the kernel for many rows 166; on 1 of 777, 12 heads: 10 and 10; but 16
 // rows on 8 of 4096, 16 heads to 4: 40 (32 rows at a time) and 21.
 struct Shares {
   int64_t n, least;

@@ -16,7 +16,8 @@ class AdamW(torch.optim.Optimizer):
     with dither) or 32.  master: keep fp32 weights of 16-bit parameters, whose
     rounded copies the parameters then are.  Gradients have the parameters' type or
     fp32; a parameter without one is left as it is, and its steps, by whose number the
-    moments are corrected, are those in which it had one.
+    moments are corrected, are those in which it had one.  Steps are counted on the
+    host: a step that is captured into a graph repeats its own corrections.
 
     The moments of a group's parameters of one type and device lie in flat buffers,
     made at the first step; adding a parameter group afterwards gives it buffers of
