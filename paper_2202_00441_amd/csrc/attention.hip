@@ -758,9 +758,9 @@ __device__ __forceinline__ int unit_at(const Args& a, int at, int& pass) {
 }
 
 // Bound by HBM: one row on 64 caches of up to 8192 keys, 270000 in all, 16 heads to 4 of 128
-// in bf16, 553 MB, 100 us, 5.5 TB/s.  Each wave has two buffers of its own, so that it waits for no other.  Keys are
-// read once and not kept in the caches (64 caches of 8192 keys each, more than the memory-side
-// cache holds: 177 us, else 200).
+// in bf16, 553 MB, 100 us, 5.5 TB/s.  Each wave has two buffers of its own, so that it waits for
+// no other.  Keys are read once and not kept in the caches (64 caches of 8192 keys each, more
+// than the memory-side cache holds: 177 us, else 200).
 template <int DT, int D>
 __global__ __launch_bounds__(kThreads, 2) void attn_split_kernel(const Args a) {
   using T = typename Mma<DT>::T;
@@ -1028,7 +1028,7 @@ __device__ __forceinline__ void fit_half(f32x16& ds, f32x16 (&sums)[D / 32], int
 // across workgroups: nothing is added atomically, and no gradient waits in memory).
 //
 // dQ: 128 rows of Q and dO to a workgroup, which walks tiles of 64 keys as the forward does;
-// delta is formed from its rows and left for the other kernel.  dS is rounded to the storage
+// delta is formed from their rows and left for the other kernel.  dS is rounded to the storage
 // type for its product with K.  Bound as the forward is: 4 x 4096 rows, 16 heads of 128 in
 // bf16, 742 to 791 us, 1040 to 1110 TFLOP/s, matrix pipes busy for 58%; 16 x 2048, causal, 488
 // to 516 us, 46%.
@@ -1472,10 +1472,11 @@ int check(const fewbit_attn* a) {
 }
 
 // Rows start at multiples of 16 bytes, in ascending order: lanes' offsets inside a load have
-// no sign.
-int check_strides(const int64_t (&s)[3]) {
-  if (s[0] < 0 || s[1] < 0 || s[2] < 0) return FEWBIT_E_INVALID;
-  return s[0] % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 ? FEWBIT_OK : FEWBIT_E_ALIGN;
+// no sign.  Packed sequences have no stride of their own.
+int check_strides(const fewbit_attn* a, const int64_t (&s)[3]) {
+  const int64_t first = a->cu_q ? 0 : s[0];
+  if (first < 0 || s[1] < 0 || s[2] < 0) return FEWBIT_E_INVALID;
+  return first % 8 == 0 && s[1] % 8 == 0 && s[2] % 8 == 0 ? FEWBIT_OK : FEWBIT_E_ALIGN;
 }
 
 int64_t over(int64_t n, int64_t per) { return (n + per - 1) / per; }
@@ -1641,7 +1642,7 @@ extern "C" int fewbit_attn_fwd(const fewbit_attn* a, const void* q, const void* 
   if (!q || !out || !lse || (a->rows_k > 0 && (!k || !v))) return FEWBIT_E_NULL;
   if (misaligned(q) || misaligned(k) || misaligned(v) || misaligned(out)) return FEWBIT_E_ALIGN;
   for (const auto* s : {&a->q_stride, &a->k_stride, &a->v_stride}) {
-    rc = check_strides(*s);
+    rc = check_strides(a, *s);
     if (rc != FEWBIT_OK) return rc;
   }
   const int64_t need = fewbit_attn_workspace(a, 0);
@@ -1703,7 +1704,7 @@ extern "C" int fewbit_attn_bwd(const fewbit_attn* a, const void* dout, const voi
       misaligned(dk) || misaligned(dv))
     return FEWBIT_E_ALIGN;
   for (const auto* s : {&a->q_stride, &a->k_stride, &a->v_stride, &a->dout_stride}) {
-    rc = check_strides(*s);
+    rc = check_strides(a, *s);
     if (rc != FEWBIT_OK) return rc;
   }
   if (workspace_bytes < fewbit_attn_workspace(a, 1)) return FEWBIT_E_INVALID;

@@ -136,6 +136,16 @@ def test_attention_strides_are_not_negative():
                 assert attn_fwd(attn(**{name: stride})) == E_INVALID, (name, i)
 
 
+def test_packed_attention_has_no_stride_of_sequences():
+    """The first stride is not used then, whatever it is: the call ends at the next check, the workspace's size."""
+    names = ("q_stride", "k_stride", "v_stride", "dout_stride")
+    for first in (3, -8):
+        odd = {name: (first, 512, 64) for name in names}
+        assert attn_bwd(attn(cu_q=16, cu_k=16, **odd), size=0) == E_INVALID
+        assert attn_bwd(attn(**odd), size=0) == (E_ALIGN if first == 3 else E_INVALID)
+    assert attn_bwd(attn(cu_q=16, cu_k=16, q_stride=(0, 516, 64)), size=0) == E_ALIGN
+
+
 def test_many_caches_are_not_divided():
     """Shares of many caches with lengths of their own would have to be found from all lengths by each workgroup: where
     every CU has several caches they are left whole, and need no room for joins."""
