@@ -14,6 +14,8 @@ from .autograd import FewBitActivation, FewBitAct
 from .block import (ADAMW_BLOCK, adamw_blocks, adamw_step, attention, attention_bwd, attention_fwd, qk_norm_rope,
                     qk_norm_rope_bwd, qk_norm_rope_fwd, rope_tables)
 from .optim import AdamW
+from .residual import (Dropout, Int8Linear, dropout, dropout_bwd, dropout_fwd, int8_linear, quantize_rows,
+                       residual_norm, residual_norm_bwd, residual_norm_fwd, residual_norm_int8)
 
 __all__ = [
     "ACTS", "BF16", "DTYPES", "F16", "F32", "FLAG_ELEMENT_FWD", "FLAG_REFINE", "FLAG_SYMMETRIC",
@@ -22,4 +24,6 @@ __all__ = [
     "bwd", "bwd_raw", "fit_table", "fwd", "fwd16_table_min", "fwd_raw", "packed_words", "strerror",
     "FewBitActivation", "FewBitAct", "ADAMW_BLOCK", "AdamW", "adamw_blocks", "adamw_step", "attention", "attention_bwd",
     "attention_fwd", "qk_norm_rope", "qk_norm_rope_bwd", "qk_norm_rope_fwd", "rope_tables",
+    "Dropout", "Int8Linear", "dropout", "dropout_bwd", "dropout_fwd", "int8_linear", "quantize_rows",
+    "residual_norm", "residual_norm_bwd", "residual_norm_fwd", "residual_norm_int8",
 ]

@@ -24,7 +24,7 @@ ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libfewbit.so")
 SOURCES = [os.path.join(CSRC, name) for name in
-           ("fewbit.hip", "attention.hip", "qk_norm_rope.hip", "adamw.hip", "fit.cpp")]
+           ("fewbit.hip", "attention.hip", "qk_norm_rope.hip", "adamw.hip", "residual.hip", "mm8.hip", "fit.cpp")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -32,12 +32,12 @@ FLAGS = [
     "-fno-gpu-flush-denormals-to-zero", "-fno-fast-math", "-ffp-contract=on",
     "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops",
     "-fconstexpr-steps=200000000", "-mllvm", "-amdgpu-kernarg-preload-count=16",
-    "-Wall", "-I", os.path.join(ROOT, "include"), "-parallel-jobs=5",
+    "-Wall", "-I", os.path.join(ROOT, "include"), "-parallel-jobs=7",
 ]
 
 
 NATIVE_OUT = os.path.join(HERE, "_native.so")
-NATIVE_SOURCES = [os.path.join(CSRC, "binding.cpp"), os.path.join(CSRC, "binding_block.cpp")]
+NATIVE_SOURCES = [os.path.join(CSRC, name) for name in ("binding.cpp", "binding_block.cpp", "binding_residual.cpp")]
 CXX = os.environ.get("CXX", "g++")
 
 

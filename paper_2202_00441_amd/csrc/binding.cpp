@@ -347,7 +347,8 @@ PyMODINIT_FUNC PyInit__native(void) {
   torch::autograd::_initFunctionPyTypeObject(node_type, "FewBitActivationBackward", node_properties, nullptr);
   torch::autograd::registerCppFunction(typeid(FewBitNode), &node_type);
   PyObject* module = PyModule_Create(&module_def);
-  if (module && PyModule_AddFunctions(module, binding::block_methods()) != 0) Py_CLEAR(module);
+  for (PyMethodDef* more : {binding::block_methods(), binding::residual_methods()})
+    if (module && PyModule_AddFunctions(module, more) != 0) Py_CLEAR(module);
   return module;
   END_HANDLE_TH_ERRORS
 }

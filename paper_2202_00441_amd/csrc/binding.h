@@ -46,5 +46,7 @@ inline void* stream_of(const at::Tensor& t) {
 
 // The block operators' calls (binding_block.cpp).
 PyMethodDef* block_methods();
+// Those between its products (binding_residual.cpp).
+PyMethodDef* residual_methods();
 
 }  // namespace binding

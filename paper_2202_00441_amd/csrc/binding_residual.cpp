@@ -1,0 +1,321 @@
+// binding_residual.cpp -- the calls on torch tensors of the operators between a block's
+// products and of the product in 8-bit integers; as binding_block.cpp does it.
+#include "binding_args.h"
+#include "fewbit_residual.h"
+
+namespace {
+
+using namespace binding;
+
+// p, the seed (a number, or an int64 tensor of one element on ref's device) and the site.
+struct Drop {
+  fewbit_drop d{};
+  at::Tensor seed;
+  bool some = false;        // elements are dropped
+};
+
+Drop drop_of(PyObject* const* args, const at::Tensor& ref) {
+  Drop r;
+  r.d.p = number(args[0], "p");
+  TORCH_CHECK_VALUE(r.d.p >= 0.0 && r.d.p <= 1.0, "p must be between 0 and 1");
+  r.some = std::nearbyint(r.d.p * 65536.0) > 0.0;
+  if (THPVariable_Check(args[1])) {
+    r.seed = tensor(args[1], "seed");
+    TORCH_CHECK_TYPE(r.seed.scalar_type() == at::kLong, "seed must be a whole number or an int64 tensor");
+    TORCH_CHECK_VALUE(r.seed.numel() == 1 && r.seed.device() == ref.device(), "a seed's tensor must have one element and be on the data's device");
+    r.d.seed_at = r.seed.data_ptr<int64_t>();
+  } else {
+    r.d.seed = whole(args[1], "seed");
+  }
+  const int64_t site = whole(args[2], "site");
+  TORCH_CHECK_VALUE(site >= 0 && site < int64_t{1} << 32, "site must be a whole number of 32 bits");
+  r.d.site = static_cast<uint32_t>(site);
+  return r;
+}
+
+// dropout(x, p, seed, site) -> y, or a status
+PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 4, "dropout takes four arguments");
+  check_mode();
+  const at::Tensor& x = tensor(args[0], "x");
+  TORCH_CHECK_TYPE(storage_type(x) >= 0, "x must be float32, float16 or bfloat16");
+  check_dense(x, "x");
+  const Drop p = drop_of(args + 1, x);
+  at::Tensor y;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(x.device());
+    y = at::empty(x.sizes(), x.options());
+    rc = fewbit_dropout(&p.d, storage_type(x), x.numel(), x.data_ptr(), y.data_ptr(), stream_of(x));
+  }
+  return rc == FEWBIT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// Sizes of rows [..., width]: rows of the last axis but one, `outer` of the axes before.
+void rows_of(const at::Tensor& t, fewbit_rnorm& a) {
+  const int64_t n = t.dim(), per = n > 0 ? t.size(n - 1) : 0;
+  TORCH_CHECK_VALUE(n >= 1 && per >= 8 && per % 8 == 0 && per <= FEWBIT_RNORM_MOST, "rows must have a multiple of 8 elements up to ",
+                    FEWBIT_RNORM_MOST);
+  a.width = static_cast<int32_t>(per);
+  a.rows = n > 1 ? t.size(n - 2) : 1;
+  a.outer = 1;
+  for (int64_t i = 0; i + 2 < n; ++i) a.outer *= t.size(i);
+  TORCH_CHECK_VALUE(a.rows < int64_t{1} << 31 && a.outer < int64_t{1} << 31 && (a.rows == 0 || a.outer < ((int64_t{1} << 31) / a.rows)),
+                    "there must be fewer than 2^31 rows");
+}
+
+// Strides {outer, row}; the axes before the last two have to be one.
+void strides_of(const at::Tensor& t, const char* name, int64_t (&s)[2]) {
+  const int64_t per = 16 / t.element_size(), n = t.dim();
+  bool fits = reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && (t.size(n - 1) <= 1 || t.stride(n - 1) == 1);
+  s[1] = n > 1 && t.size(n - 2) > 1 ? t.stride(n - 2) : 0;
+  s[0] = 0;
+  int64_t next = -1;        // the stride that the axis before would have
+  for (int64_t i = n - 3; i >= 0; --i) {
+    if (t.size(i) <= 1) continue;
+    if (next < 0)
+      s[0] = t.stride(i);
+    else
+      fits = fits && t.stride(i) == next;
+    next = t.stride(i) * t.size(i);
+  }
+  for (const int64_t v : s) fits = fits && v % per == 0;
+  TORCH_CHECK_VALUE(fits || t.numel() == 0, name, " must have contiguous rows that start at multiples of 16 bytes, in at most two even steps");
+}
+
+float eps_of(PyObject* o) {
+  const double eps = number(o, "eps");
+  TORCH_CHECK_VALUE(eps >= 0.0 && std::isfinite(static_cast<float>(eps)), "eps must be finite and not negative");
+  return static_cast<float>(eps);
+}
+
+void check_weight(const at::Tensor& w, const at::Tensor& ref, const char* ref_name) {
+  check_same(w, "weight", ref, ref_name);
+  check_shape(w, "weight", {ref.size(-1)});
+  check_dense(w, "weight");
+}
+
+fewbit_rnorm forward_of(const at::Tensor& x, const at::Tensor& residual, const at::Tensor& w, PyObject* eps) {
+  fewbit_rnorm a{};
+  TORCH_CHECK_TYPE(storage_type(x) >= 0, "x must be float32, float16 or bfloat16");
+  rows_of(x, a);
+  check_weight(w, x, "x");
+  a.dtype = storage_type(x);
+  a.eps = eps_of(eps);
+  strides_of(x, "x", a.x_stride);
+  if (residual.defined()) {
+    check_same(residual, "residual", x, "x");
+    check_shape(residual, "residual", x.sizes());
+    strides_of(residual, "residual", a.residual_stride);
+  }
+  return a;
+}
+
+// rnorm_fwd(x, residual, weight, eps, p, seed, site) -> (h, y), or a status; h is x where nothing is added or dropped
+PyObject* rnorm_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 7, "rnorm_fwd takes seven arguments");
+  check_mode();
+  const at::Tensor &x = tensor(args[0], "x"), &w = tensor(args[2], "weight");
+  const at::Tensor residual = optional(args[1], "residual");
+  fewbit_rnorm a = forward_of(x, residual, w, args[3]);
+  const Drop p = drop_of(args + 4, x);
+  a.drop = p.d;
+  at::Tensor h = x, y;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(x.device());
+    if (residual.defined() || p.some) h = at::empty(x.sizes(), x.options());
+    y = at::empty(x.sizes(), x.options());
+    rc = fewbit_rnorm_fwd(&a, x.data_ptr(), pointer(residual), w.data_ptr(), residual.defined() || p.some ? h.data_ptr() : nullptr,
+                          y.data_ptr(), stream_of(x));
+  }
+  return rc == FEWBIT_OK ? tuple_of(h, y) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// Scales of rows: x's shape without the last axis.
+at::IntArrayRef lead_of(const at::Tensor& x) { return x.sizes().slice(0, x.dim() - 1); }
+
+// rnorm_int8(x, residual, weight, eps) -> (h, codes, scale), or a status
+PyObject* rnorm_int8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 4, "rnorm_int8 takes four arguments");
+  check_mode();
+  const at::Tensor &x = tensor(args[0], "x"), &w = tensor(args[2], "weight");
+  const at::Tensor residual = optional(args[1], "residual");
+  const fewbit_rnorm a = forward_of(x, residual, w, args[3]);
+  at::Tensor h = x, codes, scale;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(x.device());
+    if (residual.defined()) h = at::empty(x.sizes(), x.options());
+    codes = at::empty(x.sizes(), x.options().dtype(at::kChar));
+    scale = at::empty(lead_of(x), x.options().dtype(at::kFloat));
+    rc = fewbit_rnorm_int8(&a, x.data_ptr(), pointer(residual), w.data_ptr(), residual.defined() ? h.data_ptr() : nullptr,
+                           codes.data_ptr<int8_t>(), scale.data_ptr<float>(), stream_of(x));
+  }
+  return rc == FEWBIT_OK ? tuple_of(h, codes, scale) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// rows8(x) -> (codes, scale), or a status
+PyObject* rows8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 1, "rows8 takes one argument");
+  check_mode();
+  const at::Tensor& x = tensor(args[0], "x");
+  fewbit_rnorm a{};
+  TORCH_CHECK_TYPE(storage_type(x) >= 0, "x must be float32, float16 or bfloat16");
+  rows_of(x, a);
+  a.dtype = storage_type(x);
+  strides_of(x, "x", a.x_stride);
+  at::Tensor codes, scale;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(x.device());
+    codes = at::empty(x.sizes(), x.options().dtype(at::kChar));
+    scale = at::empty(lead_of(x), x.options().dtype(at::kFloat));
+    rc = fewbit_rows8(&a, x.data_ptr(), codes.data_ptr<int8_t>(), scale.data_ptr<float>(), stream_of(x));
+  }
+  return rc == FEWBIT_OK ? tuple_of(codes, scale) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+// rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual) -> (dx, dresidual, dweight), or a status.
+// dresidual is dx where nothing is dropped, None where it is not asked for.
+PyObject* rnorm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 9, "rnorm_bwd takes nine arguments");
+  check_mode();
+  const at::Tensor dh = optional(args[0], "dh");
+  const at::Tensor &dy = tensor(args[1], "dy"), &h = tensor(args[2], "h"), &w = tensor(args[3], "weight");
+  fewbit_rnorm a{};
+  TORCH_CHECK_TYPE(storage_type(h) >= 0, "h must be float32, float16 or bfloat16");
+  rows_of(h, a);
+  check_dense(h, "h");
+  check_weight(w, h, "h");
+  a.dtype = storage_type(h);
+  a.eps = eps_of(args[4]);
+  const Drop p = drop_of(args + 5, h);
+  a.drop = p.d;
+  const bool apart = truth(args[8], "residual") && p.some;
+  check_same(dy, "dy", h, "h");
+  check_shape(dy, "dy", h.sizes());
+  strides_of(dy, "dy", a.dy_stride);
+  if (dh.defined()) {
+    check_same(dh, "dh", h, "h");
+    check_shape(dh, "dh", h.sizes());
+    strides_of(dh, "dh", a.dh_stride);
+  }
+  at::Tensor dx, dres, dw;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(h.device());
+    dx = at::empty(h.sizes(), h.options());
+    if (apart) dres = at::empty(h.sizes(), h.options());
+    dw = at::empty(w.sizes(), w.options().dtype(at::kFloat));
+    const int64_t need = fewbit_rnorm_workspace(&a);
+    const at::Tensor work = bytes(need, h);
+    rc = need < 0 ? static_cast<int>(need)
+                  : fewbit_rnorm_bwd(&a, pointer(dh), dy.data_ptr(), h.data_ptr(), w.data_ptr(), dx.data_ptr(), pointer(dres),
+                                     dw.data_ptr<float>(), pointer(work), need, stream_of(h));
+  }
+  if (rc != FEWBIT_OK) return PyLong_FromLong(rc);
+  if (!p.some) dres = dx;
+  THPObjectPtr r(PyTuple_New(3));
+  if (!r) return nullptr;
+  const at::Tensor* items[] = {&dx, &dres, &dw};
+  for (int i = 0; i < 3; ++i) {
+    PyObject* o = items[i]->defined() ? THPVariable_Wrap(*items[i]) : Py_NewRef(Py_None);
+    if (!o) return nullptr;
+    PyTuple_SET_ITEM(r.get(), i, o);
+  }
+  return r.release();
+  END_HANDLE_TH_ERRORS
+}
+
+// mm8(x, x_scale, weight, weight_scale, bias, act, dtype) -> y, or a status; dtype is that of the C ABI
+PyObject* mm8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  TORCH_CHECK_TYPE(nargs == 7, "mm8 takes seven arguments");
+  check_mode();
+  const at::Tensor &x = tensor(args[0], "x"), &xs = tensor(args[1], "x_scale"), &w = tensor(args[2], "weight"), &ws = tensor(args[3], "weight_scale");
+  const at::Tensor bias = optional(args[4], "bias");
+  fewbit_mm8 a{};
+  a.act = static_cast<int32_t>(whole(args[5], "act"));
+  a.dtype = static_cast<int32_t>(whole(args[6], "dtype"));
+  constexpr at::ScalarType kTypes[] = {at::kFloat, at::kHalf, at::kBFloat16};
+  TORCH_CHECK_TYPE(a.dtype >= 0 && a.dtype < 3, "y must be float32, float16 or bfloat16");
+  TORCH_CHECK_TYPE(x.scalar_type() == at::kChar && w.scalar_type() == at::kChar, "x and weight must be int8");
+  TORCH_CHECK_TYPE(xs.scalar_type() == at::kFloat && ws.scalar_type() == at::kFloat, "scales must be float32");
+  TORCH_CHECK_VALUE(x.dim() >= 1 && w.dim() == 2 && x.size(-1) == w.size(1), "x is [..., width] and weight [out, width]");
+  const int64_t width = w.size(1);
+  TORCH_CHECK_VALUE(width >= 16 && width <= 131056 && width % 16 == 0, "width must be a multiple of 16 up to 131056");
+  check_shape(xs, "x_scale", lead_of(x));
+  check_shape(ws, "weight_scale", {w.size(0)});
+  for (const auto& t : {w, xs, ws}) TORCH_CHECK_VALUE(t.device() == x.device(), "all tensors must be on x's device");
+  check_dense(xs, "x_scale");
+  check_dense(ws, "weight_scale");
+  if (bias.defined()) {
+    TORCH_CHECK_VALUE(bias.device() == x.device(), "bias must be on x's device");
+    TORCH_CHECK_TYPE(bias.scalar_type() == kTypes[a.dtype], "bias must have y's dtype");
+    check_shape(bias, "bias", {w.size(0)});
+    check_dense(bias, "bias");
+  }
+  a.width = static_cast<int32_t>(width);
+  a.out = w.size(0);
+  a.rows = x.numel() / width;
+  TORCH_CHECK_VALUE(a.rows < int64_t{1} << 31 && a.out < int64_t{1} << 31, "there must be fewer than 2^31 rows and channels");
+  // one step from row to row
+  int64_t next = -1;
+  bool fits = x.stride(-1) == 1 && w.stride(1) == 1 && reinterpret_cast<uintptr_t>(x.data_ptr()) % 16 == 0 &&
+              reinterpret_cast<uintptr_t>(w.data_ptr()) % 16 == 0;
+  for (int64_t i = x.dim() - 2; i >= 0; --i) {
+    if (x.size(i) <= 1) continue;
+    if (next < 0)
+      a.x_stride = x.stride(i);
+    else
+      fits = fits && x.stride(i) == next;
+    next = x.stride(i) * x.size(i);
+  }
+  a.w_stride = a.out > 1 ? w.stride(0) : 0;
+  fits = fits && a.x_stride % 16 == 0 && a.w_stride % 16 == 0;
+  TORCH_CHECK_VALUE(fits || a.rows == 0 || a.out == 0, "x and weight must have contiguous rows at even steps of a multiple of 16 bytes");
+  at::Tensor y;
+  int rc;
+  {
+    pybind11::gil_scoped_release no_gil;
+    at::AutoDispatchBelowADInplaceOrView below;
+    const c10::DeviceGuard guard(x.device());
+    std::vector<int64_t> shape(lead_of(x).vec());
+    shape.push_back(a.out);
+    y = at::empty(shape, x.options().dtype(kTypes[a.dtype]));
+    const int64_t need = fewbit_mm8_workspace(&a);
+    const at::Tensor work = bytes(need, x);
+    rc = need < 0 ? static_cast<int>(need)
+                  : fewbit_mm8_fwd(&a, x.data_ptr<int8_t>(), xs.data_ptr<float>(), w.data_ptr<int8_t>(), ws.data_ptr<float>(), pointer(bias),
+                                   y.data_ptr(), pointer(work), need, stream_of(x));
+  }
+  return rc == FEWBIT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(rc);
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {method<dropout>("dropout"), method<rnorm_fwd>("rnorm_fwd"), method<rnorm_bwd>("rnorm_bwd"),
+                         method<rnorm_int8>("rnorm_int8"), method<rows8>("rows8"), method<mm8>("mm8"), {nullptr, nullptr, 0, nullptr}};
+
+}  // namespace
+
+PyMethodDef* binding::residual_methods() { return methods; }
