@@ -1,7 +1,7 @@
 // drop.h -- the generator of dropout (formulas in fewbit_residual.h).
 //
-// Eight elements share a block of four words, so that an access of 16 bytes of 16-bit
-// elements needs one run of the generator.  A round is two products of 32 by 32 bits, which
+// Eight elements share a block of four words, so that eight elements of a lane need one run of
+// the generator.  A round is two products of 32 by 32 bits, which
 // the vector units form in one instruction each, and four exclusive ors.
 #pragma once
 
@@ -59,18 +59,82 @@ __device__ __forceinline__ void words(uint64_t block, Key key, uint32_t site, ui
   }
 }
 
-// Element i of eight is kept.
-__device__ __forceinline__ bool kept(const uint32_t (&c)[4], int i, uint32_t border) {
-  const uint32_t u = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xFFFFu;
-  return u >= border;
-}
+// A wave's 512 consecutive elements, eight to a lane, by accesses of 16 bytes that lie next to
+// each other (two of 32-bit elements 1 KB apart: 32 bytes of a lane at a time would bring
+// every line twice; 32768 x 1024 elements through dropout 56 us, so 41): element i of lane l
+// is 8 l + i of 16-bit elements, and 4 l + i, 256 + 4 l + i - 4 of 32-bit ones.
+constexpr int kWaveElements = kWave * 8;
+template <class T>
+struct Chunk {
+  static constexpr int kAccesses = sizeof(T) / 2, kEach = 8 / kAccesses;
 
-// Eight elements from 8 * block on.
-__device__ __forceinline__ void drop(const Drop& d, Key key, uint64_t block, float (&x)[8]) {
-  uint32_t c[4];
-  words(block, key, d.site, c);
+  // `first`: the wave's first element, relative to the stream
+  template <int P>
+  __device__ __forceinline__ static void load(const Stream& s, uint32_t first, int lane, float (&x)[8]) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) x[i] = kept(c, i, d.border) ? x[i] * d.scale : 0.0f;
+    for (int j = 0; j < kAccesses; ++j) {
+      float v[kEach];
+      s.template load<T, P>(first * sizeof(T) + j * 1024 + lane * 16, v);
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) x[j * kEach + i] = v[i];
+    }
+  }
+  template <int P>
+  __device__ __forceinline__ static void store(const Stream& s, uint32_t first, int lane, const float (&x)[8]) {
+#pragma unroll
+    for (int j = 0; j < kAccesses; ++j) {
+      float v[kEach];
+#pragma unroll
+      for (int i = 0; i < kEach; ++i) v[i] = x[j * kEach + i];
+      s.template store<T, P>(first * sizeof(T) + j * 1024 + lane * 16, v);
+    }
+  }
+  // The same elements of a tensor of floats, and of bytes (packed in two words).
+  template <int P>
+  __device__ __forceinline__ static void store_floats(const Stream& s, uint32_t first, int lane, const float (&x)[8]) {
+    if constexpr (kAccesses == 2)
+      store<P>(s, first, lane, x);
+    else
+      s.template store<float, P>(first * 4 + lane * 32, x);
+  }
+  template <int P>
+  __device__ __forceinline__ static void store_bytes(const Stream& s, uint32_t first, int lane, u32x2 x) {
+    if constexpr (kAccesses == 2) {
+      s.template put<P>(first + lane * 4, static_cast<uint32_t>(x[0]));
+      s.template put<P>(first + 256 + lane * 4, static_cast<uint32_t>(x[1]));
+    } else {
+      s.template put<P>(first + lane * 8, x);
+    }
+  }
+};
+
+// A lane's elements of the 512 from 8 * block on.  Of 32-bit elements two lanes share a block
+// in each access: the even one runs the generator for the first, the odd one for the second,
+// and they hand each other the other's half.
+template <class T>
+__device__ __forceinline__ void drop(const Drop& d, Key key, uint64_t block, int lane, float (&x)[8]) {
+  uint32_t c[4];
+  if constexpr (Chunk<T>::kAccesses == 1) {
+    words(block + lane, key, d.site, c);
+  } else {
+    const bool odd = lane % 2;
+    uint32_t own[4];
+    words(block + lane / 2 + (odd ? 32 : 0), key, d.site, own);
+    uint32_t got[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      got[i] = __builtin_bit_cast(uint32_t, dpp<0xb1 /* quad_perm 1,0,3,2 */>(__builtin_bit_cast(float, odd ? own[i] : own[2 + i])));
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      c[i] = odd ? got[i] : own[i];
+      c[2 + i] = odd ? own[2 + i] : got[i];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    const uint32_t u = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xFFFFu;
+    x[i] = u >= d.border ? x[i] * d.scale : 0.0f;
+  }
 }
 
 }  // namespace block

@@ -332,7 +332,7 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void tile_kernel(const
 }
 
 // Sums of the shares, and the epilogue: a lane takes four consecutive channels.
-constexpr int kJoinThreads = 256;
+constexpr int kJoinThreads = 64;          // small workgroups, for many CUs
 template <int DT, int ACT>
 __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Args a, int shares) {
   using T = typename Store<DT>::type;
@@ -341,17 +341,23 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Args a, int sh
   if (m >= a.rows) return;
   const int64_t n = (at - m * quads) * 4;
   const int* parts = a.parts + m * a.pitch + n;
+  const T* biases = static_cast<const T*>(a.bias);
+  // everything is on its way before the first is waited for; a row's last channels are read again
+  // past its end
+  const float xs = a.xs[m];
+  float ws[4], bias[4] = {};
+#pragma unroll
+  for (int e = 0; e < 4; ++e) ws[e] = a.ws[min(n + e, a.out - 1)];
+  if (biases)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) bias[e] = static_cast<float>(biases[min(n + e, a.out - 1)]);
   i32x4 sum = {};
 #pragma unroll 8
   for (int i = 0; i < shares; ++i) sum += *reinterpret_cast<const i32x4*>(parts + i * a.rows * a.pitch);
-  const float xs = a.xs[m];
   T* y = static_cast<T*>(a.y) + m * a.out + n;
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (n + e >= a.out) break;
-    const float bias = a.bias ? static_cast<float>(static_cast<const T*>(a.bias)[n + e]) : 0.0f;
-    y[e] = static_cast<T>(activate<DT, ACT>(static_cast<float>(sum[e]) * (xs * a.ws[n + e]) + bias));
-  }
+  for (int e = 0; e < 4; ++e)
+    if (n + e < a.out) y[e] = static_cast<T>(activate<DT, ACT>(static_cast<float>(sum[e]) * (xs * ws[e]) + bias[e]));
 }
 
 // ---------------------------------------------------------------- few tokens
