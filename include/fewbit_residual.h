@@ -83,7 +83,8 @@ int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x
  * {outer, row} in elements; rows start at multiples of 16 bytes.  h, y, dx and
  * dresidual are dense, as are codes; scale has one float per row.  Everything
  * is computed in fp32 and rounded once; dw is summed in an order that depends
- * on the sizes alone.  outer * rows stays below 2^31.
+ * on the sizes alone.  outer * rows stays below 2^31, and a launch has fewer than
+ * 2^32 threads: 64 a row of up to 2048 elements, 256 up to 8192, 1024 beyond.
  */
 #define FEWBIT_RNORM_MOST 32768   /* elements of a row                         */
 
@@ -127,10 +128,13 @@ int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const void* dy, cons
  * of fewbit.h.
  *
  * x and w have `width` contiguous codes per row and rows that start at
- * multiples of 16 bytes; the scales are dense, bias (may be NULL) has the type of y,
- * and y is dense.  rows and out stay below 2^31.
+ * multiples of 16 bytes, at most FEWBIT_MM8_STRIDE apart; the scales are dense, bias (may
+ * be NULL) has the type of y, and y is dense.  Codes may be -128.  rows and out stay
+ * below 2^31, and what a launch takes below 2^32 threads (512 for 256 x 256 results
+ * where there are many).
  */
 #define FEWBIT_MM8_LINEAR (-1)
+#define FEWBIT_MM8_STRIDE 8388608  /* 2^23 */
 
 typedef struct fewbit_mm8 {
     int32_t dtype;                /* of y and bias                             */

@@ -294,6 +294,8 @@ PyObject* mm8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   a.w_stride = a.out > 1 ? w.stride(0) : 0;
   fits = fits && a.x_stride % 16 == 0 && a.w_stride % 16 == 0;
   TORCH_CHECK_VALUE(fits || a.rows == 0 || a.out == 0, "x and weight must have contiguous rows at even steps of a multiple of 16 bytes");
+  TORCH_CHECK_VALUE(a.x_stride <= FEWBIT_MM8_STRIDE && a.w_stride <= FEWBIT_MM8_STRIDE, "rows of x and weight must be at most ", FEWBIT_MM8_STRIDE,
+                    " bytes apart");
   at::Tensor y;
   int rc;
   {

@@ -142,6 +142,20 @@ struct Scale {
   }
 };
 
+// Rows of WN elements from LDS to y, V bytes of a lane at a time.
+template <class T, int WN, int ROWS, int V>
+__device__ __forceinline__ void store_rows(const int8_t* lds, T* y, int64_t out, int rows, int cols, int lane) {
+  typedef T Piece __attribute__((ext_vector_type(V / sizeof(T))));
+  constexpr int kPer = 16 / sizeof(T), kChunks = WN / kPer;       // of a chunk of 16 bytes
+  constexpr int kEach = V / sizeof(T), kLanes = WN / kEach;       // elements of a lane, lanes of a row
+#pragma unroll 8
+  for (int at = lane; at < ROWS * kLanes; at += kWave) {
+    const int r = at / kLanes, c = at % kLanes * kEach;
+    const Piece v = *reinterpret_cast<const Piece*>(lds + (r * kChunks + (c / kPer ^ r % kChunks)) * 16 + c % kPer * sizeof(T));
+    if (r < rows && c < cols) *reinterpret_cast<Piece*>(y + r * out + c) = v;
+  }
+}
+
 // A wave's WM tokens by WN channels from its registers to y, through BYTES of LDS of its own, so that it stores whole runs of a row.  Element (r, c) lies in chunk
 // c / kPer ^ r % kChunks of row r.
 template <int DT, int ACT, int WM, int WN, int BYTES, int BM, int BN>
@@ -152,7 +166,6 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
   constexpr int kPer = 16 / sizeof(T), kChunks = WN / kPer;       // elements of a chunk, chunks of a row
   constexpr int kRows = WM * kChunks * 16 <= BYTES ? WM : BYTES / (kChunks * 16) / 16 * 16;
   const int64_t m1 = m0 + wm, n1 = n0 + wn;
-  const bool whole = a.out * sizeof(T) % 16 == 0;
 #pragma unroll
   for (int first = 0; first < WM; first += kRows) {
 #pragma unroll
@@ -170,23 +183,18 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
       }
     }
     const int rows = static_cast<int>(min(static_cast<int64_t>(kRows), a.rows - m1 - first));
+    const int cols = static_cast<int>(min(static_cast<int64_t>(WN), a.out - n1));
     T* y = static_cast<T*>(a.y) + (m1 + first) * a.out + n1;
-    if (whole) {
-      constexpr int kAt = kWave / kChunks;          // rows of an access
-#pragma unroll 4
-      for (int r = lane / kChunks; r < kRows; r += kAt) {
-        const int c = lane % kChunks;
-        const u32x4 v = *reinterpret_cast<const u32x4*>(lds + (r * kChunks + (c ^ r % kChunks)) * 16);
-        if (r < rows && n1 + c * kPer < a.out) *reinterpret_cast<u32x4*>(y + r * a.out + c * kPer) = v;
-      }
-    } else {
-      const int cols = static_cast<int>(min(static_cast<int64_t>(WN), a.out - n1));
-      for (int at = lane; at < kRows * WN; at += kWave) {
-        const int r = at / WN, c = at % WN;
-        const T v = *reinterpret_cast<const T*>(lds + r * kChunks * 16 + ((c / kPer ^ r % kChunks) * 16) + c % kPer * sizeof(T));
-        if (r < rows && c < cols) y[r * a.out + c] = v;
-      }
-    }
+    // by as many bytes as every row is aligned to
+    const int aligned = static_cast<int>(a.out * sizeof(T) % 16);
+    if (aligned == 0)
+      store_rows<T, WN, kRows, 16>(lds, y, a.out, rows, cols, lane);
+    else if (aligned % 8 == 0)
+      store_rows<T, WN, kRows, 8>(lds, y, a.out, rows, cols, lane);
+    else if (aligned % 4 == 0)
+      store_rows<T, WN, kRows, 4>(lds, y, a.out, rows, cols, lane);
+    else
+      store_rows<T, WN, kRows, sizeof(T)>(lds, y, a.out, rows, cols, lane);
   }
 }
 
@@ -431,7 +439,8 @@ __global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(const Args a) {
 }
 
 // ---------------------------------------------------------------- host side
-constexpr int64_t kMostStride = int64_t{1} << 22;      // a tile's rows are reached by offsets of 31 bits
+// A tile's rows are reached by offsets of 31 bits.
+static_assert(int64_t{255} * FEWBIT_MM8_STRIDE + 131056 < int64_t{1} << 31, "offsets of a tile's rows");
 
 int check(const fewbit_mm8* a) {
   if (!a) return FEWBIT_E_NULL;
@@ -439,7 +448,7 @@ int check(const fewbit_mm8* a) {
   if (a->act != FEWBIT_MM8_LINEAR && a->act != FEWBIT_GELU && a->act != FEWBIT_SILU) return FEWBIT_E_INVALID;
   if (a->reserved != 0 || a->rows < 0 || a->out < 0 || a->rows >= int64_t{1} << 31 || a->out >= int64_t{1} << 31) return FEWBIT_E_INVALID;
   if (a->width < 16 || a->width > 131056 || a->width % 16 != 0) return FEWBIT_E_INVALID;
-  if (a->x_stride < 0 || a->w_stride < 0 || a->x_stride > kMostStride || a->w_stride > kMostStride) return FEWBIT_E_INVALID;
+  if (a->x_stride < 0 || a->w_stride < 0 || a->x_stride > FEWBIT_MM8_STRIDE || a->w_stride > FEWBIT_MM8_STRIDE) return FEWBIT_E_INVALID;
   return FEWBIT_OK;
 }
 
@@ -455,8 +464,9 @@ struct Plan {
 
 // What is fastest by the times that each kernel was seen to take: of a step of 128 codes, and
 // of the rest, in us, with T workgroups on 256 CUs.
-//   few tokens   16.8 M weights by one token 5.4 us, in tiles 6.3; 67 M 14.4 and 11.4; with 16
-//                tokens 4.2 M 4.3 and 6.5, 16.8 M 6.5 to 10.4 and 6.2 to 8.6
+//   few tokens   16.8 M weights by one token 5.4 us, in tiles 6.3; 67 M 14.4 and 11.4; 32 M by
+//                four 13.7 and 10.2; by 16 tokens 4.2 M 4.3 and 6.5, 16.8 M 6.5 to 10.4 and 6.2
+//                to 8.6; 228 channels of 15280 codes by 13: 22 and, in shares, 8.4
 //   64 x 64      0.2 a step with a workgroup a CU (64 x 8192 by 2048: 6.1 us; with two stages
 //                instead of four 10.3), 0.38 with two
 //   128 x 128    three stages, a workgroup a CU: 0.6 (2048 x 2048 by 2048: 13.5 us, 64 x 64
@@ -469,9 +479,9 @@ Plan plan_of(const fewbit_mm8* a) {
   const int steps = (a->width + kStep - 1) / kStep;
   const int64_t weights = a->out * a->width;
   Plan best{Plan::kFew, 1, 1, steps, 1, 1};
-  if (a->rows <= 16 && weights <= (a->rows <= 8 ? 1 << 25 : 1 << 23)) {
+  if (a->rows <= 16 && weights <= (a->rows <= 2 ? 1 << 25 : a->rows <= 8 ? 1 << 24 : 1 << 23)) {
     while (best.places < 4 && a->rows <= 8 / best.places && a->out * best.places < 16 * cus) best.places *= 2;
-    return best;
+    if (a->width <= 4096 * best.places) return best;
   }
   double least = 0.0;
   const auto offer = [&](Plan::Kind kind, int side, int shares, int each, double per_cu, double step, double rest) {

@@ -184,7 +184,9 @@ def int8_linear(x, x_scale, weight, weight_scale, bias=None, act=None, dtype=tor
 
     x [..., width] and weight [out, width] int8 (as quantize_rows gives them),
     x_scale [...] and weight_scale [out] fp32, bias [out] of dtype or None; act
-    None, "gelu" or "silu".  width a multiple of 16 up to 131056; sums are exact."""
+    None, "gelu" or "silu".  width a multiple of 16 up to 131056; rows contiguous,
+    even steps of a multiple of 16 bytes and of at most 2^23 apart; sums are exact.
+    Not differentiable."""
     if act not in _ACTS:
         raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
     if dtype not in _TYPES:

@@ -405,11 +405,12 @@ def product_inputs(rows, out, width, dtype, seed=0, bias=True):
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("rows", (1, 2, 15, 16, 17, 31, 33, 64, 65, 129, 300))
 def test_product_of_every_number_of_rows(rows, dtype, act):
-    for out, width in ((1, 16), (5, 32), (16, 112), (33, 128), (127, 144), (128, 1040), (257, 256), (1000, 4096), (64, 8208)):
+    for out, width in ((1, 16), (5, 32), (16, 112), (33, 128), (127, 144), (128, 1040), (130, 96), (132, 272), (257, 256), (1000, 4096), (64, 8208)):
         check_product(*product_inputs(rows, out, width, dtype, bias=out % 3 != 1), act, dtype)
 
 
-@pytest.mark.parametrize("rows,out,width", ((1, 8192, 2048), (64, 2048, 8192), (777, 1001, 1040), (2048, 2000, 528), (1000, 4100, 2048), (4097, 520, 144)))
+@pytest.mark.parametrize("rows,out,width", ((1, 8192, 2048), (64, 2048, 8192), (777, 1001, 1040), (2048, 2000, 528), (1000, 4100, 2048), (4097, 520, 144),
+                                            (2600, 3002, 160), (5000, 4098, 144), (9001, 2052, 160), (2819, 6871, 272), (13, 228, 15280)))
 def test_product_of_larger_sizes(rows, out, width):
     check_product(*product_inputs(rows, out, width, BF16), None, BF16)
     a = check_product(*product_inputs(rows, out, width, F16), "gelu", F16)
@@ -445,6 +446,24 @@ def test_product_of_strided_rows(rows):
     assert torch.equal(P.int8_linear(same, xs, w, ws, b), P.int8_linear(same.contiguous(), xs, w, ws, b))
     assert torch.equal(P.int8_linear(x, xs, w[:1].expand(70, 160), ws, b), P.int8_linear(x, xs, w[:1].repeat(70, 1), ws, b))
     assert torch.equal(P.int8_linear(x[0], xs[0], w, ws, b), want[0])
+
+
+@pytest.mark.parametrize("rows", (3, 8, 260))
+def test_product_of_rows_far_apart(rows):
+    """As far as a tile's rows may be, of both operands; further ones are refused."""
+    x, xs, w, ws, b = product_inputs(rows, 40, 64, BF16)
+    want = P.int8_linear(x, xs, w, ws, b)
+    for far in (x, w):
+        wide = torch.empty(far.shape[0], 1 << 23, dtype=torch.int8, device="cuda")
+        wide[:, :64] = far
+        y = P.int8_linear(wide[:, :64], xs, w, ws, b) if far is x else P.int8_linear(x, xs, wide[:, :64], ws, b)
+        assert torch.equal(y, want)
+    wide = torch.empty(2, (1 << 23) + 16, dtype=torch.int8, device="cuda")
+    with pytest.raises(ValueError, match="apart"):
+        P.int8_linear(wide[:, :64], xs[:2], w, ws, b)
+    with pytest.raises(ValueError, match="apart"):
+        P.int8_linear(x, xs, wide[:, :64], ws[:2], b[:2])
+    torch.cuda.empty_cache()
 
 
 def test_product_of_nothing_and_of_scales_that_are_not_numbers():

@@ -4,8 +4,9 @@ products (no GPU, nothing is launched), and of the dropout generator's definitio
 import ctypes as C
 import os
 import re
+import subprocess
+import tempfile
 
-import numpy as np
 import pytest
 import torch
 
@@ -45,6 +46,22 @@ def test_exports_every_declared_symbol():
                      "fewbit_rnorm_int8", "fewbit_rnorm_workspace", "fewbit_rows8"]
     for name in names:
         assert hasattr(LIB, name), name
+
+
+def test_header_is_plain_c():
+    src = '#include "fewbit_residual.h"\nint main(void) { return sizeof(fewbit_rnorm) + sizeof(fewbit_mm8) > 0 ? 0 : 1; }\n'
+    r = subprocess.run(["gcc", "-std=c99", "-Wall", "-Werror", "-pedantic", "-fsyntax-only", "-I", os.path.dirname(HEADER), "-x", "c", "-"],
+                       input=src, text=True, capture_output=True)
+    assert r.returncode == 0, r.stderr
+
+
+def test_structures_are_the_headers():
+    """Sizes as the compiler lays them out."""
+    src = '#include <stdio.h>\n#include "fewbit_residual.h"\nint main(void) { printf("%zu %zu %zu", sizeof(fewbit_drop), sizeof(fewbit_rnorm), sizeof(fewbit_mm8)); return 0; }\n'
+    with tempfile.TemporaryDirectory() as d:
+        subprocess.run(["gcc", "-I", os.path.dirname(HEADER), "-x", "c", "-", "-o", os.path.join(d, "sizes")], input=src, text=True, check=True)
+        out = subprocess.run([os.path.join(d, "sizes")], capture_output=True, text=True, check=True).stdout
+    assert out.split() == [str(C.sizeof(t)) for t in (Drop, Rnorm, Mm8)]
 
 
 # ---------------------------------------------------------------- the generator
@@ -174,7 +191,7 @@ def product(a, x=A, xs=A, w=A, ws=A, bias=None, y=A, work=A, size=1 << 40):
     ({"dtype": 3}, E_DTYPE), ({"act": 2}, E_INVALID), ({"act": -2}, E_INVALID), ({"rows": -1}, E_INVALID), ({"out": -1}, E_INVALID),
     ({"rows": 1 << 31}, E_INVALID), ({"out": 1 << 31}, E_INVALID), ({"width": 0}, E_INVALID), ({"width": 24}, E_INVALID),
     ({"width": 131072}, E_INVALID), ({"reserved": 1}, E_INVALID), ({"x_stride": -64}, E_INVALID), ({"w_stride": -64}, E_INVALID),
-    ({"x_stride": 1 << 23}, E_INVALID), ({"w_stride": 1 << 23}, E_INVALID)))
+    ({"x_stride": (1 << 23) + 16}, E_INVALID), ({"w_stride": (1 << 23) + 16}, E_INVALID)))
 def test_product_refusals(changes, status):
     a = mm8(**changes)
     assert product(a) == LIB.fewbit_mm8_workspace(C.byref(a)) == status
