@@ -2,7 +2,7 @@
 // per channel, bias and activation in the epilogue.
 //
 // Formulas in fewbit_residual.h.  Few tokens are bound by the weights' bytes, many by the
-// matrix instructions (and the power that they draw: 32768 x 8192 by 2048 takes 421 us, 2.6
+// matrix instructions (and the power that they draw: 32768 x 8192 by 2048 takes 405 us, 2.7
 // POP/s).  The matrix instruction takes 16 channels by 16 tokens by
 // 64 bytes of both: its first operand holds, in lane l, 16 consecutive codes of channel l %
 // 16, the second those of token l % 16, and a lane of the result has four consecutive
@@ -143,7 +143,7 @@ struct Scale {
 };
 
 // Rows of WN elements from LDS to y, V bytes of a lane at a time.
-template <class T, int WN, int ROWS, int V>
+template <class T, int WN, int ROWS, int V, bool KEEP>
 __device__ __forceinline__ void store_rows(const int8_t* lds, T* y, int64_t out, int rows, int cols, int lane) {
   typedef T Piece __attribute__((ext_vector_type(V / sizeof(T))));
   constexpr int kPer = 16 / sizeof(T), kChunks = WN / kPer;       // of a chunk of 16 bytes
@@ -151,14 +151,23 @@ __device__ __forceinline__ void store_rows(const int8_t* lds, T* y, int64_t out,
 #pragma unroll 8
   for (int at = lane; at < ROWS * kLanes; at += kWave) {
     const int r = at / kLanes, c = at % kLanes * kEach;
-    const Piece v = *reinterpret_cast<const Piece*>(lds + (r * kChunks + (c / kPer ^ r % kChunks)) * 16 + c % kPer * sizeof(T));
-    if (r < rows && c < cols) *reinterpret_cast<Piece*>(y + r * out + c) = v;
+    const Piece v = *reinterpret_cast<const Piece*>(lds + (r * kChunks + (c / kPer ^ r / 2 % kChunks)) * 16 + c % kPer * sizeof(T));
+    if (r < rows && c < cols) {
+      if constexpr (KEEP)
+        *reinterpret_cast<Piece*>(y + r * out + c) = v;
+      else
+        __builtin_nontemporal_store(v, reinterpret_cast<Piece*>(y + r * out + c));
+    }
   }
 }
 
-// A wave's WM tokens by WN channels from its registers to y, through BYTES of LDS of its own, so that it stores whole runs of a row.  Element (r, c) lies in chunk
-// c / kPer ^ r % kChunks of row r.
-template <int DT, int ACT, int WM, int WN, int BYTES, int BM, int BN>
+// A wave's WM tokens by WN channels from its registers to y, through BYTES of LDS of its own, so
+// that it stores whole runs of a row.  Element (r, c) lies in chunk c / kPer ^ r / 2 % kChunks of
+// row r: 16 lanes that write a chunk of 16 rows meet 64 different banks.  KEEP: results stay in
+// the caches, as those of tiles of 256 hardly would (32768 x 2048 by 8192 channels with GELU 628
+// us, past the caches 600, and with the channels' scales read once instead of for every 16
+// tokens 542).
+template <int DT, int ACT, int WM, int WN, int BYTES, bool KEEP, int BM, int BN>
 __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, int8_t* lds, int64_t m0, int64_t n0, int wm, int wn, int lane,
                                        const i32x4 (&acc)[WN / 16][WM / 16]) {
   using T = typename Store<DT>::type;
@@ -169,17 +178,17 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
 #pragma unroll
   for (int first = 0; first < WM; first += kRows) {
 #pragma unroll
-    for (int j = first / 16; j < (first + kRows) / 16; ++j) {
-      const float xs = s.xs[wm + j * 16 + lane % 16];
-      const int r = j * 16 - first + lane % 16;
+    for (int i = 0; i < WN / 16; ++i) {
+      const int c = i * 16 + lane / 16 * 4;
+      const f32x4 ws = *reinterpret_cast<const f32x4*>(s.ws + wn + c), bias = *reinterpret_cast<const f32x4*>(s.bias + wn + c);
 #pragma unroll
-      for (int i = 0; i < WN / 16; ++i) {
-        const int c = i * 16 + lane / 16 * 4;
-        const f32x4 ws = *reinterpret_cast<const f32x4*>(s.ws + wn + c), bias = *reinterpret_cast<const f32x4*>(s.bias + wn + c);
+      for (int j = first / 16; j < (first + kRows) / 16; ++j) {
+        const int r = j * 16 - first + lane % 16;
+        const float xs = s.xs[wm + j * 16 + lane % 16];
         V4 v;
 #pragma unroll
         for (int e = 0; e < 4; ++e) v[e] = static_cast<T>(activate<DT, ACT>(static_cast<float>(acc[i][j][e]) * (xs * ws[e]) + bias[e]));
-        *reinterpret_cast<V4*>(lds + r * kChunks * 16 + ((c / kPer ^ r % kChunks) * 16) + c % kPer * sizeof(T)) = v;
+        *reinterpret_cast<V4*>(lds + r * kChunks * 16 + ((c / kPer ^ r / 2 % kChunks) * 16) + c % kPer * sizeof(T)) = v;
       }
     }
     const int rows = static_cast<int>(min(static_cast<int64_t>(kRows), a.rows - m1 - first));
@@ -188,13 +197,13 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
     // by as many bytes as every row is aligned to
     const int aligned = static_cast<int>(a.out * sizeof(T) % 16);
     if (aligned == 0)
-      store_rows<T, WN, kRows, 16>(lds, y, a.out, rows, cols, lane);
+      store_rows<T, WN, kRows, 16, KEEP>(lds, y, a.out, rows, cols, lane);
     else if (aligned % 8 == 0)
-      store_rows<T, WN, kRows, 8>(lds, y, a.out, rows, cols, lane);
+      store_rows<T, WN, kRows, 8, KEEP>(lds, y, a.out, rows, cols, lane);
     else if (aligned % 4 == 0)
-      store_rows<T, WN, kRows, 4>(lds, y, a.out, rows, cols, lane);
+      store_rows<T, WN, kRows, 4, KEEP>(lds, y, a.out, rows, cols, lane);
     else
-      store_rows<T, WN, kRows, sizeof(T)>(lds, y, a.out, rows, cols, lane);
+      store_rows<T, WN, kRows, sizeof(T), KEEP>(lds, y, a.out, rows, cols, lane);
   }
 }
 
@@ -232,7 +241,7 @@ struct Operands {
       read<NEXT, FROM, TO>(xt, wt);
       if constexpr (NEXT == 1) {
         // as written: left to itself the compiler gathers the reads before the barrier, which
-        // then waits for them (32768 x 8192 by 2048: 430 us, so 421)
+        // then waits for them (32768 x 8192 by 2048: 2% slower)
         __builtin_amdgcn_sched_group_barrier(0x008 /* matrix */, (TO - FROM) * (WN / 16), 0);
         __builtin_amdgcn_sched_group_barrier(0x100 /* LDS reads */, FROM < WN / 16 ? 2 : 1, 0);
       }
@@ -333,9 +342,9 @@ __global__ __launch_bounds__(BM / WM * (BN / WN) * kWave) void tile_kernel(const
     }
   } else {
     // results leave through two stages: half the waves' through each
-    constexpr int kOwn = kStage / (kWaves / 2), kBytes = kOwn >= 16384 ? 16384 : 8192;
+    constexpr int kOwn = kStage / (kWaves / 2), kBytes = 8192;       // (16384: 1 to 3% slower, for stores begin later)
     static_assert(kOwn >= kBytes, "the waves' shares of the stages");
-    finish<DT, ACT, WM, WN, kBytes>(a, scales, (wave % 2 ? s1 : s0) + wave / 2 * kBytes, m0, n0, wm, wn, lane, acc);
+    finish<DT, ACT, WM, WN, kBytes, BM < 256>(a, scales, (wave % 2 ? s1 : s0) + wave / 2 * kBytes, m0, n0, wm, wn, lane, acc);
   }
 }
 
@@ -471,7 +480,7 @@ struct Plan {
 //                instead of four 10.3), 0.38 with two
 //   128 x 128    three stages, a workgroup a CU: 0.6 (2048 x 2048 by 2048: 13.5 us, 64 x 64
 //                17, 256 x 256 25); two stages, two workgroups a CU: 1.1 for both
-//   256 x 256    1.5 (32768 x 8192 by 2048: 421 us, 128 x 128 541, 64 x 64 822)
+//   256 x 256    1.5 (32768 x 8192 by 2048: 405 us, 128 x 128 541, 64 x 64 822)
 //   shares       the second kernel takes 3.5, and 8 bytes of each share's sums at 3 TB/s
 //                (64 x 8192 by 2048 channels: one 14.4 us, four 10.4)
 Plan plan_of(const fewbit_mm8* a) {
