@@ -79,6 +79,9 @@ int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x
  *   g = dy w,  dresidual = dh + r (g - h r^2 mean(g h)),
  *   dx = dropout of dresidual before it is rounded,  dw = sum over rows of dy h r.
  *
+ * Squares are formed in fp32: magnitudes past 2^63 make r 0, those below 2^-63
+ * count only as far as eps lets them.
+ *
  * x, residual, dh and dy have `width` contiguous elements per row and strides
  * {outer, row} in elements; rows start at multiples of 16 bytes.  h, y, dx and
  * dresidual are dense, as are codes; scale has one float per row.  Everything

@@ -82,7 +82,8 @@ def dropout(x, p, seed, site=0):
 
 class Dropout(torch.nn.Module):
     """Dropout that keeps no mask.  Without a seed each call in training draws one
-    from torch's generator of the host."""
+    from torch's generator of the host (and a captured graph repeats it: give it
+    one on the device)."""
 
     def __init__(self, p: float = 0.5, site: int = 0):
         super().__init__()

@@ -515,6 +515,49 @@ def test_on_another_stream():
     assert all(torch.equal(a, b) for a, b in zip(want, got))
 
 
+def test_far_into_tensors():
+    """Offsets past 2^32 bytes: the last rows are those of a call on them alone."""
+    rows, width = 270001, 8192
+    x = torch.full((rows, width), 0.5, dtype=BF16, device="cuda")
+    x[-3:] = randn(gen(1), 3, width, dtype=BF16)
+    w = randn(gen(2), width, dtype=BF16)
+    h, y = P.residual_norm_fwd(x, x, w)
+    assert torch.equal(h[-3:], 2 * x[-3:]) and torch.equal(y[-3:], P.residual_norm_fwd(x[-3:], x[-3:], w)[1])
+    h, codes, scale = P.residual_norm_int8(x, x, w)
+    small = P.residual_norm_int8(x[-3:], x[-3:], w)
+    assert torch.equal(codes[-3:], small[1]) and torch.equal(scale[-3:], small[2])
+    dx, dres, _ = P.residual_norm_bwd(x, x, h, w, p=0.25, seed=9)
+    small = P.residual_norm_bwd(x[-3:], x[-3:], h[-3:], w, p=0.25, seed=9)
+    m, k = R.kept(3 * width, 0.25, 9, 0, first=(rows - 3) * width // 8)
+    m = torch.from_numpy(m).cuda().view(3, width)
+    assert torch.equal(dres[-3:], small[1]) and (dx[-3:][~m] == 0).all() and (dx[-3:][m] != 0).float().mean() > 0.99
+    del x, h, y, codes, dx, dres
+    rows, out = 70001, 32768
+    x, xs, w, ws, b = product_inputs(rows, out, 32, BF16)
+    y = P.int8_linear(x, xs, w, ws, b)
+    assert torch.equal(y[-200:], P.int8_linear(x[-200:].clone(), xs[-200:].clone(), w, ws, b))
+    del y
+    torch.cuda.empty_cache()
+
+
+def test_two_streams_at_once():
+    """Products with workspaces and backward passes of two streams, a few after one another on each."""
+    a, b = (product_inputs(64, 512, 8192, BF16, seed) for seed in (0, 1))
+    x, res, w, dh, dy = norm_inputs(BF16, 700, 1024)
+    want = [P.int8_linear(*t) for t in (a, b)], [P.residual_norm_bwd(dh, t, x, w) for t in (dy, dh)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [[], []]
+    for _ in range(5):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                got[i].append((P.int8_linear(*(a, b)[i]), P.residual_norm_bwd(dh, (dy, dh)[i], x, w)))
+    torch.cuda.synchronize()
+    for i in range(2):
+        for product, grads in got[i]:
+            assert torch.equal(product, want[0][i]) and all(torch.equal(s, t) for s, t in zip(grads, want[1][i]))
+
+
 # ---------------------------------------------------------------- together
 def test_layers_of_8_bits():
     """A linear layer and its 8-bit form, and that of codes that come with their scales."""
