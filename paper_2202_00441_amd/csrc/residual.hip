@@ -299,7 +299,7 @@ struct BwdArgs {
 
 // Lanes add dw up in registers over all their rows, waves that have rows of their own in
 // LDS, and a second kernel adds the workgroups' sums, each in a fixed order.  32768 x 2048 bf16
-// with dropout: 116 us with the second kernel's 5, 5.8 TB/s.
+// with dropout: 114 us with the second kernel's 4, 5.9 TB/s.
 template <int DT, int WAVES, int CHUNKS, bool DROP>
 __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_bwd_kernel(const BwdArgs a) {
   using T = typename Store<DT>::type;
@@ -377,21 +377,24 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_bwd_kernel(const
   }
 }
 
-// The sums of the workgroups' rows of `width` floats: a workgroup takes 8 columns, 128 sums
-// of every 128th row each, then adds those in pairs.
-constexpr int kColumns = 8, kRows = 128;
+// The sums of the workgroups' rows of `width` floats: a workgroup takes 32 columns, a line of
+// each row, 32 sums of every 32nd row each, then adds those in pairs.  (Eight columns by 128
+// sums fetch every line four times, on as many XCDs: 8192 x 8192 bf16 with both kernels 126 us,
+// so 118.)
+constexpr int kColumns = 32, kRows = 32;
 __global__ __launch_bounds__(kColumns* kRows) void rnorm_sum_kernel(const float* parts, int rows, int width, float* dw) {
   __shared__ float sums[kRows][kColumns];
-  const int col = blockIdx.x * kColumns + threadIdx.x % kColumns, row = threadIdx.x / kColumns;
+  const int at = threadIdx.x % kColumns, col = blockIdx.x * kColumns + at, row = threadIdx.x / kColumns;
   float sum = 0.0f;
+  if (col < width)
 #pragma unroll 8
-  for (int r = row; r < rows; r += kRows) sum += parts[static_cast<int64_t>(r) * width + col];
-  sums[row][threadIdx.x % kColumns] = sum;
+    for (int r = row; r < rows; r += kRows) sum += parts[static_cast<int64_t>(r) * width + col];
+  sums[row][at] = sum;
   for (int n = kRows / 2; n > 0; n /= 2) {
     __syncthreads();
-    if (row < n) sums[row][threadIdx.x % kColumns] += sums[row + n][threadIdx.x % kColumns];
+    if (row < n) sums[row][at] += sums[row + n][at];
   }
-  if (row == 0) dw[col] = sums[0][threadIdx.x];
+  if (row == 0 && col < width) dw[col] = sums[0][at];
 }
 
 // ---------------------------------------------------------------- host side
@@ -611,6 +614,6 @@ extern "C" int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const voi
                                                                     : start_back<FEWBIT_BF16>(a, r, s));
     if (rc != FEWBIT_OK) return rc;
   }
-  return launch_status("fewbit_rnorm_bwd", launch(rnorm_sum_kernel, dim3(a->width / kColumns), kColumns * kRows, s,
+  return launch_status("fewbit_rnorm_bwd", launch(rnorm_sum_kernel, dim3((a->width + kColumns - 1) / kColumns), kColumns * kRows, s,
                                                   static_cast<const float*>(workspace), static_cast<int>(groups), a->width, dw));
 }

@@ -14,8 +14,9 @@ below its normal range are off by at most 2^-25 besides.
   dresidual 36 such roundings of r in each term, the same number for the mean of products
             (three roundings each): 100 * 2^-24 of |dh| + r (|g| + |h r| mean|g h r|), and u
             of the result.  dx: of it before it is rounded, times the scale.
-  dw        n rows are added in runs of at most n / 768 / 4 + 3 + n / 32: 1e-5 of the sum of
-            magnitudes for the n here, which covers r's 36 roundings of 2^-24 too.
+  dw        n rows are added in runs of at most n / 512 + 3 in a workgroup, of the workgroups' sums
+            (at most 512) 16 and then 5: below 80 roundings with r's 36 for the n here, 1e-5 > 80 *
+            2^-24 of the sum of magnitudes.
   codes     equal, everything between h, w and a code being exact here (64 bits hold
             254 |h w| of 16-bit storage and, but for the last of its 56 bits, of fp32).
   scale     36 roundings for r, three for the rest: 40 * 2^-24.
