@@ -25,7 +25,11 @@ Drop drop_of(PyObject* const* args, const at::Tensor& ref) {
     TORCH_CHECK_VALUE(r.seed.numel() == 1 && r.seed.device() == ref.device(), "a seed's tensor must have one element and be on the data's device");
     r.d.seed_at = r.seed.data_ptr<int64_t>();
   } else {
-    r.d.seed = whole(args[1], "seed");
+    // of either sign, or above 2^63
+    const unsigned long long above = PyLong_Check(args[1]) ? PyLong_AsUnsignedLongLong(args[1]) : 0;
+    const bool unsigned64 = PyLong_Check(args[1]) && !PyErr_Occurred();
+    PyErr_Clear();
+    r.d.seed = unsigned64 ? static_cast<int64_t>(above) : whole(args[1], "seed");
   }
   const int64_t site = whole(args[2], "site");
   TORCH_CHECK_VALUE(site >= 0 && site < int64_t{1} << 32, "site must be a whole number of 32 bits");

@@ -310,10 +310,13 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_bwd_kernel(const
   const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const auto place = [&](int c) __attribute__((always_inline)) { return (c * WAVES + (WAVES == 1 ? 0 : wave)) * kWaveElements; };
   const uint32_t bytes = static_cast<uint32_t>(a.width) * sizeof(T);
+  // where 128 registers do not hold a row's four tensors, w and dh are read where they are used
+  constexpr bool kLate = WAVES == 16 && CHUNKS == 4;
   float w[CHUNKS][8], dw[CHUNKS][8] = {};
   const Stream sw(a.w, bytes);
+  if constexpr (!kLate)
 #pragma unroll
-  for (int c = 0; c < CHUNKS; ++c) E::template load<0>(sw, place(c), lane, w[c]);
+    for (int c = 0; c < CHUNKS; ++c) E::template load<0>(sw, place(c), lane, w[c]);
   [[maybe_unused]] const Key key = DROP ? key_of(a.drop) : Key{};
   int turn = 0;
   for (uint32_t row = blockIdx.x * G::kRows + (WAVES == 1 ? wave : 0); row < a.total; row += gridDim.x * G::kRows, turn ^= 1) {
@@ -325,22 +328,28 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_bwd_kernel(const
     for (int c = 0; c < CHUNKS; ++c) {
       E::template load<kNt>(sh, place(c), lane, h[c]);
       E::template load<kNt>(sy, place(c), lane, g[c]);
-      E::template load<kNt>(sd, place(c), lane, d[c]);
+      if constexpr (!kLate) E::template load<kNt>(sd, place(c), lane, d[c]);
     }
     float sum[2] = {0.0f, 0.0f};
 #pragma unroll
-    for (int c = 0; c < CHUNKS; ++c)
+    for (int c = 0; c < CHUNKS; ++c) {
+      if constexpr (kLate) E::template load<0>(sw, place(c), lane, w[c]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         sum[0] += h[c][i] * h[c][i];
         sum[1] += g[c][i] * w[c][i] * h[c][i];
       }
+    }
     over_row<WAVES>(sum, parts[turn], Add());
     const float r = 1.0f / sqrtf(sum[0] / a.width + a.eps);
     const float mean = sum[1] * r / a.width;              // of g h r
     const Stream dx(static_cast<T*>(a.dx) + dense, bytes), dres(static_cast<T*>(a.dres) + dense, a.dres ? bytes : 0);
 #pragma unroll
     for (int c = 0; c < CHUNKS; ++c) {
+      if constexpr (kLate) {
+        E::template load<0>(sw, place(c), lane, w[c]);
+        E::template load<kNt>(sd, place(c), lane, d[c]);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float u = h[c][i] * r;

@@ -9,8 +9,8 @@ launched.  dropout and residual_norm are the same as differentiable functions:
 they take any layout, copying tensors that the kernels cannot read; dropout
 keeps nothing, residual_norm its sum, which the next addition reads anyway.
 
-Wherever elements are dropped, `seed` is a whole number of 64 bits or an int64
-tensor of one element on the data's device, read when the kernels run: a
+Wherever elements are dropped, `seed` is a whole number of 64 bits (with or
+without a sign) or an int64 tensor of one element on the data's device, read when the kernels run: a
 captured graph draws anew where the program changes it between replays.  `site`
 (32 bits) tells apart places that share a seed.  The backward needs the same p,
 seed and site.  p is taken in steps of 2^-16; what is dropped becomes 0 whatever

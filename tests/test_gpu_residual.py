@@ -134,6 +134,27 @@ def test_dropout_differentiable_with_any_layout_and_broadcast_gradients():
     assert P.dropout(torch.empty(0, 8, device="cuda"), 0.3, 1).shape == (0, 8)
 
 
+def test_dropout_keeps_nothing_and_the_norm_its_sum():
+    kept = []
+    x, res, w, _, _ = norm_inputs(BF16, 20, 64)
+    x, res = x.requires_grad_(), res.requires_grad_()
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: kept.append(t) or t, lambda t: t):
+        P.dropout(x, 0.5, 1)
+        assert kept == []
+        h, y = P.residual_norm(x, res, w, p=0.5, seed=1)
+    assert {t.data_ptr() for t in kept} == {h.data_ptr(), w.data_ptr()}
+
+
+def test_seeds_of_64_bits():
+    x = randn(gen(9), 1000)
+    assert torch.equal(P.dropout_fwd(x, 0.5, 2 ** 64 - 3), P.dropout_fwd(x, 0.5, -3))
+    assert torch.equal(P.dropout_fwd(x, 0.5, torch.tensor(-3, device="cuda")), P.dropout_fwd(x, 0.5, -3))
+    assert torch.equal(P.dropout_fwd(x, 0.5, -2 ** 63), P.dropout_fwd(x, 0.5, 2 ** 63))
+    for bad in (2 ** 64, -2 ** 63 - 1):
+        with pytest.raises(TypeError):
+            P.dropout_fwd(x, 0.5, bad)
+
+
 def test_dropout_module():
     d = P.Dropout(0.4, site=3)
     x = randn(gen(4), 64, 40)
