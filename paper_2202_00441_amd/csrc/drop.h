@@ -108,6 +108,15 @@ struct Chunk {
   }
 };
 
+// A kept element.  The product passes an empty register barrier where it may be stored in fp16:
+// the compiler would round it straight to that, and the result would not be that of fp32.
+template <class T>
+__device__ __forceinline__ float scaled(float x, const Drop& d) {
+  x *= d.scale;
+  if constexpr (__is_same(T, _Float16)) asm("" : "+v"(x));
+  return x;
+}
+
 // A lane's elements of the 512 from 8 * block on.  Of 32-bit elements two lanes share a block
 // in each access: the even one runs the generator for the first, the odd one for the second,
 // and they hand each other the other's half.
@@ -133,7 +142,7 @@ __device__ __forceinline__ void drop(const Drop& d, Key key, uint64_t block, int
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     const uint32_t u = i % 2 ? c[i / 2] >> 16 : c[i / 2] & 0xFFFFu;
-    x[i] = u >= d.border ? x[i] * d.scale : 0.0f;
+    x[i] = u >= d.border ? scaled<T>(x[i], d) : 0.0f;
   }
 }
 

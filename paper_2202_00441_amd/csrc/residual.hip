@@ -50,7 +50,7 @@ __global__ __launch_bounds__(kDropThreads) void drop_kernel(const void* x, void*
   const uint32_t word = lane < 4 ? (lane < 2 ? c[0] : c[1]) : (lane < 6 ? c[2] : c[3]);
   const uint32_t u = lane % 2 ? word >> 16 : word & 0xFFFFu;
   const int64_t at = whole * 8 + lane;
-  static_cast<T*>(y)[at] = static_cast<T>(u >= d.border ? static_cast<float>(static_cast<const T*>(x)[at]) * d.scale : 0.0f);
+  static_cast<T*>(y)[at] = static_cast<T>(u >= d.border ? scaled<T>(static_cast<float>(static_cast<const T*>(x)[at]), d) : 0.0f);
 }
 
 // ---------------------------------------------------------------- rows
