@@ -92,13 +92,13 @@ int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x
 #define FEWBIT_RNORM_MOST 32768   /* elements of a row                         */
 
 typedef struct fewbit_rnorm {
-    int32_t dtype;                /* storage type of all but scale and dw      */
+    int32_t dtype;                /* storage type of all but scale (and dw)    */
     int32_t width;                /* a multiple of 8, 8 .. FEWBIT_RNORM_MOST   */
     int64_t outer, rows;
     int64_t x_stride[2], residual_stride[2];
     int64_t dh_stride[2], dy_stride[2];
     float eps;                    /* >= 0, finite                              */
-    int32_t reserved;             /* must be 0                                 */
+    int32_t dw_dtype;             /* storage type of dw: FEWBIT_F32 or dtype   */
     fewbit_drop drop;             /* p = 0: none                               */
 } fewbit_rnorm;
 
@@ -118,7 +118,7 @@ int64_t fewbit_rnorm_workspace(const fewbit_rnorm* a);
 /* dresidual may be NULL: it is not written then.  Where p takes nothing away
  * dx is it, and dresidual has to be NULL. */
 int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const void* dy, const void* h,
-                     const void* w, void* dx, void* dresidual, float* dw, void* workspace,
+                     const void* w, void* dx, void* dresidual, void* dw, void* workspace,
                      int64_t workspace_bytes, void* stream);
 
 /* ------------------------------------------------------------------ */

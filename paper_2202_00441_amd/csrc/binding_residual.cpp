@@ -196,11 +196,12 @@ PyObject* rows8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-// rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual) -> (dx, dresidual, dweight), or a status.
-// dresidual is dx where nothing is dropped, None where it is not asked for.
+// rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual, rounded) -> (dx, dresidual, dweight), or a status.
+// dresidual is dx where nothing is dropped, None where it is not asked for; dweight is fp32, or, rounded, of
+// weight's type.
 PyObject* rnorm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
-  TORCH_CHECK_TYPE(nargs == 9, "rnorm_bwd takes nine arguments");
+  TORCH_CHECK_TYPE(nargs == 10, "rnorm_bwd takes ten arguments");
   check_mode();
   const at::Tensor dh = optional(args[0], "dh");
   const at::Tensor &dy = tensor(args[1], "dy"), &h = tensor(args[2], "h"), &w = tensor(args[3], "weight");
@@ -214,6 +215,7 @@ PyObject* rnorm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   const Drop p = drop_of(args + 5, h);
   a.drop = p.d;
   const bool apart = truth(args[8], "residual") && p.some;
+  if (truth(args[9], "rounded")) a.dw_dtype = a.dtype;
   check_same(dy, "dy", h, "h");
   check_shape(dy, "dy", h.sizes());
   strides_of(dy, "dy", a.dy_stride);
@@ -230,12 +232,12 @@ PyObject* rnorm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     const c10::DeviceGuard guard(h.device());
     dx = at::empty(h.sizes(), h.options());
     if (apart) dres = at::empty(h.sizes(), h.options());
-    dw = at::empty(w.sizes(), w.options().dtype(at::kFloat));
+    dw = at::empty(w.sizes(), a.dw_dtype == a.dtype ? w.options() : w.options().dtype(at::kFloat));
     const int64_t need = fewbit_rnorm_workspace(&a);
     const at::Tensor work = bytes(need, h);
     rc = need < 0 ? static_cast<int>(need)
                   : fewbit_rnorm_bwd(&a, pointer(dh), dy.data_ptr(), h.data_ptr(), w.data_ptr(), dx.data_ptr(), pointer(dres),
-                                     dw.data_ptr<float>(), pointer(work), need, stream_of(h));
+                                     dw.data_ptr(), pointer(work), need, stream_of(h));
   }
   if (rc != FEWBIT_OK) return PyLong_FromLong(rc);
   if (!p.some) dres = dx;

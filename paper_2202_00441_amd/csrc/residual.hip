@@ -391,7 +391,8 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_bwd_kernel(const
 // sums fetch every line four times, on as many XCDs: 8192 x 8192 bf16 with both kernels 126 us,
 // so 118.)
 constexpr int kColumns = 32, kRows = 32;
-__global__ __launch_bounds__(kColumns* kRows) void rnorm_sum_kernel(const float* parts, int rows, int width, float* dw) {
+template <int DT>
+__global__ __launch_bounds__(kColumns* kRows) void rnorm_sum_kernel(const float* parts, int rows, int width, void* dw) {
   __shared__ float sums[kRows][kColumns];
   const int at = threadIdx.x % kColumns, col = blockIdx.x * kColumns + at, row = threadIdx.x / kColumns;
   float sum = 0.0f;
@@ -403,14 +404,14 @@ __global__ __launch_bounds__(kColumns* kRows) void rnorm_sum_kernel(const float*
     __syncthreads();
     if (row < n) sums[row][at] += sums[row + n][at];
   }
-  if (row == 0 && col < width) dw[col] = sums[0][at];
+  if (row == 0 && col < width) static_cast<typename Store<DT>::type*>(dw)[col] = static_cast<typename Store<DT>::type>(sums[0][at]);
 }
 
 // ---------------------------------------------------------------- host side
 int check(const fewbit_rnorm* a) {
   if (!a) return FEWBIT_E_NULL;
   if (a->dtype < FEWBIT_F32 || a->dtype > FEWBIT_BF16) return FEWBIT_E_DTYPE;
-  if (a->reserved != 0 || a->outer < 0 || a->rows < 0) return FEWBIT_E_INVALID;
+  if ((a->dw_dtype != FEWBIT_F32 && a->dw_dtype != a->dtype) || a->outer < 0 || a->rows < 0) return FEWBIT_E_INVALID;
   if (a->width < 8 || a->width % 8 != 0 || a->width > FEWBIT_RNORM_MOST) return FEWBIT_E_INVALID;
   if (!(a->eps >= 0.0f && std::isfinite(a->eps))) return FEWBIT_E_INVALID;
   // rows are counted in 31 bits
@@ -582,7 +583,7 @@ extern "C" int64_t fewbit_rnorm_workspace(const fewbit_rnorm* a) {
 }
 
 extern "C" int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const void* dy, const void* h, const void* w, void* dx, void* dresidual,
-                                float* dw, void* workspace, int64_t workspace_bytes, void* stream) {
+                                void* dw, void* workspace, int64_t workspace_bytes, void* stream) {
   int rc = check(a);
   if (rc != FEWBIT_OK) return rc;
   BwdArgs r{};
@@ -623,6 +624,7 @@ extern "C" int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const voi
                                                                     : start_back<FEWBIT_BF16>(a, r, s));
     if (rc != FEWBIT_OK) return rc;
   }
-  return launch_status("fewbit_rnorm_bwd", launch(rnorm_sum_kernel, dim3((a->width + kColumns - 1) / kColumns), kColumns * kRows, s,
+  const auto sum = a->dw_dtype == FEWBIT_F32 ? rnorm_sum_kernel<FEWBIT_F32> : a->dw_dtype == FEWBIT_F16 ? rnorm_sum_kernel<FEWBIT_F16> : rnorm_sum_kernel<FEWBIT_BF16>;
+  return launch_status("fewbit_rnorm_bwd", launch(sum, dim3((a->width + kColumns - 1) / kColumns), kColumns * kRows, s,
                                                   static_cast<const float*>(workspace), static_cast<int>(groups), a->width, dw));
 }

@@ -122,14 +122,14 @@ def residual_norm_bwd(dh, dy, h, weight, eps=1e-6, p=0.0, seed=0, site=0, residu
     """(dx, dresidual, dweight) from the gradients of h (None: none) and y; h as
     residual_norm_fwd gave it; dweight is fp32.  Without dropout dresidual is dx;
     residual=False with dropout: it is not formed (None)."""
-    return _result(_native.rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual), "fewbit_rnorm_bwd")
+    return _result(_native.rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual, False), "fewbit_rnorm_bwd")
 
 
 class ResidualNorm(torch.autograd.Function):
     @staticmethod
     def forward(ctx, x, residual, weight, eps, p, seed, site):
         ctx.set_materialize_grads(False)
-        x, weight = _rows2(x), _rows(weight)
+        x, weight = _rows2(x), _flat(weight)
         residual = None if residual is None else _rows2(residual)
         h, y = residual_norm_fwd(x, residual, weight, eps, p, seed, site)
         _keep_seed(ctx, seed, _flat(h), weight)
@@ -146,13 +146,16 @@ class ResidualNorm(torch.autograd.Function):
         dh = None if dh is None else _rows2(dh)
         eps, p, site = ctx.rest
         need = ctx.needs_input_grad[1]
-        dx, dresidual, dweight = residual_norm_bwd(dh, dy, h, weight, eps, p, _kept_seed(ctx), site, need)
-        return dx, dresidual if need else None, dweight.to(weight.dtype), None, None, None, None
+        dx, dresidual, dweight = _result(_native.rnorm_bwd(dh, dy, h, weight, eps, p, _kept_seed(ctx), site, need, True),
+                                         "fewbit_rnorm_bwd")
+        return dx, dresidual if need else None, dweight, None, None, None, None
 
 
 def _rows2(t):
     """t, or a contiguous copy of it where its rows are not contiguous, do not start at multiples of 16
     bytes, or their first axes are not one step apart."""
+    if t.is_contiguous() and t.data_ptr() % 16 == 0:
+        return t
     t = _rows(t)
     ahead = [(n, s) for n, s in zip(t.shape[:-2], t.stride()[:-2]) if n > 1]
     if all(s == n2 * s2 for (_, s), (n2, s2) in zip(ahead, ahead[1:])):

@@ -31,7 +31,7 @@ class Drop(C.Structure):
 class Rnorm(C.Structure):
     _fields_ = [("dtype", C.c_int32), ("width", C.c_int32), ("outer", C.c_int64), ("rows", C.c_int64),
                 ("x_stride", C.c_int64 * 2), ("residual_stride", C.c_int64 * 2), ("dh_stride", C.c_int64 * 2),
-                ("dy_stride", C.c_int64 * 2), ("eps", C.c_float), ("reserved", C.c_int32), ("drop", Drop)]
+                ("dy_stride", C.c_int64 * 2), ("eps", C.c_float), ("dw_dtype", C.c_int32), ("drop", Drop)]
 
 
 class Mm8(C.Structure):
@@ -150,7 +150,7 @@ def bwd(a, dh=A, dy=A, h=A, w=A, dx=A, dres=None, dw=A, work=A, size=1 << 40):
 @pytest.mark.parametrize("changes,status", (
     ({"dtype": 3}, E_DTYPE), ({"dtype": -1}, E_DTYPE), ({"width": 0}, E_INVALID), ({"width": 12}, E_INVALID), ({"width": 32776}, E_INVALID),
     ({"outer": -1}, E_INVALID), ({"rows": -1}, E_INVALID), ({"rows": 1 << 31}, E_INVALID), ({"outer": 1 << 16, "rows": 1 << 15}, E_INVALID),
-    ({"eps": -1.0}, E_INVALID), ({"eps": float("inf")}, E_INVALID), ({"eps": float("nan")}, E_INVALID), ({"reserved": 1}, E_INVALID)))
+    ({"eps": -1.0}, E_INVALID), ({"eps": float("inf")}, E_INVALID), ({"eps": float("nan")}, E_INVALID), ({"dw_dtype": P.F16}, E_INVALID), ({"dw_dtype": 3}, E_INVALID)))
 def test_norm_refusals(changes, status):
     a = rnorm(**changes)
     assert fwd(a) == int8(a) == rows8(a) == bwd(a) == LIB.fewbit_rnorm_workspace(C.byref(a)) == status
@@ -163,7 +163,7 @@ def test_norm_arguments():
         assert f(None) == E_NULL
         for name in names:
             assert f(a, **{name: None}) == E_NULL, name
-            if name not in ("scale", "dw"):          # written a float at a time
+            if name not in ("scale", "dw"):          # written an element at a time
                 assert f(a, **{name: ODD}) == E_ALIGN, name
     assert fwd(a, res=ODD) == int8(a, res=ODD) == bwd(a, dh=ODD) == bwd(p, dres=ODD) == E_ALIGN
     assert fwd(p, res=None, h=None) == E_NULL            # the sum of dropout alone is written
