@@ -164,6 +164,19 @@ PyObject* bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   throw e;
 }
 
+}  // namespace
+
+void binding::throw_status(int rc, const char* where) {
+  pybind11::gil_scoped_acquire gil;
+  if (PyObject* e = PyObject_CallFunction(error_class, "is", rc, where)) {
+    PyErr_SetObject(error_class, e);
+    Py_DECREF(e);
+  }
+  throw_python();
+}
+
+namespace {
+
 // The gradient of one call of the layer.
 at::Tensor layer_grad(const fewbit_table& t, const at::Tensor& grad, const at::Tensor& codes) {
   const at::Tensor g = grad.contiguous();
@@ -174,12 +187,7 @@ at::Tensor layer_grad(const fewbit_table& t, const at::Tensor& grad, const at::T
     at::Tensor gin = at::empty_like(g);
     const int rc = run_bwd(t, g, codes, gin);
     if (rc == FEWBIT_OK) return gin;
-    pybind11::gil_scoped_acquire gil;
-    if (PyObject* e = PyObject_CallFunction(error_class, "is", rc, "fewbit_bwd")) {
-      PyErr_SetObject(error_class, e);
-      Py_DECREF(e);
-    }
-    throw_python();
+    throw_status(rc, "fewbit_bwd");
   }
   // codes that a hook has moved or replaced, a gradient of another kind
   pybind11::gil_scoped_acquire gil;

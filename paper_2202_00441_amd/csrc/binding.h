@@ -44,6 +44,9 @@ inline void* stream_of(const at::Tensor& t) {
   return c10::hip::getCurrentHIPStreamMasqueradingAsCUDA(t.device().index()).stream();
 }
 
+// Throws the package's exception of a status, on any thread.
+[[noreturn]] void throw_status(int rc, const char* where);
+
 // The block operators' calls (binding_block.cpp).
 PyMethodDef* block_methods();
 // Those between its products (binding_residual.cpp).

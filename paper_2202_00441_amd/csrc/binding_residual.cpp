@@ -1,5 +1,8 @@
 // binding_residual.cpp -- the calls on torch tensors of the operators between a block's
 // products and of the product in 8-bit integers; as binding_block.cpp does it.
+#include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+
 #include "binding_args.h"
 #include "fewbit_residual.h"
 
@@ -37,6 +40,15 @@ Drop drop_of(PyObject* const* args, const at::Tensor& ref) {
   return r;
 }
 
+// x with elements dropped; x as check_dense has it.
+at::Tensor run_dropout(const at::Tensor& x, const fewbit_drop& d, int& rc) {
+  at::AutoDispatchBelowADInplaceOrView below;
+  const c10::DeviceGuard guard(x.device());
+  at::Tensor y = at::empty(x.sizes(), x.options());
+  rc = fewbit_dropout(&d, storage_type(x), x.numel(), x.data_ptr(), y.data_ptr(), stream_of(x));
+  return y;
+}
+
 // dropout(x, p, seed, site) -> y, or a status
 PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
@@ -50,10 +62,7 @@ PyObject* dropout(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    at::AutoDispatchBelowADInplaceOrView below;
-    const c10::DeviceGuard guard(x.device());
-    y = at::empty(x.sizes(), x.options());
-    rc = fewbit_dropout(&p.d, storage_type(x), x.numel(), x.data_ptr(), y.data_ptr(), stream_of(x));
+    y = run_dropout(x, p.d, rc);
   }
   return rc == FEWBIT_OK ? THPVariable_Wrap(y) : PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
@@ -72,8 +81,8 @@ void rows_of(const at::Tensor& t, fewbit_rnorm& a) {
                     "there must be fewer than 2^31 rows");
 }
 
-// Strides {outer, row}; the axes before the last two have to be one.
-void strides_of(const at::Tensor& t, const char* name, int64_t (&s)[2]) {
+// Strides {outer, row}, or false; the axes before the last two have to be one.
+bool strides_fit(const at::Tensor& t, int64_t (&s)[2]) {
   const int64_t per = 16 / t.element_size(), n = t.dim();
   bool fits = reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0 && (t.size(n - 1) <= 1 || t.stride(n - 1) == 1);
   s[1] = n > 1 && t.size(n - 2) > 1 ? t.stride(n - 2) : 0;
@@ -88,7 +97,10 @@ void strides_of(const at::Tensor& t, const char* name, int64_t (&s)[2]) {
     next = t.stride(i) * t.size(i);
   }
   for (const int64_t v : s) fits = fits && v % per == 0;
-  TORCH_CHECK_VALUE(fits || t.numel() == 0, name, " must have contiguous rows that start at multiples of 16 bytes, in at most two even steps");
+  return fits || t.numel() == 0;
+}
+void strides_of(const at::Tensor& t, const char* name, int64_t (&s)[2]) {
+  TORCH_CHECK_VALUE(strides_fit(t, s), name, " must have contiguous rows that start at multiples of 16 bytes, in at most two even steps");
 }
 
 float eps_of(PyObject* o) {
@@ -119,6 +131,17 @@ fewbit_rnorm forward_of(const at::Tensor& x, const at::Tensor& residual, const a
   return a;
 }
 
+struct Sum {
+  at::Tensor h, y;
+};
+Sum run_rnorm(const fewbit_rnorm& a, const at::Tensor& x, const at::Tensor& residual, const at::Tensor& w, bool sums, int& rc) {
+  at::AutoDispatchBelowADInplaceOrView below;
+  const c10::DeviceGuard guard(x.device());
+  Sum r{sums ? at::empty(x.sizes(), x.options()) : x, at::empty(x.sizes(), x.options())};
+  rc = fewbit_rnorm_fwd(&a, x.data_ptr(), pointer(residual), w.data_ptr(), sums ? r.h.data_ptr() : nullptr, r.y.data_ptr(), stream_of(x));
+  return r;
+}
+
 // rnorm_fwd(x, residual, weight, eps, p, seed, site) -> (h, y), or a status; h is x where nothing is added or dropped
 PyObject* rnorm_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   HANDLE_TH_ERRORS
@@ -129,18 +152,13 @@ PyObject* rnorm_fwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   fewbit_rnorm a = forward_of(x, residual, w, args[3]);
   const Drop p = drop_of(args + 4, x);
   a.drop = p.d;
-  at::Tensor h = x, y;
+  Sum r;
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    at::AutoDispatchBelowADInplaceOrView below;
-    const c10::DeviceGuard guard(x.device());
-    if (residual.defined() || p.some) h = at::empty(x.sizes(), x.options());
-    y = at::empty(x.sizes(), x.options());
-    rc = fewbit_rnorm_fwd(&a, x.data_ptr(), pointer(residual), w.data_ptr(), residual.defined() || p.some ? h.data_ptr() : nullptr,
-                          y.data_ptr(), stream_of(x));
+    r = run_rnorm(a, x, residual, w, residual.defined() || p.some, rc);
   }
-  return rc == FEWBIT_OK ? tuple_of(h, y) : PyLong_FromLong(rc);
+  return rc == FEWBIT_OK ? tuple_of(r.h, r.y) : PyLong_FromLong(rc);
   END_HANDLE_TH_ERRORS
 }
 
@@ -196,6 +214,23 @@ PyObject* rows8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
+struct Gradients {
+  at::Tensor dx, dres, dw;
+};
+Gradients run_rnorm_bwd(const fewbit_rnorm& a, const at::Tensor& dh, const at::Tensor& dy, const at::Tensor& h, const at::Tensor& w, bool apart,
+                        int& rc) {
+  at::AutoDispatchBelowADInplaceOrView below;
+  const c10::DeviceGuard guard(h.device());
+  Gradients g{at::empty(h.sizes(), h.options()), apart ? at::empty(h.sizes(), h.options()) : at::Tensor(),
+              at::empty(w.sizes(), a.dw_dtype == a.dtype ? w.options() : w.options().dtype(at::kFloat))};
+  const int64_t need = fewbit_rnorm_workspace(&a);
+  const at::Tensor work = bytes(need, h);
+  rc = need < 0 ? static_cast<int>(need)
+                : fewbit_rnorm_bwd(&a, pointer(dh), dy.data_ptr(), h.data_ptr(), w.data_ptr(), g.dx.data_ptr(), pointer(g.dres), g.dw.data_ptr(),
+                                   pointer(work), need, stream_of(h));
+  return g;
+}
+
 // rnorm_bwd(dh, dy, h, weight, eps, p, seed, site, residual, rounded) -> (dx, dresidual, dweight), or a status.
 // dresidual is dx where nothing is dropped, None where it is not asked for; dweight is fp32, or, rounded, of
 // weight's type.
@@ -224,26 +259,17 @@ PyObject* rnorm_bwd(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     check_shape(dh, "dh", h.sizes());
     strides_of(dh, "dh", a.dh_stride);
   }
-  at::Tensor dx, dres, dw;
+  Gradients g;
   int rc;
   {
     pybind11::gil_scoped_release no_gil;
-    at::AutoDispatchBelowADInplaceOrView below;
-    const c10::DeviceGuard guard(h.device());
-    dx = at::empty(h.sizes(), h.options());
-    if (apart) dres = at::empty(h.sizes(), h.options());
-    dw = at::empty(w.sizes(), a.dw_dtype == a.dtype ? w.options() : w.options().dtype(at::kFloat));
-    const int64_t need = fewbit_rnorm_workspace(&a);
-    const at::Tensor work = bytes(need, h);
-    rc = need < 0 ? static_cast<int>(need)
-                  : fewbit_rnorm_bwd(&a, pointer(dh), dy.data_ptr(), h.data_ptr(), w.data_ptr(), dx.data_ptr(), pointer(dres),
-                                     dw.data_ptr(), pointer(work), need, stream_of(h));
+    g = run_rnorm_bwd(a, dh, dy, h, w, apart, rc);
   }
   if (rc != FEWBIT_OK) return PyLong_FromLong(rc);
-  if (!p.some) dres = dx;
+  if (!p.some) g.dres = g.dx;
   THPObjectPtr r(PyTuple_New(3));
   if (!r) return nullptr;
-  const at::Tensor* items[] = {&dx, &dres, &dw};
+  const at::Tensor* items[] = {&g.dx, &g.dres, &g.dw};
   for (int i = 0; i < 3; ++i) {
     PyObject* o = items[i]->defined() ? THPVariable_Wrap(*items[i]) : Py_NewRef(Py_None);
     if (!o) return nullptr;
@@ -321,7 +347,147 @@ PyObject* mm8(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
   END_HANDLE_TH_ERRORS
 }
 
-PyMethodDef methods[] = {method<dropout>("dropout"), method<rnorm_fwd>("rnorm_fwd"), method<rnorm_bwd>("rnorm_bwd"),
+// ---------------------------------------------------------------- layers
+// The differentiable calls without Python between them, for ordinary tensors whose layout the
+// kernels take; for everything else they return None before they have done anything, and the
+// package's own functions take over (they also raise what a wrong argument raises).
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+bool ordinary(PyObject* o) {
+  if (!THPVariable_CheckExact(o)) return false;
+  const at::Tensor& t = THPVariable_Unpack(o);
+  return plain(t) && storage_type(t) >= 0 && !t.is_inference() && !t._fw_grad(0).defined();
+}
+bool dense(const at::Tensor& t) { return t.is_contiguous() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0; }
+at::Tensor made_dense(const at::Tensor& t) { return dense(t) ? t : t.clone(at::MemoryFormat::Contiguous); }
+
+// What a backward needs of the dropout; the seed's tensor, if it is one, is saved last.
+void keep(AutogradContext* ctx, const fewbit_drop& d) {
+  ctx->saved_data["p"] = d.p;
+  ctx->saved_data["seed"] = d.seed;
+  ctx->saved_data["site"] = static_cast<int64_t>(d.site);
+}
+fewbit_drop kept(AutogradContext* ctx, const at::Tensor& seed_at) {
+  return {ctx->saved_data["p"].toDouble(), ctx->saved_data["seed"].toInt(), seed_at.defined() ? seed_at.data_ptr<int64_t>() : nullptr,
+          static_cast<uint32_t>(ctx->saved_data["site"].toInt()), 0};
+}
+
+struct DropoutFn : torch::autograd::Function<DropoutFn> {
+  static at::Tensor forward(AutogradContext* ctx, const at::Tensor& x, const fewbit_drop* d, const at::Tensor* seed_at) {
+    keep(ctx, *d);
+    if (seed_at->defined()) ctx->save_for_backward({*seed_at});
+    int rc;
+    at::Tensor y = run_dropout(x, *d, rc);
+    if (rc != FEWBIT_OK) throw_status(rc, "fewbit_dropout");
+    return y;
+  }
+  // The same function of the gradient, to any order.
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    const variable_list saved = ctx->get_saved_variables();
+    const at::Tensor seed_at = saved.empty() ? at::Tensor() : saved[0], dy = made_dense(grads[0]);
+    const fewbit_drop d = kept(ctx, seed_at);
+    at::Tensor dx;
+    if (at::GradMode::is_enabled()) {
+      dx = apply(dy, &d, &seed_at);
+    } else {
+      TORCH_CHECK_VALUE(plain(dy), "the gradient must be an ordinary device tensor");
+      int rc;
+      dx = run_dropout(dy, d, rc);
+      if (rc != FEWBIT_OK) throw_status(rc, "fewbit_dropout");
+    }
+    return {dx, at::Tensor(), at::Tensor()};
+  }
+};
+
+// dropout_layer(x, p, seed, site) -> y with its history, or None
+PyObject* dropout_layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 4 || !plain_mode() || !ordinary(args[0]) || !dense(THPVariable_Unpack(args[0]))) Py_RETURN_NONE;
+  const at::Tensor& x = THPVariable_Unpack(args[0]);
+  const Drop p = drop_of(args + 1, x);
+  at::Tensor y;
+  {
+    pybind11::gil_scoped_release no_gil;
+    y = DropoutFn::apply(x, &p.d, &p.seed);
+  }
+  return THPVariable_Wrap(y);
+  END_HANDLE_TH_ERRORS
+}
+
+struct ResidualNormFn : torch::autograd::Function<ResidualNormFn> {
+  static variable_list forward(AutogradContext* ctx, const at::Tensor& x, const std::optional<at::Tensor>& residual, const at::Tensor& w,
+                               const fewbit_rnorm* a, const at::Tensor* seed_at) {
+    int rc;
+    const Sum r = run_rnorm(*a, x, residual.value_or(at::Tensor()), w, true, rc);
+    if (rc != FEWBIT_OK) throw_status(rc, "fewbit_rnorm_fwd");
+    keep(ctx, a->drop);
+    ctx->saved_data["eps"] = static_cast<double>(a->eps);
+    ctx->saved_data["residual"] = residual.has_value();        // else the weight is the second input
+    variable_list saved{r.h, w};
+    if (seed_at->defined()) saved.push_back(*seed_at);
+    ctx->save_for_backward(std::move(saved));
+    ctx->set_materialize_grads(false);
+    return {r.h, r.y};
+  }
+  static variable_list backward(AutogradContext* ctx, variable_list grads) {
+    variable_list none(5);
+    if (!grads[0].defined() && !grads[1].defined()) return none;
+    const variable_list saved = ctx->get_saved_variables();
+    const at::Tensor &h = saved[0], &w = saved[1];
+    fewbit_rnorm a{};
+    rows_of(h, a);
+    a.dtype = a.dw_dtype = storage_type(h);
+    a.eps = static_cast<float>(ctx->saved_data["eps"].toDouble());
+    a.drop = kept(ctx, saved.size() > 2 ? saved[2] : at::Tensor());
+    at::Tensor dh = grads[0], dy = grads[1].defined() ? grads[1] : at::zeros_like(h);
+    for (const at::Tensor& t : {h, w, dh, dy}) TORCH_CHECK_VALUE(!t.defined() || plain(t), "saved tensors and gradients must be ordinary device tensors");
+    if (dh.defined() && !strides_fit(dh, a.dh_stride)) {
+      dh = dh.clone(at::MemoryFormat::Contiguous);
+      strides_of(dh, "dh", a.dh_stride);
+    }
+    if (!strides_fit(dy, a.dy_stride)) {
+      dy = dy.clone(at::MemoryFormat::Contiguous);
+      strides_of(dy, "dy", a.dy_stride);
+    }
+    const bool some = std::nearbyint(a.drop.p * 65536.0) > 0.0, residual = ctx->saved_data["residual"].toBool() && ctx->needs_input_grad(1);
+    int rc;
+    Gradients g = run_rnorm_bwd(a, dh, dy, made_dense(h), made_dense(w), some && residual, rc);
+    if (rc != FEWBIT_OK) throw_status(rc, "fewbit_rnorm_bwd");
+    if (!some) g.dres = g.dx;
+    variable_list out{g.dx, residual ? g.dres : at::Tensor(), g.dw, at::Tensor(), at::Tensor()};
+    if (!at::GradMode::is_enabled()) return out;
+    // gradients of these gradients are not formed: asking for them raises
+    for (at::Tensor& t : out)
+      if (t.defined()) t = t.detach().set_requires_grad(true);
+    return std::make_shared<torch::autograd::DelayedError>("the gradient of residual_norm cannot be differentiated", static_cast<int64_t>(out.size()))
+        ->operator()(std::move(out));
+  }
+};
+
+// residual_norm_layer(x, residual, weight, eps, p, seed, site) -> (h, y) with their history, or None
+PyObject* residual_norm_layer(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
+  HANDLE_TH_ERRORS
+  if (nargs != 7 || !plain_mode() || !ordinary(args[0]) || !ordinary(args[2]) || (args[1] != Py_None && !ordinary(args[1]))) Py_RETURN_NONE;
+  const at::Tensor &x = THPVariable_Unpack(args[0]), &w = THPVariable_Unpack(args[2]);
+  const at::Tensor residual = args[1] == Py_None ? at::Tensor() : THPVariable_Unpack(args[1]);
+  int64_t s[2];
+  if (x.dim() < 1 || !strides_fit(x, s) || !dense(w) || (residual.defined() && (residual.dim() < 1 || !strides_fit(residual, s)))) Py_RETURN_NONE;
+  fewbit_rnorm a = forward_of(x, residual, w, args[3]);
+  const Drop p = drop_of(args + 4, x);
+  if (!residual.defined() && !p.some) Py_RETURN_NONE;       // h is x
+  a.drop = p.d;
+  variable_list r;
+  {
+    pybind11::gil_scoped_release no_gil;
+    r = ResidualNormFn::apply(x, residual.defined() ? std::optional<at::Tensor>(residual) : std::nullopt, w, &a, &p.seed);
+  }
+  return tuple_of(r[0], r[1]);
+  END_HANDLE_TH_ERRORS
+}
+
+PyMethodDef methods[] = {method<dropout_layer>("dropout_layer"), method<residual_norm_layer>("residual_norm_layer"),
+                         method<dropout>("dropout"), method<rnorm_fwd>("rnorm_fwd"), method<rnorm_bwd>("rnorm_bwd"),
                          method<rnorm_int8>("rnorm_int8"), method<rows8>("rows8"), method<mm8>("mm8"), {nullptr, nullptr, 0, nullptr}};
 
 }  // namespace

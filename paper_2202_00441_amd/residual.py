@@ -69,15 +69,16 @@ class Dropping(torch.autograd.Function):
         return dropout_fwd(_flat(x), p, seed, site)
 
     @staticmethod
-    @torch.autograd.function.once_differentiable
     def backward(ctx, dy):
         p, site = ctx.rest
-        return dropout_bwd(_flat(dy), p, _kept_seed(ctx), site), None, None, None
+        return dropout(dy, p, _kept_seed(ctx), site), None, None, None
 
 
 def dropout(x, p, seed, site=0):
-    """dropout_fwd, differentiable with respect to x; keeps no mask."""
-    return Dropping.apply(x, p, seed, site)
+    """dropout_fwd, differentiable with respect to x, to any order; keeps no mask."""
+    # ordinary device tensors: the same function in C++ (None: not one of those)
+    y = _native.dropout_layer(x, p, seed, site)
+    return Dropping.apply(x, p, seed, site) if y is None else y
 
 
 class Dropout(torch.nn.Module):
@@ -165,7 +166,8 @@ def _rows2(t):
 
 def residual_norm(x, residual, weight, eps=1e-6, p=0.0, seed=0, site=0):
     """residual_norm_fwd, differentiable with respect to x, residual and weight."""
-    return ResidualNorm.apply(x, residual, weight, eps, p, seed, site)
+    r = _native.residual_norm_layer(x, residual, weight, eps, p, seed, site)
+    return ResidualNorm.apply(x, residual, weight, eps, p, seed, site) if r is None else r
 
 
 # ---------------------------------------------------------------- 8-bit integers

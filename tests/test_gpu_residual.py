@@ -144,6 +144,48 @@ def test_dropout_differentiable_with_any_layout_and_broadcast_gradients():
     assert P.dropout(torch.empty(0, 8, device="cuda"), 0.3, 1).shape == (0, 8)
 
 
+@pytest.mark.parametrize("strided", (False, True))
+def test_layers_differentiated_twice(strided):
+    """Dropout's gradient is dropout again, to any order; the norm's raises.  By both of the layers' paths."""
+    g = gen(12)
+    x = (randn(g, 24, 40).t() if strided else randn(g, 40, 24)).requires_grad_()
+    y = P.dropout(x, 0.5, 3)
+    dx, = torch.autograd.grad((y * y).sum(), x, create_graph=True)
+    m, k = mask(x.shape, 0.5, 3)
+    assert torch.equal(dx, torch.where(m, 2 * k * k * x, 0.0))
+    ddx, = torch.autograd.grad(dx.sum(), x)
+    assert torch.equal(ddx, torch.where(m, torch.full_like(ddx, 2 * k * k), 0.0))
+    w = torch.ones(24, device="cuda", requires_grad=True)
+    h, y = P.residual_norm(x, None if strided else x.detach(), w, p=0.0 if strided else 0.5, seed=1)
+    dx, dw = torch.autograd.grad((y * y * y).sum(), (x, w), create_graph=True)
+    with pytest.raises(RuntimeError, match="twice|cannot be differentiated"):
+        (dx.sum() + dw.sum()).backward()
+
+
+def test_layers_without_gradients_and_with_some_wanted():
+    x, res, w, dh, dy = norm_inputs(BF16, 30, 72)
+    want = P.residual_norm_fwd(x, res, w, p=0.3, seed=2)
+    for t in (x, res, w):
+        t.requires_grad_()
+        h, y = P.residual_norm(x, res, w, p=0.3, seed=2)
+        assert torch.equal(h, want[0]) and torch.equal(y, want[1]) and h.requires_grad and y.requires_grad
+        g, = torch.autograd.grad((h, y), t, (dh, dy))
+        all_ = P.residual_norm_bwd(dh, dy, want[0], w.detach(), p=0.3, seed=2)
+        assert torch.equal(g, all_[0 if t is x else 1 if t is res else 2].to(BF16))
+        h, y = P.residual_norm(x, None, w, p=0.3, seed=2)
+        if t is not res:
+            g, = torch.autograd.grad((h, y), t, (dh, dy))
+            all_ = P.residual_norm_bwd(dh, dy, h.detach(), w.detach(), p=0.3, seed=2)
+            assert torch.equal(g, all_[0 if t is x else 2].to(BF16))
+        with torch.no_grad():
+            h, y = P.residual_norm(x, res, w, p=0.3, seed=2)
+            assert not h.requires_grad and not P.dropout(x, 0.5, 1).requires_grad
+        t.requires_grad_(False)
+    with torch.inference_mode():
+        h, y = P.residual_norm(x, res, w, p=0.3, seed=2)
+        assert torch.equal(y, want[1]) and P.dropout(h, 0.5, 1).is_inference()
+
+
 def test_dropout_keeps_nothing_and_the_norm_its_sum():
     kept = []
     x, res, w, _, _ = norm_inputs(BF16, 20, 64)
