@@ -61,7 +61,7 @@ __device__ __forceinline__ void words(uint64_t block, Key key, uint32_t site, ui
 
 // A wave's 512 consecutive elements, eight to a lane, by accesses of 16 bytes that lie next to
 // each other (two of 32-bit elements 1 KB apart: 32 bytes of a lane at a time would bring
-// every line twice; 32768 x 1024 elements through dropout 56 us, so 41): element i of lane l
+// every line twice; 32768 x 1024 elements through dropout 56 us, so 43): element i of lane l
 // is 8 l + i of 16-bit elements, and 4 l + i, 256 + 4 l + i - 4 of 32-bit ones.
 constexpr int kWaveElements = kWave * 8;
 template <class T>

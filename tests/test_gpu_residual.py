@@ -197,6 +197,17 @@ def test_dropout_keeps_nothing_and_the_norm_its_sum():
     assert {t.data_ptr() for t in kept} == {h.data_ptr(), w.data_ptr()}
 
 
+def test_saved_tensors_kept_on_the_host():
+    x, res, w, dh, dy = (t.requires_grad_() for t in norm_inputs(BF16, 20, 64))
+    seed = torch.tensor([4], device="cuda")
+    with torch.autograd.graph.save_on_cpu():
+        h, y = P.residual_norm(x, res, w, p=0.25, seed=seed)
+        z = P.dropout(y, 0.5, seed, 1)
+    got = torch.autograd.grad((h, z), (x, res, w), (dh.detach(), dy.detach()))
+    want = P.residual_norm_bwd(dh.detach(), P.dropout_bwd(dy.detach(), 0.5, 4, 1), h.detach(), w.detach(), p=0.25, seed=4)
+    assert all(torch.equal(a, b.to(BF16)) for a, b in zip(got, want))
+
+
 def test_seeds_of_64_bits():
     x = randn(gen(9), 1000)
     assert torch.equal(P.dropout_fwd(x, 0.5, 2 ** 64 - 3), P.dropout_fwd(x, 0.5, -3))
@@ -215,6 +226,20 @@ def test_dropout_module():
     torch.manual_seed(0)
     assert torch.equal(a, d(x)) and not torch.equal(a, b)
     assert torch.equal(d(x, seed=5), dropped(x, 0.4, 5, 3)) and d.eval()(x) is x
+
+
+@pytest.mark.parametrize("reentrant", (False, True))
+def test_dropout_in_a_checkpoint(reentrant):
+    """What is computed again in the backward draws the same seed and so the same mask."""
+    from torch.utils.checkpoint import checkpoint
+    net = torch.nn.Sequential(torch.nn.Linear(32, 64), P.Dropout(0.4), torch.nn.ReLU(), P.Dropout(0.2, site=1), torch.nn.Linear(64, 8)).cuda()
+    x = randn(gen(15), 20, 32).requires_grad_()
+    torch.manual_seed(3)
+    want = torch.autograd.grad(net(x).square().sum(), [x, *net.parameters()])
+    torch.manual_seed(3)
+    checkpoint(net, x, use_reentrant=reentrant).square().sum().backward()
+    for t, g in zip([x, *net.parameters()], want):
+        assert torch.equal(t.grad, g)
 
 
 def test_seed_on_the_device_in_a_replayed_graph():
