@@ -71,9 +71,10 @@ int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x
  *   code = 127 a / m to the nearest whole number, halves to the even one,
  *   scale = r m / 127,  so that code * scale stands for y;
  * for rows8 a = x and r = 1.  Codes are exact: of 16-bit storage no rounding
- * lies between h and w and their code (of fp32 those of 64-bit products).  A
- * row of zeros has codes and scale 0; a row that holds a NaN or an infinity
- * (in h w) has codes 0 and scale NaN.
+ * lies between h and w and their code, as long as h w is not below fp32's
+ * normal range (of fp32 those of 64-bit products).  A row of zeros has codes
+ * and scale 0; a row that holds a NaN or an infinity (in h w) has codes 0 and
+ * scale NaN.
  *
  * Backward, from dh and dy, the gradients of h and y (dh may be NULL: 0):
  *   g = dy w,  dresidual = dh + r (g - h r^2 mean(g h)),
