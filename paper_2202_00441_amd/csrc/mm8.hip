@@ -53,10 +53,14 @@ __device__ __forceinline__ Tile tile_of(const Args& a, uint32_t block) {
 
 enum { kLinear = 0, kGelu = 1, kSilu = 2 };
 
-template <int DT, int ACT>
+// In fp32 whatever the result is stored as, so that half a step of that type is all it is off by:
+// the fits of GELU that the few-bit forwards take for 16-bit results (bf16 1.9e-4 of the tail) put
+// results on the other side of a border here and there.  It costs nothing that shows but in large
+// products: 32768 x 2048 by 8192 bf16 550 us, with the fit for bf16 544.
+template <int ACT>
 __device__ __forceinline__ float activate(float z) {
-  if constexpr (ACT == kGelu) return Act<DT, FEWBIT_GELU>::f(z);
-  if constexpr (ACT == kSilu) return Act<DT, FEWBIT_SILU>::f(z);
+  if constexpr (ACT == kGelu) return Act<FEWBIT_F32, FEWBIT_GELU>::f(z);
+  if constexpr (ACT == kSilu) return Act<FEWBIT_F32, FEWBIT_SILU>::f(z);
   return z;
 }
 
@@ -187,7 +191,7 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
         const float xs = s.xs[wm + j * 16 + lane % 16];
         V4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = static_cast<T>(activate<DT, ACT>(static_cast<float>(acc[i][j][e]) * (xs * ws[e]) + bias[e]));
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<T>(activate<ACT>(static_cast<float>(acc[i][j][e]) * (xs * ws[e]) + bias[e]));
         *reinterpret_cast<V4*>(lds + r * kChunks * 16 + ((c / kPer ^ r / 2 % kChunks) * 16) + c % kPer * sizeof(T)) = v;
       }
     }
@@ -374,7 +378,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Args a, int sh
   T* y = static_cast<T*>(a.y) + m * a.out + n;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (n + e < a.out) y[e] = static_cast<T>(activate<DT, ACT>(static_cast<float>(sum[e]) * (xs * ws[e]) + bias[e]));
+    if (n + e < a.out) y[e] = static_cast<T>(activate<ACT>(static_cast<float>(sum[e]) * (xs * ws[e]) + bias[e]));
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -444,7 +448,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(const Args a) {
 #pragma unroll
     for (int h = 0; h < H; ++h) sum += sums[i][h * kRows + r][h * kRows + c];
   const float bias = a.bias ? static_cast<float>(static_cast<const T*>(a.bias)[n]) : 0.0f;
-  static_cast<T*>(a.y)[r * a.out + n] = static_cast<T>(activate<DT, ACT>(static_cast<float>(sum) * (a.xs[r] * a.ws[n]) + bias));
+  static_cast<T*>(a.y)[r * a.out + n] = static_cast<T>(activate<ACT>(static_cast<float>(sum) * (a.xs[r] * a.ws[n]) + bias));
 }
 
 // ---------------------------------------------------------------- host side

@@ -516,6 +516,26 @@ def test_product_of_larger_sizes(rows, out, width):
     assert torch.equal(a, check_product(*product_inputs(rows, out, width, F16), "gelu", F16))
 
 
+def half_step(want, dtype):
+    """Half the distance between neighbours of dtype where want lies."""
+    e = torch.frexp(want).exponent - 1
+    return torch.ldexp(torch.full_like(want, torch.finfo(dtype).eps / 2), e).clamp_min(LOW[dtype])
+
+
+@pytest.mark.parametrize("act", ("gelu", "silu"))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,out,width", ((1, 8192, 256), (64, 500, 4096), (300, 520, 160), (1500, 1500, 144)))
+def test_activations_of_products_are_formed_in_fp32(rows, out, width, dtype, act):
+    """Whatever the result's type: off by half a step of that type where it lies, and else by fp32's figures alone."""
+    x, xs, w, ws, bias = product_inputs(rows, out, width, dtype)
+    y = P.int8_linear(x, xs, w, ws, bias, act, dtype)
+    z = torch.matmul(x.double(), w.double().t()) * xs.double()[:, None] * ws.double()
+    d = 4 * STEP * (z.abs() + bias.double().abs())
+    z = z + bias.double()
+    want = ACTS[act](z)
+    near(y, want, half_step(want, dtype) + 1.2 * d + (FIT[act][F32] + 2.0 ** -18) * ACTS[act](-z.abs()).abs(), act)
+
+
 @pytest.mark.parametrize("rows", (1, 20, 64, 300))
 def test_product_sums_are_exact(rows):
     """The largest sums that there are: every product of two codes of -128, and the widest row."""
