@@ -38,7 +38,8 @@ class Cache:
 
 
 def _eps(norm: torch.nn.RMSNorm) -> float:
-    return torch.finfo(norm.weight.dtype).eps if norm.eps is None else norm.eps
+    """What the norm adds to the mean square; without a number of its own torch's takes fp32's step for 16-bit types too."""
+    return torch.finfo(torch.promote_types(norm.weight.dtype, torch.float32)).eps if norm.eps is None else norm.eps
 
 
 class Block(torch.nn.Module):

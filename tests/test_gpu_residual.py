@@ -711,6 +711,40 @@ def test_stack_without_dropping_is_the_plain_stack():
         assert float((s.double() - t.double()).norm() / t.double().norm()) < 0.06
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+def test_epsilon_of_norms_without_one(dtype):
+    """The fused passes take the one that torch's norm takes: of rows whose mean square is near it, the same numbers.
+    Each side is off by half a step and 36 roundings."""
+    norm = torch.nn.RMSNorm(256).cuda().to(dtype)
+    x = torch.cat([randn(gen(51), 8, 256) * s for s in (1.0, 0.02, 1e-3, 1e-4)]).to(dtype)
+    want = norm(x).detach().double()
+    near(P.residual_norm_fwd(x, None, norm.weight.detach(), TR._eps(norm))[1], want, 2 * (U[dtype] + 36 * STEP) * want.abs() + 2 * LOW[dtype], "y")
+
+
+def small_stack(p):
+    """Embeddings as small as they usually are: rows whose mean square is 4e-4."""
+    model = stack(p)
+    with torch.no_grad():
+        model.embed.weight.mul_(0.02)
+    return model.bfloat16().eval()
+
+
+def test_stack_of_small_embeddings():
+    """The fused passes (dropout=0.0), torch's norms (None), serving from a cache and serving in 8 bits are one function:
+    the bounds of test_stack_without_dropping_is_the_plain_stack and test_serving_in_8_bits."""
+    a, b = small_stack(0.0), small_stack(None)
+    b.load_state_dict(a.state_dict())
+    tokens = torch.randint(0, 50, (3, 60), device="cuda", generator=gen(9))
+    with torch.no_grad():
+        want = b(tokens).float()
+        fused = a(tokens).float()
+    off = lambda y: float((y.float() - want).norm() / want.norm())
+    assert off(fused) < 0.03
+    assert off(a.extend(tokens, a.cache(3, 100))) < 0.03 and off(b.extend(tokens, b.cache(3, 100))) < 0.03
+    served = TR.Int8Transformer(a)
+    assert off(served.extend(tokens, served.cache(3, 100))) < 0.06
+
+
 def test_stack_with_dropout_against_plain_formulas():
     """Gradients of the whole stack with the masks formed apart: in fp64 on the same weights, bf16's roundings of about
     ten tensors in a row in each of two layers between the two, with random signs."""

@@ -258,3 +258,15 @@ def test_host_seed_follows_torchs_generator():
     a = [draw_seed() for _ in range(3)]
     torch.manual_seed(5)
     assert a == [draw_seed() for _ in range(3)] and len(set(a)) == 3 and all(-2 ** 63 <= v < 2 ** 63 for v in a)
+
+
+@pytest.mark.parametrize("dtype", (torch.bfloat16, torch.float16, torch.float32, torch.float64))
+def test_epsilon_of_norms_without_one(dtype):
+    """What torch's norm takes: a value so small that the mean square hardly counts beside it gives it away.
+    2^-14 squared is 1/32 of fp32's step: half a step of the type and a few roundings of 32 bits (or 64)."""
+    norm = torch.nn.RMSNorm(64).to(dtype)
+    x = torch.full((64,), 2.0 ** -14, dtype=dtype)
+    want = 2.0 ** -14 * (2.0 ** -28 + transformer._eps(norm)) ** -0.5
+    assert abs(float(norm(x)[0].detach()) / want - 1) < max(torch.finfo(dtype).eps / 2, 2.0 ** -24) + 8 * 2.0 ** -24
+    norm.eps = 0.25
+    assert transformer._eps(norm) == 0.25
