@@ -17,6 +17,13 @@ struct Drop {
   bool some = false;        // elements are dropped
 };
 
+// The place of a seed's ordinary device tensor.
+const int64_t* seed_of(const at::Tensor& seed, const at::Tensor& ref) {
+  TORCH_CHECK_TYPE(seed.scalar_type() == at::kLong, "seed must be a whole number or an int64 tensor");
+  TORCH_CHECK_VALUE(seed.numel() == 1 && seed.device() == ref.device(), "a seed's tensor must have one element and be on the data's device");
+  return seed.data_ptr<int64_t>();
+}
+
 Drop drop_of(PyObject* const* args, const at::Tensor& ref) {
   Drop r;
   r.d.p = number(args[0], "p");
@@ -24,9 +31,7 @@ Drop drop_of(PyObject* const* args, const at::Tensor& ref) {
   r.some = std::nearbyint(r.d.p * 65536.0) > 0.0;
   if (THPVariable_Check(args[1])) {
     r.seed = tensor(args[1], "seed");
-    TORCH_CHECK_TYPE(r.seed.scalar_type() == at::kLong, "seed must be a whole number or an int64 tensor");
-    TORCH_CHECK_VALUE(r.seed.numel() == 1 && r.seed.device() == ref.device(), "a seed's tensor must have one element and be on the data's device");
-    r.d.seed_at = r.seed.data_ptr<int64_t>();
+    r.d.seed_at = seed_of(r.seed, ref);
   } else {
     // of either sign, or above 2^63
     const unsigned long long above = PyLong_Check(args[1]) ? PyLong_AsUnsignedLongLong(args[1]) : 0;
@@ -362,14 +367,21 @@ bool ordinary(PyObject* o) {
 bool dense(const at::Tensor& t) { return t.is_contiguous() && reinterpret_cast<uintptr_t>(t.data_ptr()) % 16 == 0; }
 at::Tensor made_dense(const at::Tensor& t) { return dense(t) ? t : t.clone(at::MemoryFormat::Contiguous); }
 
+// A hook may have put anything in the place of a saved tensor, so what a backward takes is checked
+// as the arguments of a call are.
+void check_ordinary(at::ArrayRef<at::Tensor> all) {
+  for (const at::Tensor& t : all) TORCH_CHECK_VALUE(!t.defined() || plain(t), "saved tensors and gradients must be ordinary device tensors");
+}
+
 // What a backward needs of the dropout; the seed's tensor, if it is one, is saved last.
 void keep(AutogradContext* ctx, const fewbit_drop& d) {
   ctx->saved_data["p"] = d.p;
   ctx->saved_data["seed"] = d.seed;
   ctx->saved_data["site"] = static_cast<int64_t>(d.site);
 }
-fewbit_drop kept(AutogradContext* ctx, const at::Tensor& seed_at) {
-  return {ctx->saved_data["p"].toDouble(), ctx->saved_data["seed"].toInt(), seed_at.defined() ? seed_at.data_ptr<int64_t>() : nullptr,
+fewbit_drop kept(AutogradContext* ctx, const at::Tensor& seed_at, const at::Tensor& ref) {
+  check_ordinary({seed_at});
+  return {ctx->saved_data["p"].toDouble(), ctx->saved_data["seed"].toInt(), seed_at.defined() ? seed_of(seed_at, ref) : nullptr,
           static_cast<uint32_t>(ctx->saved_data["site"].toInt()), 0};
 }
 
@@ -385,13 +397,13 @@ struct DropoutFn : torch::autograd::Function<DropoutFn> {
   // The same function of the gradient, to any order.
   static variable_list backward(AutogradContext* ctx, variable_list grads) {
     const variable_list saved = ctx->get_saved_variables();
+    check_ordinary({grads[0]});
     const at::Tensor seed_at = saved.empty() ? at::Tensor() : saved[0], dy = made_dense(grads[0]);
-    const fewbit_drop d = kept(ctx, seed_at);
+    const fewbit_drop d = kept(ctx, seed_at, dy);
     at::Tensor dx;
     if (at::GradMode::is_enabled()) {
       dx = apply(dy, &d, &seed_at);
     } else {
-      TORCH_CHECK_VALUE(plain(dy), "the gradient must be an ordinary device tensor");
       int rc;
       dx = run_dropout(dy, d, rc);
       if (rc != FEWBIT_OK) throw_status(rc, "fewbit_dropout");
@@ -435,13 +447,22 @@ struct ResidualNormFn : torch::autograd::Function<ResidualNormFn> {
     if (!grads[0].defined() && !grads[1].defined()) return none;
     const variable_list saved = ctx->get_saved_variables();
     const at::Tensor &h = saved[0], &w = saved[1];
+    at::Tensor dh = grads[0], dy = grads[1];
+    check_ordinary({h, w, dh, dy});
     fewbit_rnorm a{};
+    TORCH_CHECK_TYPE(storage_type(h) >= 0, "h must be float32, float16 or bfloat16");
     rows_of(h, a);
     a.dtype = a.dw_dtype = storage_type(h);
     a.eps = static_cast<float>(ctx->saved_data["eps"].toDouble());
-    a.drop = kept(ctx, saved.size() > 2 ? saved[2] : at::Tensor());
-    at::Tensor dh = grads[0], dy = grads[1].defined() ? grads[1] : at::zeros_like(h);
-    for (const at::Tensor& t : {h, w, dh, dy}) TORCH_CHECK_VALUE(!t.defined() || plain(t), "saved tensors and gradients must be ordinary device tensors");
+    a.drop = kept(ctx, saved.size() > 2 ? saved[2] : at::Tensor(), h);
+    check_same(w, "weight", h, "h");
+    check_shape(w, "weight", {h.size(-1)});
+    for (const at::Tensor& t : {dh, dy}) {
+      if (!t.defined()) continue;
+      check_same(t, "the gradient", h, "h");
+      check_shape(t, "the gradient", h.sizes());
+    }
+    if (!dy.defined()) dy = at::zeros_like(h);
     if (dh.defined() && !strides_fit(dh, a.dh_stride)) {
       dh = dh.clone(at::MemoryFormat::Contiguous);
       strides_of(dh, "dh", a.dh_stride);

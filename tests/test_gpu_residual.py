@@ -208,6 +208,34 @@ def test_saved_tensors_kept_on_the_host():
     assert all(torch.equal(a, b.to(BF16)) for a, b in zip(got, want))
 
 
+@pytest.mark.parametrize("change,kind", ((lambda t: t.cpu(), ValueError), (lambda t: t.float(), TypeError), (lambda t: t.half(), TypeError),
+                                         (lambda t: t.flatten()[:8].clone(), ValueError)))
+def test_saved_tensors_that_a_hook_replaced(change, kind):
+    """On the host, of another type or shape: refused before anything is launched, one of them alone too."""
+    x, res, w, dh, dy = norm_inputs(BF16, 20, 64)
+    leaves = [t.requires_grad_() for t in (x, res, w)]
+    for which in (lambda t: True, lambda t: t.dim() == 2, lambda t: t.dim() == 1):
+        with torch.autograd.graph.saved_tensors_hooks(lambda t: change(t) if t.is_floating_point() and which(t) else t, lambda t: t):
+            h, y = P.residual_norm(x, res, w, p=0.25, seed=5)
+        for grads in ((dh.detach(), dy.detach()), (dh.detach(), None), (None, dy.detach())):
+            outs, grads = zip(*((o, g) for o, g in zip((h, y), grads) if g is not None))
+            with pytest.raises((kind, ValueError)):
+                torch.autograd.grad(outs, leaves, grads, retain_graph=True)
+
+
+@pytest.mark.parametrize("change,kind", ((lambda t: t.cpu(), ValueError), (lambda t: t.int(), TypeError), (lambda t: t.expand(2).clone(), ValueError)))
+@pytest.mark.parametrize("create_graph", (False, True))
+def test_saved_seeds_that_a_hook_replaced(change, kind, create_graph):
+    x, res, w, dh, dy = norm_inputs(BF16, 20, 64)
+    seed = torch.tensor([5], device="cuda")
+    with torch.autograd.graph.saved_tensors_hooks(lambda t: t if t.is_floating_point() else change(t), lambda t: t):
+        h, _ = P.residual_norm(x.requires_grad_(), res, w, p=0.25, seed=seed)
+        z = P.dropout(x, 0.5, seed)
+    for t, g in ((h, dh), (z, dy)):
+        with pytest.raises(kind):
+            torch.autograd.grad(t, x, g, create_graph=create_graph)
+
+
 def test_seeds_of_64_bits():
     x = randn(gen(9), 1000)
     assert torch.equal(P.dropout_fwd(x, 0.5, 2 ** 64 - 3), P.dropout_fwd(x, 0.5, -3))
