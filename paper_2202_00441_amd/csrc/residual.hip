@@ -280,8 +280,9 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_fwd_kernel(const
       }
       E::template store_bytes<kNt>(codes, place(c), lane, v);
     }
+    // of a row of zeros 0 also without eps, where size is infinite
     if (lane == 0 && (WAVES == 1 || wave == 0))
-      a.scale[row] = finite ? size * static_cast<float>(m) / 127.0f : __builtin_nanf("");
+      a.scale[row] = !finite ? __builtin_nanf("") : zero ? 0.0f : size * static_cast<float>(m) / 127.0f;
   }
 }
 

@@ -502,6 +502,25 @@ def test_codes_of_rows_without_numbers(dtype):
     assert P.residual_norm_int8(x, None, w)[2].isnan().all()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("width", (8, 2048, 4104, 32768))
+def test_rows_of_zeros_without_epsilon(width, dtype):
+    """Codes and scale 0, and the product of such a row its bias."""
+    x, res, w, _, _ = norm_inputs(dtype, 3, width)
+    x[1], res[1] = 0.0, 0.0
+    for residual in (res, None):
+        h, codes, scale = P.residual_norm_int8(x, residual, w, 0.0)
+        want, m = codes_of(h.double() * w.double())
+        size = h.double().square().mean(-1).rsqrt() * m / 127
+        size[1] = 0.0
+        assert torch.equal(codes, want) and scale[1] == 0
+        near(scale, size, 40 * STEP * size, "scale")
+    if width % 16 == 0:
+        bias = randn(gen(1), 16, dtype=dtype)
+        ones = torch.ones(16, width, dtype=torch.int8, device="cuda")
+        assert torch.equal(P.int8_linear(codes, scale, ones, torch.ones(16, device="cuda"), bias, dtype=dtype)[1], bias)
+
+
 ACTS = {None: lambda z: z, "gelu": lambda z: z * torch.special.ndtr(z), "silu": lambda z: z * torch.sigmoid(z)}
 FIT = {"gelu": {BF16: 1.9e-4, F16: 5.5e-5, F32: 1.3e-6}, "silu": {BF16: 0.0, F16: 0.0, F32: 0.0}}
 
