@@ -151,7 +151,7 @@ __device__ __forceinline__ u32x2 codes_of(const float (&a)[8], const A (&wide)[8
       k -= 127.0 * b < k * top;             // t may lie on the other side of a whole number
       const double twice = 254.0 * b, border = (2 * k + 1) * top;
       k += twice > border || (twice == border && (k & 1));
-      k = x < 0.0f ? -k : k;
+      k = y < 0 ? -k : k;                   // (x may have no sign left)
 #pragma unroll
       for (int i = 0; i < 8; ++i) q[i] = at == i ? static_cast<uint32_t>(k) : q[i];
     }
@@ -280,9 +280,15 @@ __global__ __launch_bounds__(Group<WAVES>::kThreads) void rnorm_fwd_kernel(const
       }
       E::template store_bytes<kNt>(codes, place(c), lane, v);
     }
-    // of a row of zeros 0 also without eps, where size is infinite
-    if (lane == 0 && (WAVES == 1 || wave == 0))
-      a.scale[row] = !finite ? __builtin_nanf("") : zero ? 0.0f : size * static_cast<float>(m) / 127.0f;
+    // of a row of zeros 0 also without eps, where size is infinite; m of 64 bits may have no place in 32
+    if (lane == 0 && (WAVES == 1 || wave == 0)) {
+      float scale;
+      if constexpr (kWide)
+        scale = static_cast<float>(static_cast<double>(size) * m / 127.0);
+      else
+        scale = size * m / 127.0f;
+      a.scale[row] = !finite ? __builtin_nanf("") : zero ? 0.0f : scale;
+    }
   }
 }
 

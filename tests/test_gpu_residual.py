@@ -521,6 +521,24 @@ def test_rows_of_zeros_without_epsilon(width, dtype):
         assert torch.equal(P.int8_linear(codes, scale, ones, torch.ones(16, device="cuda"), bias, dtype=dtype)[1], bias)
 
 
+@pytest.mark.parametrize("width", (16, 512, 2056, 8200))
+def test_codes_of_products_below_fp32s_range(width):
+    """Of 32-bit storage products of 64 bits count: signs, codes and scales where fp32's products would be subnormal or 0.
+    Squares vanish beside eps here, so r = eps^-1/2; the scale's roundings, and 2^-149 where it is subnormal itself."""
+    g = gen(width)
+    x = torch.randn(7, width, generator=g, device="cuda") * torch.exp2(torch.tensor([-80.0, -90, -100, -110, -120, -80, -100], device="cuda"))[:, None]
+    w = torch.randn(width, generator=g, device="cuda") * 2.0 ** -50
+    x[5] *= torch.exp2(-20 * torch.rand(width, generator=g, device="cuda"))
+    x[6, 3:] = 0.0
+    for eps in (1e-6, 1e-20):
+        h, codes, scale = P.residual_norm_int8(x, None, w, eps)
+        a = x.double() * w.double()
+        want, m = codes_of(a)
+        assert torch.equal(codes, want) and (want.abs().amax(1) == 127).all()
+        size = m / 127 * float(torch.tensor(eps)) ** -0.5
+        near(scale, size, 40 * STEP * size + 2.0 ** -149, "scale")
+
+
 ACTS = {None: lambda z: z, "gelu": lambda z: z * torch.special.ndtr(z), "silu": lambda z: z * torch.sigmoid(z)}
 FIT = {"gelu": {BF16: 1.9e-4, F16: 5.5e-5, F32: 1.3e-6}, "silu": {BF16: 0.0, F16: 0.0, F32: 0.0}}
 
