@@ -128,8 +128,9 @@ int fewbit_rnorm_bwd(const fewbit_rnorm* a, const void* dh, const void* dy, cons
 /*
  *   y[m][n] = act(x_scale[m] w_scale[n] sum_k x[m][k] w[n][k] + bias[n])
  * The sum is exact (32-bit integers: width up to 131056); the rest is formed in
- * fp32 and rounded once.  act: FEWBIT_MM8_LINEAR, or FEWBIT_GELU or FEWBIT_SILU
- * of fewbit.h.
+ * fp32, the sum times x_scale first, and rounded once: x_scale from 2^-126 to
+ * 2^96, where such a product neither vanishes nor overflows, w_scale any.
+ * act: FEWBIT_MM8_LINEAR, or FEWBIT_GELU or FEWBIT_SILU of fewbit.h.
  *
  * x and w have `width` contiguous codes per row and rows that start at
  * multiples of 16 bytes, at most FEWBIT_MM8_STRIDE apart; the scales are dense, bias (may

@@ -64,6 +64,13 @@ __device__ __forceinline__ float activate(float z) {
   return z;
 }
 
+// A result from its sum.  The sum meets one scale after the other: the product of both may pass
+// fp32's range at either end where the result does not.
+template <int ACT>
+__device__ __forceinline__ float finished(int sum, float xs, float ws, float bias) {
+  return activate<ACT>(static_cast<float>(sum) * xs * ws + bias);
+}
+
 // Rows from a matrix of codes into LDS, 128 bytes of each, by buffer loads that go there
 // directly: a wave's load brings 8 rows of 8 chunks of 16 bytes.  Chunk c of row r lies at
 // c ^ (r / 2 % 8), so that 16 lanes that read a chunk of 16 rows meet 64 different banks.
@@ -191,7 +198,7 @@ __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, i
         const float xs = s.xs[wm + j * 16 + lane % 16];
         V4 v;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = static_cast<T>(activate<ACT>(static_cast<float>(acc[i][j][e]) * (xs * ws[e]) + bias[e]));
+        for (int e = 0; e < 4; ++e) v[e] = static_cast<T>(finished<ACT>(acc[i][j][e], xs, ws[e], bias[e]));
         *reinterpret_cast<V4*>(lds + r * kChunks * 16 + ((c / kPer ^ r / 2 % kChunks) * 16) + c % kPer * sizeof(T)) = v;
       }
     }
@@ -378,7 +385,7 @@ __global__ __launch_bounds__(kJoinThreads) void join_kernel(const Args a, int sh
   T* y = static_cast<T*>(a.y) + m * a.out + n;
 #pragma unroll
   for (int e = 0; e < 4; ++e)
-    if (n + e < a.out) y[e] = static_cast<T>(activate<ACT>(static_cast<float>(sum[e]) * (xs * ws[e]) + bias[e]));
+    if (n + e < a.out) y[e] = static_cast<T>(finished<ACT>(sum[e], xs, ws[e], bias[e]));
 }
 
 // ---------------------------------------------------------------- few tokens
@@ -448,7 +455,7 @@ __global__ __launch_bounds__(kFewWaves* kWave) void few_kernel(const Args a) {
 #pragma unroll
     for (int h = 0; h < H; ++h) sum += sums[i][h * kRows + r][h * kRows + c];
   const float bias = a.bias ? static_cast<float>(static_cast<const T*>(a.bias)[n]) : 0.0f;
-  static_cast<T*>(a.y)[r * a.out + n] = static_cast<T>(activate<ACT>(static_cast<float>(sum) * (a.xs[r] * a.ws[n]) + bias));
+  static_cast<T*>(a.y)[r * a.out + n] = static_cast<T>(finished<ACT>(sum, a.xs[r], a.ws[n], bias));
 }
 
 // ---------------------------------------------------------------- host side

@@ -191,8 +191,9 @@ def int8_linear(x, x_scale, weight, weight_scale, bias=None, act=None, dtype=tor
     x [..., width] and weight [out, width] int8 (as quantize_rows gives them),
     x_scale [...] and weight_scale [out] fp32, bias [out] of dtype or None; act
     None, "gelu" or "silu".  width a multiple of 16 up to 131056; rows contiguous,
-    even steps of a multiple of 16 bytes and of at most 2^23 apart; sums are exact.
-    Not differentiable."""
+    even steps of a multiple of 16 bytes and of at most 2^23 apart; scales dense, from
+    multiples of 16 bytes on, x_scale between 2^-126 and 2^96; sums are exact.  Not
+    differentiable."""
     if act not in _ACTS:
         raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
     if dtype not in _TYPES:

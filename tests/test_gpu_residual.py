@@ -650,6 +650,30 @@ def test_product_of_rows_far_apart(rows):
     torch.cuda.empty_cache()
 
 
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,out,width", ((1, 100, 2048), (5, 100, 2048), (64, 500, 4096), (300, 520, 160), (1500, 1500, 144)))
+def test_scales_of_any_size(rows, out, width, dtype):
+    """Small ones whose product is below fp32's range while the result is not, large ones whose product is above it, and
+    sums of 0 by those: the bias."""
+    x, _, w, _, bias = product_inputs(rows, out, width, dtype)
+    x[-1] = 0
+    z = torch.matmul(x.double(), w.double().t())
+    g = gen(rows)
+    low = F16 if dtype is F16 else F32
+    for xs, ws in ((1e-20, 1e-21), (2.0 ** -126, 0.5), (1e-22, 1e-17), (1e28, 1e-30), (1e-30, 1e28), (1e-37, 1e30)):
+        xs, ws = xs * (1 + torch.rand(rows, generator=g, device="cuda")), ws * (1 + torch.rand(out, generator=g, device="cuda"))
+        y = P.int8_linear(x, xs, w, ws, None, None, dtype)
+        want = z * xs.double()[:, None] * ws.double()
+        small = {BF16: 2.0 ** -134, F16: LOW[F16], F32: 2.0 ** -150}[dtype] + 2.0 ** -149      # where results are subnormal
+        most = torch.finfo(dtype).max
+        fits = want.abs() < 0.99 * most
+        near(torch.where(fits, y, 0.0), torch.where(fits, want, 0.0), (U[dtype] + 4 * STEP) * want.abs() + small, f"{float(xs[0])} {float(ws[0])}")
+        assert (y[want.abs() > 1.01 * most].isinf()).all()
+    large = torch.full((rows,), 1e29, device="cuda"), torch.full((out,), 1e30, device="cuda")
+    y = P.int8_linear(x, large[0], w, large[1], bias, None, dtype)
+    assert torch.equal(y[z == 0], bias.expand_as(y)[z == 0])
+
+
 def test_product_of_nothing_and_of_scales_that_are_not_numbers():
     x, xs, w, ws, b = product_inputs(20, 40, 64, BF16)
     assert P.int8_linear(x[:0], xs[:0], w, ws, b).shape == (0, 40)
