@@ -204,7 +204,9 @@ def int8_linear(x, x_scale, weight, weight_scale, bias=None, act=None, dtype=tor
 class Int8Linear(torch.nn.Module):
     """A torch.nn.Linear on a device for serving, its weight in 8-bit integers with a
     scale per channel; what comes in is laid out in 8 bits too, with a scale per
-    row, unless it comes as (codes, scale).  act: "gelu" or "silu" after the bias."""
+    row, unless it comes as (codes, scale).  act: "gelu" or "silu" after the bias.
+    Converted to another type (.half(), .to(dtype)) its results have that type, its
+    scales stay fp32."""
 
     def __init__(self, linear: torch.nn.Linear, act: str | None = None):
         super().__init__()
@@ -217,6 +219,14 @@ class Int8Linear(torch.nn.Module):
         self.register_buffer("weight_scale", scale)
         self.register_buffer("bias", None if linear.bias is None else linear.bias.detach().clone())
         self.act, self.dtype = act, linear.weight.dtype
+
+    def _apply(self, fn, recurse=True):
+        scale = self.weight_scale
+        super()._apply(fn, recurse)
+        if self.weight_scale.dtype != scale.dtype:
+            self.weight_scale = scale.to(self.weight_scale.device)
+        self.dtype = fn(torch.empty(0, dtype=self.dtype, device=scale.device)).dtype
+        return self
 
     def forward(self, x, scale=None):
         if scale is None:

@@ -782,6 +782,29 @@ def test_layers_of_8_bits():
     assert torch.equal(q(x.transpose(0, 1)), y.transpose(0, 1))
 
 
+@pytest.mark.parametrize("bias", (True, False))
+def test_layer_of_8_bits_converted(bias):
+    """Scales stay fp32, whatever the module becomes; the result's type follows, and so do copies and devices."""
+    import copy
+    lin = torch.nn.Linear(64, 48, bias=bias).cuda().bfloat16()
+    q = P.Int8Linear(lin, "silu")
+    x = randn(gen(61), 5, 64, dtype=BF16)
+    codes, scale = P.quantize_rows(x)
+    kept = q.weight_scale.clone()
+    for convert, dtype in ((lambda m: m.half(), F16), (lambda m: m.to(F32), F32), (lambda m: m.bfloat16(), BF16),
+                           (lambda m: torch.nn.Sequential(m).to(F16)[0], F16), (lambda m: copy.deepcopy(m).cpu().cuda().float(), F32)):
+        q = convert(q)
+        assert q.weight_scale.dtype is F32 and torch.equal(q.weight_scale, kept) and q.weight.dtype is torch.int8
+        b = None if not bias else lin.bias.detach().to(dtype)
+        y = q(codes, scale)
+        assert y.dtype is dtype and torch.equal(y, P.int8_linear(codes, scale, q.weight, kept, b, "silu", dtype))
+        assert q(x.to(dtype)).dtype is dtype
+    assert q.cpu().weight_scale.device.type == "cpu" and q.to("meta").weight_scale.is_meta
+    assert q.to_empty(device="cuda").weight_scale.dtype is F32
+    with pytest.raises(TypeError, match="dtype"):
+        q.double()(codes, scale)
+
+
 def stack(p, **more):
     torch.manual_seed(3)
     return TR.Transformer(50, 256, 2, 4, 2, 512, most=128, dropout=p, **more).cuda()
