@@ -13,6 +13,7 @@ tokens.
 from __future__ import annotations
 
 import argparse
+import copy
 import json
 import time
 
@@ -93,6 +94,18 @@ class Block(torch.nn.Module):
         return attended
 
 
+def _alias(module: torch.nn.Module) -> torch.nn.Module:
+    """A module without children on the same memory, with parameters of its own: converting or moving one of the two
+    leaves the other as it is."""
+    other = copy.copy(module)
+    other._parameters = {name: None if p is None else _alias_parameter(p) for name, p in module._parameters.items()}
+    return other
+
+
+def _alias_parameter(p: torch.nn.Parameter) -> torch.nn.Parameter:
+    return torch.nn.Parameter(p.detach(), p.requires_grad)
+
+
 class Int8Block(Block):
     """A block for serving: its four products in 8-bit integers, each from tokens that are laid out in 8 bits
     where they arise (by the norm, or by quantize_rows after attention and activation)."""
@@ -100,7 +113,8 @@ class Int8Block(Block):
     def __init__(self, block: Block):
         torch.nn.Module.__init__(self)
         self.heads, self.kv_heads, self.head_dim = block.heads, block.kv_heads, block.head_dim
-        self.norm1, self.norm2, self.q_norm, self.k_norm = block.norm1, block.norm2, block.q_norm, block.k_norm
+        self.norm1, self.norm2 = _alias(block.norm1), _alias(block.norm2)
+        self.q_norm, self.k_norm = _alias_parameter(block.q_norm), _alias_parameter(block.k_norm)
         name = _act_name(block.act)
         self.qkv, self.out = Int8Linear(block.qkv), Int8Linear(block.out)
         self.up, self.down = Int8Linear(block.up, name), Int8Linear(block.down)
@@ -212,12 +226,12 @@ class Transformer(torch.nn.Module):
 
 
 class Int8Transformer(Transformer):
-    """A transformer for serving, the blocks' products in 8-bit integers; embeddings, norms and head are the
-    model's own.  cache, extend and generate are as there."""
+    """A transformer for serving, the blocks' products in 8-bit integers; embeddings, norms and head are on the
+    model's own memory until one of the two is converted or moved.  cache, extend and generate are as there."""
 
     def __init__(self, model: Transformer):
         torch.nn.Module.__init__(self)
-        self.embed, self.norm, self.head, self.most = model.embed, model.norm, model.head, model.most
+        self.embed, self.norm, self.head, self.most = _alias(model.embed), _alias(model.norm), _alias(model.head), model.most
         self.blocks = torch.nn.ModuleList(Int8Block(b) for b in model.blocks)
         self._tables = None
 

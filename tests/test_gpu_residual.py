@@ -958,6 +958,26 @@ def test_serving_in_8_bits(bits, act):
         served(tokens)
 
 
+def test_stack_in_8_bits_converted():
+    """Another type for the served stack, and the model that it was made of as it was."""
+    model = stack(None).bfloat16().eval()
+    tokens = torch.randint(0, 50, (2, 30), device="cuda", generator=gen(10))
+    with torch.no_grad():
+        want = model(tokens)
+    served = TR.Int8Transformer(model).half()
+    got = served.extend(tokens, served.cache(2, 40))
+    assert got.dtype is F16 and float((got.float() - want.float()).norm() / want.float().norm()) < 0.06
+    with torch.no_grad():
+        assert all(t.dtype is BF16 for t in model.parameters()) and torch.equal(model(tokens), want)
+    served.cpu()
+    assert all(t.is_cuda for t in model.parameters())
+    # one memory all the same: a step of training is served
+    served = TR.Int8Transformer(model)
+    with torch.no_grad():
+        model.head.weight.mul_(2.0)
+    assert torch.equal(served.head.weight, model.head.weight) and served.embed.weight.data_ptr() == model.embed.weight.data_ptr()
+
+
 def test_serving_step_in_a_replayed_graph():
     """A norm, a product, an activation, another layout and product, captured together."""
     g = gen(41)
