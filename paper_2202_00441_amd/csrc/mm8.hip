@@ -538,12 +538,16 @@ int64_t pitch_of(const fewbit_mm8* a) { return (a->out + 3) / 4 * 4; }
 template <int DT, int ACT, int SIDE, int WM, int WN, int STAGES>
 hipError_t start_tiles(const Args& r, const Plan& p, hipStream_t s) {
   constexpr int kThreads = SIDE / WM * (SIDE / WN) * kWave;
-  if (p.shares == 1) return launch(tile_kernel<DT, ACT, SIDE, SIDE, WM, WN, STAGES, false>, dim3(r.tiles), kThreads, s, r);
-  // the sums do not depend on the types and the activation
-  const hipError_t e = launch(tile_kernel<FEWBIT_F32, kLinear, SIDE, SIDE, WM, WN, STAGES, true>, dim3(r.tiles, p.shares), kThreads, s, r);
-  if (e != hipSuccess) return e;
-  const int64_t quads = r.rows * (r.pitch / 4);
-  return launch(join_kernel<DT, ACT>, dim3(static_cast<unsigned>((quads + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, s, r, p.shares);
+  if constexpr (SIDE == 64) {       // the tiles that shares are offered for
+    if (p.shares > 1) {
+      // the sums do not depend on the types and the activation
+      const hipError_t e = launch(tile_kernel<FEWBIT_F32, kLinear, SIDE, SIDE, WM, WN, STAGES, true>, dim3(r.tiles, p.shares), kThreads, s, r);
+      if (e != hipSuccess) return e;
+      const int64_t quads = r.rows * (r.pitch / 4);
+      return launch(join_kernel<DT, ACT>, dim3(static_cast<unsigned>((quads + kJoinThreads - 1) / kJoinThreads)), kJoinThreads, s, r, p.shares);
+    }
+  }
+  return launch(tile_kernel<DT, ACT, SIDE, SIDE, WM, WN, STAGES, false>, dim3(r.tiles), kThreads, s, r);
 }
 template <int DT, int ACT, int H>
 hipError_t start_few(const Args& r, hipStream_t s) {

@@ -4,6 +4,7 @@ products (no GPU, nothing is launched), and of the dropout generator's definitio
 import ctypes as C
 import os
 import re
+import shutil
 import subprocess
 import tempfile
 
@@ -218,6 +219,15 @@ def test_product_workspace_is_asked_for_and_checked(rows, out, width):
     assert 0 <= need <= 256 << 20
     if need:
         assert product(a, work=None) == E_NULL and product(a, size=need - 1) == E_INVALID
+
+
+@pytest.mark.skipif(shutil.which("nm") is None, reason="needs nm")
+def test_library_holds_the_kernels_that_a_product_may_take():
+    """Shares of the width are offered for tiles of 64 alone (the last argument: whether there are shares)."""
+    names = subprocess.run(["nm", "-C", P.LIB_PATH], capture_output=True, text=True, check=True).stdout
+    tiles = {tuple(t.replace(" ", "").split(",")) for t in re.findall(r"::tile_kernel<([^>]*)>", names)}
+    assert {t[2] for t in tiles if t[-1] == "false"} == {"64", "128", "256"}
+    assert {t[2] for t in tiles if t[-1] == "true"} == {"64"}
 
 
 # ---------------------------------------------------------------- the package's calls
