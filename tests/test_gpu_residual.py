@@ -601,6 +601,27 @@ def test_activations_of_products_are_formed_in_fp32(rows, out, width, dtype, act
     near(y, want, half_step(want, dtype) + 1.2 * d + (FIT[act][F32] + 2.0 ** -18) * ACTS[act](-z.abs()).abs(), act)
 
 
+@pytest.mark.parametrize("act", (None, "gelu", "silu"))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,out,width", ((1500, 1500, 144), (1025, 2004, 272), (2600, 3002, 160), (1000, 4100, 400), (4100, 4100, 160), (7001, 4099, 144),
+                                            (5003, 4104, 272), (64, 1001, 4112), (200, 260, 8192), (20, 250, 16400)))
+def test_product_of_every_tile_and_type(rows, out, width, dtype, act):
+    """Tiles of 128 (one and two workgroups a CU) and of 256, and shares of the width; rows that end inside a tile, results
+    whose rows are aligned to 2, 4, 8 and 16 bytes."""
+    x, xs, w, ws, bias = product_inputs(rows, out, width, dtype)
+    y = check_product(x, xs, w, ws, bias, act, dtype)
+    assert torch.equal(y, P.int8_linear(x, xs, w, ws, bias, act, dtype))
+
+
+@pytest.mark.parametrize("act", (None, "gelu", "silu"))
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("rows,out,width", ((1, 2048, 8192), (8, 1000, 4096), (5, 1600, 8176), (7, 333, 272), (4, 500, 8192), (1, 100, 2048), (2, 900, 16368),
+                                            (3, 300, 16384), (3, 17, 1040), (1, 5, 400)))
+def test_product_of_few_rows_with_places_of_the_width(rows, out, width, dtype, act):
+    """Two and four places in an operand's rows, each with codes of its own, some past its first run or cut short."""
+    check_product(*product_inputs(rows, out, width, dtype), act, dtype)
+
+
 @pytest.mark.parametrize("rows", (1, 20, 64, 300))
 def test_product_sums_are_exact(rows):
     """The largest sums that there are: every product of two codes of -128, and the widest row."""
