@@ -52,7 +52,8 @@ typedef struct fewbit_drop {
     uint32_t reserved;            /* must be 0                                 */
 } fewbit_drop;
 
-/* y may be x; both are 16-byte aligned.  n stays below 2^37. */
+/* y may be x; both are 16-byte aligned.  n is at most 2^37 - 8192
+ * (a launch has fewer than 2^32 threads). */
 int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x, void* y,
                    void* stream);
 

@@ -544,10 +544,13 @@ hipError_t start_back(const fewbit_rnorm* a, const BwdArgs& r, hipStream_t s) {
   return r.drop.border ? start_bwd<DT, true>(a, r, s) : start_bwd<DT, false>(a, r, s);
 }
 
+int64_t drop_groups(int64_t n) {
+  constexpr int64_t kPer = int64_t{8} * kDropBlocks * kDropThreads;
+  return (n + kPer - 1) / kPer;
+}
 template <int DT>
 hipError_t start_drop(const void* x, void* y, int64_t n, const Drop& d, hipStream_t s) {
-  constexpr int64_t kPer = int64_t{8} * kDropBlocks * kDropThreads;
-  return launch(drop_kernel<DT>, dim3(static_cast<unsigned>((n + kPer - 1) / kPer)), kDropThreads, s, x, y, n, d);
+  return launch(drop_kernel<DT>, dim3(static_cast<unsigned>(drop_groups(n))), kDropThreads, s, x, y, n, d);
 }
 
 }  // namespace
@@ -558,7 +561,7 @@ extern "C" int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, co
   Drop r{};
   int rc = drop_of(*d, r);
   if (rc != FEWBIT_OK) return rc;
-  if (n < 0 || n >= int64_t{1} << 37) return FEWBIT_E_INVALID;
+  if (n < 0 || n >= int64_t{1} << 37 || !fits_launch(drop_groups(n), kDropThreads)) return FEWBIT_E_INVALID;
   if (n == 0) return FEWBIT_OK;
   if (!x || !y) return FEWBIT_E_NULL;
   if (misaligned(x) || misaligned(y)) return FEWBIT_E_ALIGN;

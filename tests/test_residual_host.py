@@ -122,6 +122,13 @@ def test_dropout_arguments():
     assert dropout(drop(), n=0, x=None, y=None) == OK
 
 
+def test_dropout_of_more_than_a_launch_takes():
+    """256 threads for 8192 elements: at 2^37 - 8191 they would be 2^32.  (Without a device a call that is not refused
+    ends at the stream.)"""
+    assert dropout(drop(), n=(1 << 37) - 8191) == dropout(drop(), n=(1 << 37) - 1) == E_INVALID
+    assert dropout(drop(), n=(1 << 37) - 8192, x=None) == E_NULL
+
+
 # ---------------------------------------------------------------- residual and norm
 def rnorm(**changes):
     a = Rnorm(dtype=P.BF16, width=64, outer=2, rows=5, eps=1e-6, drop=drop(p=0.0))
