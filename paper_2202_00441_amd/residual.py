@@ -204,7 +204,8 @@ def int8_linear(x, x_scale, weight, weight_scale, bias=None, act=None, dtype=tor
 class Int8Linear(torch.nn.Module):
     """A torch.nn.Linear on a device for serving, its weight in 8-bit integers with a
     scale per channel; what comes in is laid out in 8 bits too, with a scale per
-    row, unless it comes as (codes, scale).  act: "gelu" or "silu" after the bias.
+    row, unless it comes as (codes, scale).  in_features a multiple of 16 up to 32768,
+    the longest rows that quantize_rows takes.  act: "gelu" or "silu" after the bias.
     Converted to another type (.half(), .to(dtype)) its results have that type, its
     scales stay fp32."""
 
@@ -212,8 +213,8 @@ class Int8Linear(torch.nn.Module):
         super().__init__()
         if act not in _ACTS:
             raise ValueError(f"act must be None, 'gelu' or 'silu', not {act!r}")
-        if linear.in_features % 16 != 0:
-            raise ValueError("in_features must be a multiple of 16")
+        if linear.in_features % 16 != 0 or not 0 < linear.in_features <= 32768:
+            raise ValueError("in_features must be a multiple of 16 up to 32768")
         codes, scale = quantize_rows(_rows(linear.weight.detach()))
         self.register_buffer("weight", codes)
         self.register_buffer("weight_scale", scale)

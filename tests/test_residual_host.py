@@ -269,6 +269,12 @@ def test_modules_check_their_arguments():
     assert P.Dropout(0.5).eval()(x) is x and P.Dropout(0.0)(x) is x
 
 
+@pytest.mark.parametrize("width", (0, 32784, 131056))
+def test_layer_of_8_bits_takes_rows_that_are_laid_out(width):
+    with pytest.raises(ValueError, match="in_features must be a multiple of 16 up to 32768"):
+        P.Int8Linear(torch.nn.Linear(width, 4, device="meta"))
+
+
 def test_host_seed_follows_torchs_generator():
     from paper_2202_00441_amd.residual import draw_seed
     torch.manual_seed(5)
