@@ -15,6 +15,9 @@
  *                  bits with a scale per token
  *   rows8          any rows in 8 bits with a scale per row
  *   mm8            the product of such rows with weights in 8 bits
+ *
+ * Pointers are 16-byte aligned, but for rnorm's and rows8's `scale`, dw and a
+ * seed's place, which need no more than their type.
  */
 #ifndef FEWBIT_RESIDUAL_H
 #define FEWBIT_RESIDUAL_H
@@ -82,7 +85,8 @@ int fewbit_dropout(const fewbit_drop* d, int32_t dtype, int64_t n, const void* x
  *   dx = dropout of dresidual before it is rounded,  dw = sum over rows of dy h r.
  *
  * Squares are formed in fp32: magnitudes past 2^63 make r 0, those below 2^-63
- * count only as far as eps lets them.
+ * count only as far as eps lets them.  With eps = 0 a row of zeros has no r: y
+ * and the gradients are NaN, as the formulas make them (codes and scale are 0).
  *
  * x, residual, dh and dy have `width` contiguous elements per row and strides
  * {outer, row} in elements; rows start at multiples of 16 bytes.  h, y, dx and

@@ -2,8 +2,8 @@
 // per channel, bias and activation in the epilogue.
 //
 // Formulas in fewbit_residual.h.  Few tokens are bound by the weights' bytes, many by the
-// matrix instructions (and the power that they draw: 32768 x 8192 by 2048 takes 405 us, 2.7
-// POP/s).  The matrix instruction takes 16 channels by 16 tokens by
+// matrix instructions (and the power that they draw: 32768 x 8192 by 2048 takes 400 us in a loop
+// over the same codes, 2.7 POP/s, and 435 over several of full range).  The matrix instruction takes 16 channels by 16 tokens by
 // 64 bytes of both: its first operand holds, in lane l, 16 consecutive codes of channel l %
 // 16, the second those of token l % 16, and a lane of the result has four consecutive
 // channels of one token.  Which 64 codes an instruction takes does not matter as long as
@@ -174,10 +174,11 @@ __device__ __forceinline__ void store_rows(const int8_t* lds, T* y, int64_t out,
 
 // A wave's WM tokens by WN channels from its registers to y, through BYTES of LDS of its own, so
 // that it stores whole runs of a row.  Element (r, c) lies in chunk c / kPer ^ r / 2 % kChunks of
-// row r: 16 lanes that write a chunk of 16 rows meet 64 different banks.  KEEP: results stay in
-// the caches, as those of tiles of 256 hardly would (32768 x 2048 by 8192 channels with GELU 628
-// us, past the caches 600, and with the channels' scales read once instead of for every 16
-// tokens 542).
+// row r, so that lanes that write a chunk of 16 rows meet different banks (all but: of 16-bit
+// results four cycles of conflicts are counted for every write of 8 bytes a lane).  KEEP: results
+// stay in the caches, as those of tiles of 256 hardly would (32768 x 2048 by 8192 channels with
+// GELU 628 us, past the caches 600, and with the channels' scales read once instead of for every
+// 16 tokens 542, 550 with the fit for fp32).
 template <int DT, int ACT, int WM, int WN, int BYTES, bool KEEP, int BM, int BN>
 __device__ __forceinline__ void finish(const Args& a, const Scales<BM, BN>& s, int8_t* lds, int64_t m0, int64_t n0, int wm, int wn, int lane,
                                        const i32x4 (&acc)[WN / 16][WM / 16]) {

@@ -112,7 +112,7 @@ def residual_norm_fwd(x, residual, weight, eps=1e-6, p=0.0, seed=0, site=0):
     pass: (h, y), dense.
 
     x [..., width], residual alike or None (nothing is added; without dropout
-    either h is x itself), weight [width], fp32, fp16 or bf16; width a multiple
+    either h is x itself), weight [width], all fp32, all fp16 or all bf16; width a multiple
     of 8 up to 32768; rows contiguous, from multiples of 16 bytes on, the axes
     before the last two one step apart (x[:, a:b] and views of a projection
     are)."""
